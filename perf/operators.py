@@ -11,7 +11,7 @@ Kinds of cases:
             queries rotated beside them; the new tokens are then read back as the values that they stand for;
 - "attend"  queries against the cache: one token, a draft tree, a piece of a prompt, a whole prompt;
 - "fork"    sequences are forked into drafts, which get pages for their next tokens (a shared last page is copied);
-            what the drafts see there is read back, and the next pass begins by dropping them;
+            the last tokens that the drafts share are read back, and the next pass begins by dropping the drafts;
 - "accept"  a draft tree's accepted tokens are moved together, the rest is given back, the accepted ones are read back.
 
 Sizes: the head layouts of the 7B- and 70B-shaped stacks of `synth.py` (32 and 32 heads, 64 and 8 heads of 128) and
@@ -151,7 +151,7 @@ def work(case):
         rows = case["rows"] * case["branches"]
         tables = 8 * sum(case["branches"] * -(-(n + case["new"]) // case["page"]) for n, _ in lens)
         copied = 2 * each * sum(case["branches"] * (n % case["page"]) for n, _ in lens)
-        back = rows * (case["page"] + case["new"]) * (each + case["groups"] * 4 * d)
+        back = rows * case["page"] * (each + case["groups"] * 4 * d)
         return {"bytes": tables + copied + back, "flops": 0}
     kept = sum(_kept(case, b) for b in range(case["rows"]))
     return {"bytes": kept * (3 * each + case["groups"] * 4 * d), "flops": 0}
@@ -244,8 +244,8 @@ def prepare(case, seed):
         s["src"] = _int([b for b in range(rows) for _ in range(forks)])
         s["dst"] = _int([rows + i for i in range(rows * forks)])
         s["none"], s["add"] = _int([0] * (rows * forks)), _int([add] * (rows * forks))
-        s["starts"], s["back"], s["first"] = None, add + page, rows
-        s["most"], s["total"] = s["back"], s["back"] * rows * forks
+        s["before"] = _int([n for n, _ in lens for _ in range(forks)])
+        s["starts"], s["first"], s["total"] = None, rows, page * rows * forks
     else:
         s["rows"], s["base"], s["add"] = _int(list(range(rows))), _int([n for n, _ in lens]), _int([add] * rows)
         counts = [_kept(case, b) for b in range(rows)]
@@ -253,7 +253,7 @@ def prepare(case, seed):
         s["keep"], s["counts"] = _int(keep), _int(counts)
         s["after"] = s["base"] + s["counts"]
         s["starts"] = _int([sum(counts[:i]) for i in range(rows + 1)])
-        s["most"], s["total"], s["first"] = max(counts), sum(counts), 0
+        s["total"], s["first"] = sum(counts), 0
     return s
 
 
@@ -295,9 +295,9 @@ def _values(code, scale):
     return (x * factor[..., None]).flatten(-2)
 
 
-def _new(s):
-    """(row, position) of each packed token: the last tokens of the rows from s["first"] on."""
-    lens = s["lens"][s.get("first", 0):].long()
+def _new(s, lens=None):
+    """(row, position, number) of each packed token: the last tokens of the rows from s["first"] on."""
+    lens = (s["lens"] if lens is None else lens).long()
     rows = lens.numel()
     t = torch.arange(s["total"], device=DEV)
     if s["starts"] is None:
@@ -316,8 +316,8 @@ def _place(s, row, at):
     return s["table"][s.get("first", 0):][row, at // page].long(), at % page
 
 
-def _read(s):
-    row, at, _ = _new(s)
+def _read(s, lens=None):
+    row, at, _ = _new(s, lens)
     p, o = _place(s, row, at)
     kq, ks, vq, vs = (x[p, :, o] for x in s["cache"])
     return _values(kq, ks).to(torch.bfloat16), _values(vq, vs).to(torch.bfloat16)
@@ -416,7 +416,7 @@ def _plain_extend(s, rows, add):
     fresh = got.gather(1, last[:, None])[:, 0]
     there = torch.where(copies, fresh, mine)                         # a row that copies nothing copies its page onto itself
     at, to = mine[open_], there[open_]
-    for x in s["cache"]:
+    for x in s["cache"]:                                             # (slots behind the sequence's end hold nothing yet)
         x[to] = x[at]
     s["refs"].index_add_(0, mine.clamp(min=0), -copies.to(torch.int32))
     s["refs"].index_add_(0, torch.where(wants, got, 0).flatten(), wants.flatten().to(torch.int32))
@@ -439,7 +439,7 @@ def _plain_fork_case(s):
     _plain_release(s, s["dst"], s["none"])
     _plain_fork(s, s["src"], s["dst"])
     _plain_extend(s, s["dst"], s["add"])
-    return [s["table"], s["lens"], s["refs"], *_read(s)]
+    return [s["table"], s["lens"], s["refs"], *_read(s, s["before"])]
 
 
 def _plain_accept(s):
@@ -468,12 +468,13 @@ def _own(s):
         binding.mxfp4_kv_release(pool, cache, table, lens, s["dst"], s["none"])
         binding.mxfp4_kv_fork(pool, cache, table, lens, s["src"], s["dst"])
         binding.mxfp4_kv_extend(pool, cache, table, lens, s["dst"], s["add"])
+        return [table, lens, s["refs"], *binding.mxfp4_kv_read(cache, table[first:], s["before"], s["total"])]
     else:
         binding.mxfp4_kv_release(pool, cache, table, lens, s["rows"], s["base"])
         binding.mxfp4_kv_extend(pool, cache, table, lens, s["rows"], s["add"])
         binding.mxfp4_kv_compact(cache, table, s["base"], s["keep"], s["counts"])
         binding.mxfp4_kv_release(pool, cache, table, lens, s["rows"], s["after"])
-    return [table, lens, s["refs"], *binding.mxfp4_kv_read(cache, table[first:], lens[first:], s["total"], starts=s["starts"])]
+    return [table, lens, s["refs"], *binding.mxfp4_kv_read(cache, table, lens, s["total"], starts=s["starts"])]
 
 
 def run(s):
@@ -558,9 +559,29 @@ def _exact_attend(case, s):
     return [torch.cat(outs)] + ([torch.cat(lses)] if case["lse"] else [])
 
 
+def _exact_pages(case, s):
+    """The values that the first pass reads back: moved as they were (table, lengths and counts are whole numbers)."""
+    page, rows, free = case["page"], case["rows"], torch.nonzero(s["refs"] == 0).flatten().tolist()
+    k, v = [], []
+    for b, n in enumerate(s["lens"].tolist()[:rows]):
+        mine = s["table"][b].tolist()
+        if case["kind"] == "fork":
+            at = list(range(n - page, n)) * case["branches"]
+        else:
+            for w in range(-(-n // page), -(-(n + case["new"]) // page)):
+                mine[w] = free.pop(0)
+            at = [n + i for i in s["keep"][b].tolist()[: _kept(case, b)]]
+        p = torch.tensor([mine[i // page] for i in at], device=DEV)
+        o = torch.tensor([i % page for i in at], device=DEV)
+        kq, ks, vq, vs = (x[p, :, o] for x in s["cache"])
+        k.append(_meaning(kq, ks))
+        v.append(_meaning(vq, vs))
+    return [None, None, None, torch.cat(k), torch.cat(v)]
+
+
 def exact(case, seed):
     if case["kind"] in ("fork", "accept"):
-        return None                                                  # numbers are moved, none is computed
+        return _exact_pages(case, prepare(case, seed))
     if case["kind"] == "attend" and work(case)["flops"] * max(1, case["new"] / 64) > 3e14:
         return None
     s = prepare(case, seed)
