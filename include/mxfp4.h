@@ -33,6 +33,9 @@
  *   Next to the method: mxfp4_bf16_gemm* (the unquantised target's linear), mxfp4_e4m3_*,
  *     mxfp4_e2m3_* and mxfp4_fmt_* (8-, 6- and 2-bit element formats as drafts), mxfp4_woq_gemm_t
  *     (the value side of attention over a cache held in the same format).
+ *   The paged cache of a speculative decoder, in the same format: mxfp4_kv_append, mxfp4_kv_read,
+ *     mxfp4_kv_attention (+ _workspace_bytes), and its pages: mxfp4_kv_fork, mxfp4_kv_extend,
+ *     mxfp4_kv_release, mxfp4_kv_compact, mxfp4_kv_copy_pages.
  *   Diagnostics, for tests and measurements only: mxfp4_*_path (a kernel family forced),
  *     mxfp4_direct_cast_bits / mxfp4_*_direct_cast_bits (the integer rounding rule in place of the
  *     convert instruction), mxfp4_dequant*, mxfp4_diag_stream_*.
@@ -227,6 +230,174 @@ int mxfp4_woq_gemm_t(const void* x_bf16, int64_t M, int64_t ldx,
                      const void* q_packed, const void* scales_e8m0, int64_t N, int64_t K,
                      void* y_bf16, int64_t ldy,
                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A cache of keys and values held in MXFP4 (section 5 names the quantised attention cache as the next step
+ * of the method and gives no procedure; the reading: one token per row, 32-element blocks along the head
+ * dimension, a token cast on its own by the rule of mxfp4_direct_cast when it is stored), in pages.
+ *   kq, vq  uint8 [pages][heads][page][dim / 2]     ks, vs  uint8 [pages][heads][page][dim / 32]
+ * A page of one head is an ordinary q/s pair with one token per row.  `page` tokens per page: a power of two
+ * in [16, 1024]; dim 32, 64, 96, 128, 192 or 256; heads 1 .. 65535; all four arrays 16-byte aligned.  Pages lie
+ * page_stride_q / page_stride_s bytes apart (multiples of 16, at least a page), so that the layers of a
+ * model can share one array [pages][layers][heads]...: a layer's cache starts at its own offset.
+ * Position p of sequence b is slot p % page of page table[b * ldt + p / page].  A page number outside
+ * [0, pages) and a position outside [0, width * page) name no token: nothing is stored or moved
+ * there, nothing is read, and attention leaves it out.  No call reads or writes out of bounds for any contents of
+ * table, lens, starts, keep, counts, src or dst.
+ */
+typedef struct mxfp4_kv_cache {
+    void* kq;
+    void* ks;
+    void* vq;
+    void* vs;
+    int64_t pages;
+    int64_t page_stride_q;
+    int64_t page_stride_s;
+    int32_t heads;
+    int32_t page;
+    int32_t dim;
+    int32_t reserved; /* 0 */
+} mxfp4_kv_cache;
+
+/*
+ * A batch: `rows` sequences, their tables, lengths and new tokens.  The new tokens of sequence b are rows
+ * starts[b] .. starts[b + 1] - 1 of the packed tensors [tokens][...] (starts: rows + 1 ascending numbers,
+ * starts[0] = 0) and stand at the last positions of the sequence, lens[b] - n .. lens[b] - 1.  starts = NULL:
+ * the same number each, tokens / rows (tokens must be a multiple of rows).  table, lens and starts are
+ * device pointers; width is the number of entries of a table row.
+ */
+typedef struct mxfp4_kv_rows {
+    const int32_t* table;
+    int64_t ldt;
+    int64_t width;
+    const int32_t* lens;
+    const int32_t* starts;
+    int64_t rows;
+    int64_t tokens;
+} mxfp4_kv_rows;
+
+/*
+ * Rotary positions for mxfp4_kv_append: the first `dim` elements of a head (dim a multiple of 16, at most
+ * the head dimension; 0: no rotation) are turned in pairs (i, i + dim / 2) by the angle of row p of the
+ * tables, cos_f32 and sin_f32 [length][dim / 2], 16-byte aligned: (a, b) -> (a cos - b sin, b cos + a sin), each product rounded
+ * to FP32, one rounding to BF16 at the end.  p is the token's position in its sequence, or
+ * positions[t] (device, [tokens]) where that is given, as for the nodes of a draft tree.  A p outside the tables makes
+ * the token's turned elements NaN.
+ */
+typedef struct mxfp4_kv_rope {
+    const float* cos_f32;
+    const float* sin_f32;
+    const int32_t* positions;
+    int64_t length;
+    int64_t dim;
+} mxfp4_kv_rope;
+
+/* A BF16 tensor [tokens][heads][dim] with strides in elements (multiples of 8, the last one 1), 16-byte aligned. */
+typedef struct mxfp4_kv_tensor {
+    void* data;
+    int64_t token;
+    int64_t head;
+} mxfp4_kv_tensor;
+
+/*
+ * Stores the batch's new tokens: keys (turned by `rope`, NULL: as they are) and values are cast and put into their pages.
+ * q (NULL: none), [tokens][q_heads][dim], is turned the same way into q_out, which must not overlap it.  The bits in
+ * the cache are those of mxfp4_direct_cast on the (turned, BF16) rows.  tokens = 0 is a no-op.  Two tokens
+ * with the same place (sequences that share a page, see mxfp4_kv_extend) leave either one's bits.
+ */
+int mxfp4_kv_append(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, const mxfp4_kv_tensor* k,
+                    const mxfp4_kv_tensor* v, const mxfp4_kv_tensor* q, const mxfp4_kv_tensor* q_out,
+                    int64_t q_heads, const mxfp4_kv_rope* rope, void* stream);
+
+/* The batch's last tokens as the values that the cache holds, BF16 [tokens][heads][dim]; a token that is
+ * nowhere (see above) reads as zeros.  k_out or v_out may be NULL. */
+int mxfp4_kv_read(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, const mxfp4_kv_tensor* k_out,
+                  const mxfp4_kv_tensor* v_out, void* stream);
+
+/*
+ * Attention of the batch's new tokens over the cache:  out[t][h] = sum_j softmax_j(scale q[t][h] . k[j]) v[j] over the
+ * positions j that token t sees, k and v of head h / (q_heads / heads).  FP32 sums and softmax, attention
+ * weights rounded to BF16 before they meet the values, BF16 result.
+ *   causal != 0   token i of a sequence, at position p, sees j <= p
+ *   window > 0    and only j > p - window (any causal)
+ *   tree          (device, [tokens], NULL: none) bit m of a token's word: it sees new token m of its
+ *                 sequence (at most 64 new tokens can be seen); earlier tokens are seen by all.  Takes the
+ *                 place of the causal rule.
+ *   lse_f32       (NULL: none) [tokens][q_heads]: the natural logarithm of the sum of exp(scale q . k)
+ * A token that sees nothing gives zeros and an lse of -infinity.  What a token does not see does not
+ * touch its result, NaN blocks included; a NaN block that it sees gives NaN.
+ *   workspace     mxfp4_kv_attention_workspace_bytes bytes, 16-byte aligned, the first MXFP4_KV_COUNTERS * 4 of them
+ *                 ZERO before the first call; every call leaves them zero.  Calls that overlap in time must not share it.
+ * q_heads is a multiple of cache->heads.  The summation order follows from the sizes, the lengths and
+ * starts: the same inputs give the same bits.
+ */
+#define MXFP4_KV_COUNTERS 16384
+typedef struct mxfp4_kv_attention_args {
+    mxfp4_kv_tensor q;
+    mxfp4_kv_tensor out;
+    float* lse_f32;
+    const uint64_t* tree;
+    int64_t q_heads;
+    int64_t window;
+    float scale;
+    int32_t causal;
+} mxfp4_kv_attention_args;
+size_t mxfp4_kv_attention_workspace_bytes(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, int64_t q_heads);
+int mxfp4_kv_attention(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, const mxfp4_kv_attention_args* args,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Who holds which page.  refs int32 [pages]: how many table entries name the page; free_bits uint32
+ * [(pages + 31) / 32]: bit p % 32 of word p / 32 is set where refs[p] is 0 (bits past the last page are clear).  Both are device arrays that
+ * the calls below keep; an empty cache has all refs 0.  `table` [any rows][ldt] and `lens` cover every sequence,
+ * `rows_list` (device, `count` distinct numbers in [0, rows)) names those that a call is about; entries outside
+ * are left out.  A row's first ceil(lens / page) entries are its pages, the others are -1.
+ */
+typedef struct mxfp4_kv_pool {
+    int32_t* refs;
+    uint32_t* free_bits;
+    int64_t pages;
+    int64_t page;
+    int32_t* table;
+    int64_t ldt;
+    int64_t width;
+    int64_t rows;
+    int32_t* lens;
+} mxfp4_kv_pool;
+
+/* dst[i] becomes a second owner of all that sequence src[i] holds (table, length; nothing is copied).  The dst rows
+ * are distinct, empty (lens 0) and no src. */
+int mxfp4_kv_fork(const mxfp4_kv_pool* pool, const int32_t* src, const int32_t* dst, int64_t count, void* stream);
+
+/*
+ * Makes room for add[i] more tokens of sequence rows_list[i] (they are stored by mxfp4_kv_append afterwards) and adds
+ * them to its length.  New pages are the free ones of the lowest numbers, in the order of rows_list.  A
+ * last page that is begun, not full and held by others too is replaced by a copy of its own (of the tokens in it), in
+ * that order, while others hold it.  `cache` (NULL: no copying, the caller has `copies`): arrays whose pages
+ * hold all layers.  copies (device, int32 [count][2]): (from, to) of each row's copied page, -1 where none.
+ * missing (device, int32 [1]): 0, or how many pages (or -1: a row would pass its table's width) are missing; then
+ * nothing was changed.  count <= 4096; add >= 0.
+ */
+int mxfp4_kv_extend(const mxfp4_kv_pool* pool, const mxfp4_kv_cache* cache, const int32_t* rows_list,
+                    const int32_t* add, int64_t count, int32_t* copies, int32_t* missing, void* stream);
+
+/* Cuts sequence rows_list[i] down to its first min(lens, keep[i]) tokens and gives back the pages behind them (0: all of
+ * it).  A page is free when its last holder gives it back. */
+int mxfp4_kv_release(const mxfp4_kv_pool* pool, const int32_t* rows_list, const int32_t* keep, int64_t count,
+                     void* stream);
+
+/*
+ * Moves tokens of each sequence together: position base[b] + keep[b * ldk + i] goes to base[b] + i, i = 0 .. counts[b] - 1 (at
+ * most ldk), in place, as when the accepted path of a draft tree is kept.  keep ascends strictly, from 0 on.
+ * Lengths are the caller's.  The pages from base on must not be shared (mxfp4_kv_extend sees to that).
+ */
+int mxfp4_kv_compact(const mxfp4_kv_cache* cache, const int32_t* table, int64_t ldt, int64_t width,
+                     const int32_t* base, const int32_t* keep, int64_t ldk, const int32_t* counts, int64_t rows, void* stream);
+
+/* Page src[i] is copied to page dst[i], i < count (device lists; entries outside the cache are left out; no dst
+ * is a src or another dst). */
+int mxfp4_kv_copy_pages(const mxfp4_kv_cache* cache, const int32_t* src, const int32_t* dst, int64_t count,
+                        void* stream);
 
 /*
  * Dequantise to BF16 (exact whenever 2^(scale-127) * 6 is a normal BF16 number): the inverse

@@ -11,7 +11,7 @@ import contextlib
 import ctypes
 import os
 import warnings
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
@@ -35,6 +35,8 @@ EXPORTS = [
     "mxfp4_fmt_block_bytes", "mxfp4_fmt_direct_cast", "mxfp4_fmt_direct_cast_bits", "mxfp4_fmt_dequant",
     "mxfp4_fmt_woq_gemm", "mxfp4_fmt_woq_gemm_argmax",
     "mxfp4_woq_gemm_t_workspace_bytes", "mxfp4_woq_gemm_t",
+    "mxfp4_kv_append", "mxfp4_kv_read", "mxfp4_kv_attention_workspace_bytes", "mxfp4_kv_attention",
+    "mxfp4_kv_fork", "mxfp4_kv_extend", "mxfp4_kv_release", "mxfp4_kv_compact", "mxfp4_kv_copy_pages",
     "mxfp4_tile_repack_q_bytes", "mxfp4_tile_repack_s_bytes", "mxfp4_tile_repack", "mxfp4_woq_gemm_tiled",
     "mxfp4_woq_gemm_tiled_ws",
     "mxfp4_woq_gemm_tiled_argmax", "mxfp4_woq_gemm_tiled_verify", "mxfp4_woq_gemm_tiled_fused",
@@ -78,6 +80,39 @@ class ChainOpts(ctypes.Structure):
     _fields_ = [("wait_us", ctypes.c_int64), ("phantom_workgroups", ctypes.c_int32), ("mode", ctypes.c_int32)]
 
 
+class KvCacheDesc(ctypes.Structure):
+    """``mxfp4_kv_cache`` of the header, field for field (as the four below it)."""
+    _fields_ = [("kq", ctypes.c_void_p), ("ks", ctypes.c_void_p), ("vq", ctypes.c_void_p), ("vs", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page_stride_q", ctypes.c_int64), ("page_stride_s", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("page", ctypes.c_int32), ("dim", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class KvRowsDesc(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("ldt", ctypes.c_int64), ("width", ctypes.c_int64), ("lens", ctypes.c_void_p),
+                ("starts", ctypes.c_void_p), ("rows", ctypes.c_int64), ("tokens", ctypes.c_int64)]
+
+
+class KvRopeDesc(ctypes.Structure):
+    _fields_ = [("cos_f32", ctypes.c_void_p), ("sin_f32", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("length", ctypes.c_int64), ("dim", ctypes.c_int64)]
+
+
+class KvTensorDesc(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+class KvAttentionArgs(ctypes.Structure):
+    _fields_ = [("q", KvTensorDesc), ("out", KvTensorDesc), ("lse_f32", ctypes.c_void_p), ("tree", ctypes.c_void_p),
+                ("q_heads", ctypes.c_int64), ("window", ctypes.c_int64), ("scale", ctypes.c_float), ("causal", ctypes.c_int32)]
+
+
+class KvPoolDesc(ctypes.Structure):
+    _fields_ = [("refs", ctypes.c_void_p), ("free_bits", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page", ctypes.c_int64),
+                ("table", ctypes.c_void_p), ("ldt", ctypes.c_int64), ("width", ctypes.c_int64), ("rows", ctypes.c_int64),
+                ("lens", ctypes.c_void_p)]
+
+
+KV_COUNTERS = 16384
 CHAIN_STATUS_OFFSET = 4224
 CHAIN_AUTO, CHAIN_PERSISTENT, CHAIN_SEPARATE = 0, 1, 2
 
@@ -189,6 +224,20 @@ def load() -> ctypes.CDLL:
     lib.mxfp4_woq_gemm_chain_init.restype = i32
     lib.mxfp4_woq_gemm_chain.argtypes = [ctypes.POINTER(GemmDesc), i64, vp, sz, ctypes.POINTER(ChainOpts), vp]
     lib.mxfp4_woq_gemm_chain.restype = i32
+    ref = ctypes.POINTER
+    lib.mxfp4_kv_append.argtypes = [ref(KvCacheDesc), ref(KvRowsDesc), ref(KvTensorDesc), ref(KvTensorDesc), ref(KvTensorDesc),
+                                    ref(KvTensorDesc), i64, ref(KvRopeDesc), vp]
+    lib.mxfp4_kv_read.argtypes = [ref(KvCacheDesc), ref(KvRowsDesc), ref(KvTensorDesc), ref(KvTensorDesc), vp]
+    lib.mxfp4_kv_attention_workspace_bytes.argtypes = [ref(KvCacheDesc), ref(KvRowsDesc), i64]
+    lib.mxfp4_kv_attention_workspace_bytes.restype = sz
+    lib.mxfp4_kv_attention.argtypes = [ref(KvCacheDesc), ref(KvRowsDesc), ref(KvAttentionArgs), vp, sz, vp]
+    lib.mxfp4_kv_fork.argtypes = [ref(KvPoolDesc), vp, vp, i64, vp]
+    lib.mxfp4_kv_extend.argtypes = [ref(KvPoolDesc), ref(KvCacheDesc), vp, vp, i64, vp, vp, vp]
+    lib.mxfp4_kv_release.argtypes = [ref(KvPoolDesc), vp, vp, i64, vp]
+    lib.mxfp4_kv_compact.argtypes = [ref(KvCacheDesc), vp, i64, i64, vp, vp, i64, vp, i64, vp]
+    lib.mxfp4_kv_copy_pages.argtypes = [ref(KvCacheDesc), vp, vp, i64, vp]
+    for name in ("append", "read", "attention", "fork", "extend", "release", "compact", "copy_pages"):
+        getattr(lib, "mxfp4_kv_" + name).restype = i32
     lib.mxfp4_diag_stream_read.argtypes = [vp, sz, vp, vp]
     lib.mxfp4_diag_stream_copy.argtypes = [vp, vp, sz, vp]
     for name in ("mxfp4_direct_cast", "mxfp4_direct_cast_bits", "mxfp4_dequant", "mxfp4_dequant_hwcvt", "mxfp4_woq_gemm",
@@ -966,3 +1015,244 @@ def mxfp4_diag_stream_read(src: torch.Tensor, sink: torch.Tensor) -> None:
 def mxfp4_diag_stream_copy(src: torch.Tensor, dst: torch.Tensor) -> None:
     with _on(src.device):
         _check(load().mxfp4_diag_stream_copy(_ptr(src), _ptr(dst), src.numel() * src.element_size(), _stream()))
+
+
+# ---- the paged cache ------------------------------------------------------------------------------------------------
+
+
+class KvCache(NamedTuple):
+    """Keys and values in MXFP4: ``kq``, ``vq`` uint8 ``[pages, heads, page, dim/2]``, ``ks``, ``vs`` uint8
+    ``[pages, heads, page, dim/32]``; pages may lie further apart (``x[:, layer]`` of an array with all layers)."""
+    kq: torch.Tensor
+    ks: torch.Tensor
+    vq: torch.Tensor
+    vs: torch.Tensor
+
+
+class KvPool(NamedTuple):
+    """Who holds which page: ``refs`` int32 ``[pages]``, ``free`` int32 ``[ceil(pages / 32)]``, a bit per free page."""
+    refs: torch.Tensor
+    free: torch.Tensor
+
+
+def mxfp4_kv_cache(pages: int, heads: int, page: int, dim: int, layers: Optional[int] = None, device="cuda") -> KvCache:
+    """A cache of zeros.  With ``layers`` the arrays are ``[pages, layers, heads, page, ...]``; ``mxfp4_kv_layer`` gives a
+    layer's cache, ``mxfp4_kv_all_layers`` the one whose pages hold every layer (for extend, compact and copies)."""
+    mid = (heads,) if layers is None else (layers, heads)
+    return KvCache(*(torch.zeros((pages, *mid, page, dim // n), dtype=torch.uint8, device=device) for n in (2, 32, 2, 32)))
+
+
+def mxfp4_kv_layer(cache: KvCache, layer: int) -> KvCache:
+    return KvCache(*(x[:, layer] for x in cache))
+
+
+def mxfp4_kv_all_layers(cache: KvCache) -> KvCache:
+    return KvCache(*(x.flatten(1, 2) for x in cache))
+
+
+def mxfp4_kv_pool(pages: int, device="cuda") -> KvPool:
+    """A pool whose pages are all free."""
+    words = [-1] * (pages // 32) + ([(1 << pages % 32) - 1] if pages % 32 else [])
+    return KvPool(torch.zeros((pages,), dtype=torch.int32, device=device),
+                  torch.tensor(words, dtype=torch.int64).to(torch.int32).to(device))
+
+
+def _kv_cache_desc(c: KvCache) -> KvCacheDesc:
+    _dev(c.kq)
+    if c.kq.dim() != 4 or c.ks.dim() != 4:
+        raise ValueError("the cache's arrays are [pages, heads, page, dim/2] and [pages, heads, page, dim/32]")
+    pages, heads, page, half = c.kq.shape
+    for x, want, like in ((c.kq, half, c.kq), (c.ks, half // 16, c.ks), (c.vq, half, c.kq), (c.vs, half // 16, c.ks)):
+        if (x.dtype != torch.uint8 or tuple(x.shape) != (pages, heads, page, want) or x.device != c.kq.device
+                or x.stride()[1:] != (page * want, want, 1) or x.stride(0) != like.stride(0)):
+            raise ValueError("the cache's arrays must be uint8, of one number of pages, heads and tokens, on one device, and contiguous "
+                             "within a page: got %r" % [(tuple(x.shape), x.stride(), x.dtype) for x in c])
+    return KvCacheDesc(c.kq.data_ptr(), c.ks.data_ptr(), c.vq.data_ptr(), c.vs.data_ptr(), pages,
+                       c.kq.stride(0) if pages > 1 else heads * page * half, c.ks.stride(0) if pages > 1 else heads * page * (half // 16),
+                       heads, page, half * 2, 0)
+
+
+def _kv_ints(t: Optional[torch.Tensor], device, what: str, *shape) -> None:
+    if t is not None and (t.dtype != torch.int32 or t.device != device or t.dim() != len(shape) or not t.is_contiguous()
+                          or any(n is not None and m != n for m, n in zip(t.shape, shape))):
+        raise ValueError("%s must be a contiguous int32 tensor of shape %r on %s" % (what, shape, device))
+
+
+def _kv_table(table: torch.Tensor, device) -> int:
+    """The checks of a table; its row stride."""
+    if table.dtype != torch.int32 or table.device != device or table.dim() != 2 or (table.shape[1] > 1 and table.stride(1) != 1):
+        raise ValueError("table must be an int32 tensor [rows, width] on %s with contiguous rows" % (device,))
+    return table.stride(0) if table.shape[0] > 1 else table.shape[1]
+
+
+def _kv_rows_desc(table, lens, starts, tokens: int, device) -> KvRowsDesc:
+    ldt = _kv_table(table, device)
+    rows = table.shape[0]
+    _kv_ints(lens, device, "lens", rows)
+    _kv_ints(starts, device, "starts", rows + 1)
+    return KvRowsDesc(table.data_ptr(), ldt, table.shape[1], lens.data_ptr(), _ptr(starts), rows, tokens)
+
+
+def _kv_tensor_desc(t: torch.Tensor, what: str, device, tokens: int, heads: Optional[int], dim: int) -> KvTensorDesc:
+    if (t.dtype != torch.bfloat16 or t.device != device or t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != dim
+            or (heads is not None and t.shape[1] != heads) or t.stride(2) != 1):
+        raise ValueError("%s must be a BF16 tensor [%d, %s, %d] on %s with a contiguous last dimension: got %r" % (
+            what, tokens, "heads" if heads is None else heads, dim, device, tuple(t.shape)))
+    return KvTensorDesc(t.data_ptr(), t.stride(0) if tokens > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def mxfp4_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                    starts: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                    rope: Optional[Tuple[torch.Tensor, torch.Tensor]] = None, positions: Optional[torch.Tensor] = None,
+                    q_out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Stores the new tokens ``k``, ``v`` BF16 ``[tokens, heads, dim]`` of the sequences of ``table`` int32 ``[rows, width]`` at the
+    ends of their lengths ``lens`` int32 ``[rows]`` (which count them already).  ``rope``: (cos, sin) float32 ``[length, d/2]``
+    turns the first d elements of ``k``, and of ``q`` into the tensor that is returned, at the tokens' places or at
+    ``positions`` int32 ``[tokens]``.  ``starts`` int32 ``[rows + 1]``: whose rows are whose; None: the same number each."""
+    c = _kv_cache_desc(cache)
+    dev, tokens = cache.kq.device, k.shape[0]
+    b = _kv_rows_desc(table, lens, starts, tokens, dev)
+    kd, vd = _kv_tensor_desc(k, "k", dev, tokens, c.heads, c.dim), _kv_tensor_desc(v, "v", dev, tokens, c.heads, c.dim)
+    qd = od = rd = None
+    if q is not None:
+        qd = _kv_tensor_desc(q, "q", dev, tokens, None, c.dim)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        od = _kv_tensor_desc(q_out, "q_out", dev, tokens, q.shape[1], c.dim)
+    if rope is not None:
+        cos, sin = rope
+        if (cos.dim() != 2 or cos.shape != sin.shape or any(x.dtype != torch.float32 or x.device != dev or not x.is_contiguous() for x in rope)):
+            raise ValueError("rope must be two contiguous float32 tensors [length, d/2] on %s" % (dev,))
+        _kv_ints(positions, dev, "positions", tokens)
+        rd = KvRopeDesc(cos.data_ptr(), sin.data_ptr(), _ptr(positions), cos.shape[0], 2 * cos.shape[1])
+    elif positions is not None:
+        raise ValueError("positions without rope")
+    with _on(dev):
+        _check(load().mxfp4_kv_append(c, b, kd, vd, qd, od, 0 if q is None else q.shape[1], rd, _stream()))
+    return q_out if q is not None else None
+
+
+def mxfp4_kv_read(cache: KvCache, table: torch.Tensor, lens: torch.Tensor, tokens: int, starts: Optional[torch.Tensor] = None,
+                  out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The last tokens of the sequences, ``tokens`` in all, as the values that the cache holds: (k, v) BF16 ``[tokens, heads, dim]``."""
+    c = _kv_cache_desc(cache)
+    dev = cache.kq.device
+    b = _kv_rows_desc(table, lens, starts, tokens, dev)
+    k, v = out if out is not None else (torch.empty((tokens, c.heads, c.dim), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    kd, vd = _kv_tensor_desc(k, "k", dev, tokens, c.heads, c.dim), _kv_tensor_desc(v, "v", dev, tokens, c.heads, c.dim)
+    with _on(dev):
+        _check(load().mxfp4_kv_read(c, b, kd, vd, _stream()))
+    return k, v
+
+
+# One workspace for each stream that attention has run on, as a program would keep it: zeroed when it is made, left with its
+# counters at zero by every call, and used by calls that the stream runs one after the other.  Under graph capture a call gets one of
+# its own, which belongs to the graph.
+_kv_workspaces = {}
+
+
+def _kv_workspace(device: torch.device, stream: int, need: int) -> torch.Tensor:
+    if torch.cuda.is_current_stream_capturing():
+        return torch.zeros((need,), dtype=torch.uint8, device=device)
+    ws = _kv_workspaces.get((device.index, stream))
+    if ws is None or ws.numel() < need:
+        ws = _kv_workspaces[device.index, stream] = torch.zeros((need,), dtype=torch.uint8, device=device)
+    return ws
+
+
+def mxfp4_kv_attention_workspace_bytes(cache: KvCache, rows: int, tokens: int, q_heads: int) -> int:
+    """Bytes of a workspace for this many sequences and new tokens (its first ``4 * KV_COUNTERS`` bytes must be zero before the first call)."""
+    return int(load().mxfp4_kv_attention_workspace_bytes(_kv_cache_desc(cache), KvRowsDesc(None, 0, 0, None, None, rows, tokens), q_heads))
+
+
+def mxfp4_kv_attention(q: torch.Tensor, cache: KvCache, table: torch.Tensor, lens: torch.Tensor,
+                       starts: Optional[torch.Tensor] = None, scale: Optional[float] = None, causal: bool = True, window: int = 0,
+                       tree: Optional[torch.Tensor] = None, return_lse: bool = False, out: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None):
+    """Attention of the new tokens ``q`` BF16 ``[tokens, q_heads, dim]`` over the cached ones (the new ones among them, see
+    ``mxfp4_kv_append``); ``scale``: dim ** -0.5.  ``window`` > 0: only the last ``window`` tokens.  ``tree`` int64 ``[tokens]``: bit m says
+    that the query sees new token m of its sequence, in place of the causal rule.  Returns BF16 ``[tokens, q_heads, dim]``, with
+    ``return_lse`` also the logarithms of the softmax sums, float32 ``[tokens, q_heads]``.  ``workspace``: None takes the one that the binding
+    keeps for the current stream."""
+    c = _kv_cache_desc(cache)
+    dev = cache.kq.device
+    tokens = q.shape[0]
+    b = _kv_rows_desc(table, lens, starts, tokens, dev)
+    qd = _kv_tensor_desc(q, "q", dev, tokens, None, c.dim)
+    q_heads = q.shape[1]
+    if out is None:
+        out = torch.empty((tokens, q_heads, c.dim), dtype=torch.bfloat16, device=dev)
+    od = _kv_tensor_desc(out, "out", dev, tokens, q_heads, c.dim)
+    if tree is not None and (tree.dtype != torch.int64 or tree.device != dev or tuple(tree.shape) != (tokens,) or not tree.is_contiguous()):
+        raise ValueError("tree must be a contiguous int64 tensor [%d] on %s" % (tokens, dev))
+    lse = torch.empty((tokens, q_heads), dtype=torch.float32, device=dev) if return_lse else None
+    args = KvAttentionArgs(qd, od, _ptr(lse), _ptr(tree), q_heads, window, c.dim ** -0.5 if scale is None else scale, int(causal))
+    with _on(dev):
+        lib, stream = load(), _stream()
+        if workspace is None:
+            workspace = _kv_workspace(dev, stream, int(lib.mxfp4_kv_attention_workspace_bytes(c, b, q_heads)))
+        _check(lib.mxfp4_kv_attention(c, b, args, workspace.data_ptr(), workspace.numel() * workspace.element_size(), stream))
+    return (out, lse) if return_lse else out
+
+
+def _kv_pool_desc(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: torch.Tensor) -> KvPoolDesc:
+    _dev(pool.refs)
+    dev, pages = pool.refs.device, pool.refs.shape[0]
+    _kv_ints(pool.refs, dev, "refs", None)
+    _kv_ints(pool.free, dev, "free", (pages + 31) // 32)
+    ldt = _kv_table(table, dev)
+    _kv_ints(lens, dev, "lens", table.shape[0])
+    return KvPoolDesc(pool.refs.data_ptr(), pool.free.data_ptr(), pages, cache.kq.shape[2], table.data_ptr(), ldt, table.shape[1],
+                      table.shape[0], lens.data_ptr())
+
+
+def _kv_two_lists(a: torch.Tensor, b: torch.Tensor, names: str, device) -> int:
+    _kv_ints(a, device, names, None)
+    _kv_ints(b, device, names, a.shape[0])
+    return a.shape[0]
+
+
+def mxfp4_kv_fork(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) -> None:
+    """Sequence ``dst[i]`` (empty) becomes a second owner of what sequence ``src[i]`` holds; nothing is copied."""
+    p, n = _kv_pool_desc(pool, cache, table, lens), _kv_two_lists(src, dst, "src and dst", pool.refs.device)
+    with _on(pool.refs.device):
+        _check(load().mxfp4_kv_fork(p, _ptr(src), _ptr(dst), n, _stream()))
+
+
+def mxfp4_kv_extend(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: torch.Tensor, rows: torch.Tensor, add: torch.Tensor
+                    ) -> torch.Tensor:
+    """Room for ``add[i]`` more tokens of sequence ``rows[i]``: pages are taken, a shared last page becomes a copy, ``lens`` grows.
+    ``cache``: its pages hold all that belongs to a token (all layers).  Returns int32 ``[1]`` on the device: 0, or what is missing
+    (pages, or -1 for a table that is too narrow); then nothing has changed."""
+    dev = pool.refs.device
+    p, n = _kv_pool_desc(pool, cache, table, lens), _kv_two_lists(rows, add, "rows and add", dev)
+    got = torch.empty((2 * n + 1,), dtype=torch.int32, device=dev)
+    with _on(dev):
+        _check(load().mxfp4_kv_extend(p, _kv_cache_desc(cache), _ptr(rows), _ptr(add), n, got.data_ptr() + 4, got.data_ptr(), _stream()))
+    return got[:1]
+
+
+def mxfp4_kv_release(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: torch.Tensor, rows: torch.Tensor, keep: torch.Tensor) -> None:
+    """Sequence ``rows[i]`` is cut down to its first ``keep[i]`` tokens (0: all of it is given up); pages that nobody holds any more are free."""
+    p, n = _kv_pool_desc(pool, cache, table, lens), _kv_two_lists(rows, keep, "rows and keep", pool.refs.device)
+    with _on(pool.refs.device):
+        _check(load().mxfp4_kv_release(p, _ptr(rows), _ptr(keep), n, _stream()))
+
+
+def mxfp4_kv_compact(cache: KvCache, table: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, counts: torch.Tensor) -> None:
+    """Token ``base[b] + keep[b, i]`` of sequence b moves to ``base[b] + i`` for i below ``counts[b]``; ``keep`` ascends."""
+    c, dev = _kv_cache_desc(cache), cache.kq.device
+    ldt, rows = _kv_table(table, dev), table.shape[0]
+    _kv_ints(base, dev, "base", rows)
+    _kv_ints(counts, dev, "counts", rows)
+    _kv_ints(keep, dev, "keep", rows, None)
+    with _on(dev):
+        _check(load().mxfp4_kv_compact(c, table.data_ptr(), ldt, table.shape[1], _ptr(base), _ptr(keep), keep.shape[1], _ptr(counts), rows,
+                                       _stream()))
+
+
+def mxfp4_kv_copy_pages(cache: KvCache, src: torch.Tensor, dst: torch.Tensor) -> None:
+    """Page ``src[i]`` is copied to page ``dst[i]``."""
+    c, n = _kv_cache_desc(cache), _kv_two_lists(src, dst, "src and dst", cache.kq.device)
+    with _on(cache.kq.device):
+        _check(load().mxfp4_kv_copy_pages(c, _ptr(src), _ptr(dst), n, _stream()))

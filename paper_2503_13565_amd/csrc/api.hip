@@ -23,13 +23,13 @@ static thread_local bool g_check_only = false;
 // Every entry point starts here: no error text yet, and a HIP error left behind by earlier calls of
 // the caller (the runtime keeps the last one until somebody reads it) must not be reported as the
 // status of the launches that follow.
-static void begin_call()
+void begin_call()
 {
     g_err[0] = 0;
     (void)hipGetLastError();
 }
 
-static int fail(int code, const char* fmt, ...)
+int fail(int code, const char* fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -38,13 +38,13 @@ static int fail(int code, const char* fmt, ...)
     return code;
 }
 
-static int hip_fail(hipError_t e, const char* what)
+int hip_fail(hipError_t e, const char* what)
 {
     return fail(MXFP4_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
 // Per-device facts, looked up once per device.
-static int device_info(DeviceInfo* out)
+int device_info(DeviceInfo* out)
 {
     static DeviceInfo cache[64];
     static std::atomic<bool> have[64];              // set after the entry is complete (racing threads write the same values)

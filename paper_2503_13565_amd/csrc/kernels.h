@@ -55,6 +55,12 @@ struct DeviceInfo {
     int lds_bytes;       // LDS per workgroup the device allows
 };
 
+// What every entry point shares (api.hip): the start of a call, the thread's error text, the device's facts.
+void begin_call();
+int fail(int code, const char* fmt, ...);
+int hip_fail(hipError_t e, const char* what);
+int device_info(DeviceInfo* out);
+
 // `integer_rule`: round the elements with the integer-only rule instead of the convert instruction.
 hipError_t launch_direct_cast(const void* w, int64_t n_rows, int64_t k, int64_t ldw, void* q, void* s,
                               bool integer_rule, hipStream_t stream);

@@ -1,0 +1,402 @@
+// Attention over a paged MXFP4 cache for gfx950, few queries per key/value head: drafting (one token), verifying (a draft or
+// a draft tree), short pieces of prompts.
+//
+//   out[t][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q[t][h] . k_j - m)
+//
+// in one pass over the keys with the running maximum m.  Bound by HBM: 17/16 bytes per element of the head dimension and token
+// (codes and scales of key and value).  The queries of all heads that share a key/value head, and all new tokens, are the 16
+// columns of v_mfma_f32_16x16x32_bf16 (QT times 16), so a cached token is read and decoded once for all of them:
+//   scores   S^T[token][query]  = K . Q^T      keys are the left operand, decoded in registers (kv_tile.h)
+//   values   O^T[element][query] += V^T . P^T   the scores leave the first product in the layout in which the second one takes
+//                                               them as its right operand: no LDS and no crossing of lanes in the loop
+#include "kv_tile.h"
+
+namespace mxfp4 {
+
+// What a query may see, for the lane's column of query tile qt.
+struct KvSight {
+    int lo, hi;                      // positions lo .. hi - 1
+    uint64_t tree;                   // and, from `base` on, the bits that are set
+    int base;
+};
+
+__device__ __forceinline__ bool kv_sees(const KvSight& s, bool tree, int j)
+{
+    bool ok = j >= s.lo && j < s.hi;
+    if (tree && j >= s.base)
+        ok = ok && j - s.base < 64 && ((s.tree >> (j - s.base)) & 1);
+    return ok;
+}
+
+template <int NB, int QT, bool kPad>
+__global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAttend a)
+{
+    typedef KvTile<NB, kPad> T;
+    constexpr int NW = 4, kRows = 16 * QT, kEl = T::kEl, kChunks = T::kChunks;
+    constexpr int kSlot = QT * NB * 512 + 32 * QT;                     // floats of a partial result
+    __shared__ __align__(16) float comb[NW][kEl][4][64];
+    __shared__ float ml[NW][QT][16][2];
+    __shared__ int last;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    KvItem it;
+    if (!kv_find<NW * 32>(a, blockIdx.x, kRows, &it))
+        return;                                                        // (the whole workgroup)
+    const int rows = it.n * a.group, row0 = it.tile * kRows;
+    const int i0 = row0 / a.group, i1 = min((row0 + kRows - 1) / a.group, it.n - 1);
+    const bool tree = a.tree != nullptr, causal = a.causal && !tree;
+    const int hi = causal ? max(0, min(it.len, it.len - it.n + i1 + 1)) : it.len;
+    const int lo = a.window > 0 ? max(0, it.len - it.n + i0 + 1 - a.window) & ~31 : 0;
+    const int tiles = max(0, (hi - lo + 31) >> 5);
+    const int t_begin = (lo >> 5) + (int)((int64_t)tiles * it.s / it.S), t_end = (lo >> 5) + (int)((int64_t)tiles * (it.s + 1) / it.S);
+    // tiles from `plain_lo` on and up to `plain_hi` need no mask: every query of this workgroup sees all of their tokens
+    const int plain_hi = causal ? it.len - it.n + i0 + 1 : tree ? it.len - it.n : it.len;
+    const int plain_lo = a.window > 0 ? it.len - it.n + i1 + 1 - a.window : 0;
+
+    bf16x8_t q[QT][NB];
+    KvSight sight[QT];
+    int64_t out_at[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        const int row = row0 + qt * 16 + c;
+        const int i = row / a.group, head = it.h * a.group + row - i * a.group;
+        const bool live = row < rows;
+        const int p = it.len - it.n + i;
+        sight[qt].lo = a.window > 0 ? p - a.window + 1 : 0;
+        sight[qt].hi = !live ? 0 : causal ? p + 1 : it.len;
+        sight[qt].base = it.len - it.n;
+        sight[qt].tree = tree && live ? a.tree[it.first + i] : 0;
+        out_at[qt] = live ? (int64_t)(it.first + i) * a.out.token + (int64_t)head * a.out.head : -1;
+        const uint16_t* from = a.q.p + (int64_t)(it.first + (live ? i : 0)) * a.q.token + (int64_t)(live ? head : it.h * a.group) * a.q.head;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            if (!kPad || 8 * NB * g + 8 * j < 32 * a.c.nb)
+                q[qt][j] = *reinterpret_cast<const bf16x8_t*>(from + 8 * NB * g + 8 * j);
+            else
+                q[qt][j] = __builtin_bit_cast(bf16x8_t, (u32x4_t{0, 0, 0, 0}));
+        }
+    }
+
+    f32x4_t o[QT][2 * NB];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        m[qt] = -INFINITY;
+        l[qt] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 2 * NB; ++e)
+            o[qt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    }
+
+    const float scale = a.scale;
+    auto compute = [&](T& t, int tile) {
+        const int j0 = tile * 32;
+        const bool whole = t.page[0] >= 0 && t.page[1] >= 0 && j0 + 32 <= it.len;
+        const bool masked = !(whole && j0 + 32 <= plain_hi && j0 >= plain_lo);
+        f32x4_t s[QT][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                const bf16x8_t k = key_operand(t, h, j);
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt)
+                    s[qt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[qt][j], j ? s[qt][h] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+            }
+        uint32_t nan_at = 0;                                           // bit (chunk, half, token): a NaN block, taken out of the values
+        if (masked) {
+            // Tokens behind the end and pages that are not there: whatever lies in the memory must not reach the sums.
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int here = t.page[h] < 0 ? 0 : it.len - j0 - 16 * h;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int j = j0 + 16 * h + 4 * g + i;
+                    const bool there = 4 * g + i < here;
+#pragma unroll
+                    for (int qt = 0; qt < QT; ++qt)
+                        s[qt][h][i] = there && kv_sees(sight[qt], tree, j) ? s[qt][h][i] : -INFINITY;
+#pragma unroll
+                    for (int ch = 0; ch < kChunks; ++ch) {
+                        const bool bad = value_scale(t, h, i, ch) == 0xFFu;
+                        if (bad || !there) {
+                            clear_value(t, h, i, ch);
+                            nan_at |= (there && bad ? 1u : 0u) << (ch * 8 + h * 4 + i);
+                        }
+                    }
+                }
+            }
+        }
+        bf16x8_t p[QT];
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            float top = fmaxf(fmaxf(fmaxf(s[qt][0][0], s[qt][0][1]), fmaxf(s[qt][0][2], s[qt][0][3])),
+                              fmaxf(fmaxf(s[qt][1][0], s[qt][1][1]), fmaxf(s[qt][1][2], s[qt][1][3])));
+            top = max_of_rows(top);
+            // The sums move to a new maximum only when it is 2^8 above the old one: the weights then stay below 2^8, which FP32 sums and
+            // BF16 weights hold as well as weights up to 1.
+            if (__ballot((top - m[qt]) * scale > 8.f || (m[qt] == -INFINITY && top > -INFINITY))) {
+                const float now = fmaxf(m[qt], top);
+                const float f = now == -INFINITY ? 1.f : exp2f((m[qt] - now) * scale);
+                m[qt] = now;
+                l[qt] *= f;
+#pragma unroll
+                for (int e = 0; e < 2 * NB; ++e)
+                    o[qt][e] *= f;
+            }
+            const float off = m[qt] == -INFINITY ? 0.f : -m[qt] * scale;
+            float w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(fmaf(s[qt][i >> 2][i & 3], scale, off));
+                l[qt] += w[i];
+            }
+            // rounded to BF16 (the type of the values' product; half a step, 2^-8 of a weight at most, and the weights' errors average out)
+            typedef __attribute__((ext_vector_type(4))) uint32_t words;
+            p[qt] = __builtin_bit_cast(bf16x8_t, (words{f32_to_bf16_rne2(w[0], w[1]), f32_to_bf16_rne2(w[2], w[3]),
+                                                        f32_to_bf16_rne2(w[4], w[5]), f32_to_bf16_rne2(w[6], w[7])}));
+        }
+#pragma unroll
+        for (int ch = 0; ch < kChunks; ++ch) {
+            bf16x8_t x[kEl];
+            value_operands(t, ch, x);
+#pragma unroll
+            for (int e = 0; e < kEl; ++e)
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt)
+                    o[qt][ch * kEl + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[e], p[qt], o[qt][ch * kEl + e], 0, 0, 0);
+        }
+        if (masked && __ballot(nan_at != 0)) {
+            // NaN blocks in a tile that not every query sees whole: counted for each query that sees one, by the same product with
+            // ones in the places of the blocks and of what is seen.
+#pragma unroll
+            for (int ch = 0; ch < kChunks; ++ch) {
+                typedef __attribute__((ext_vector_type(8))) uint16_t ones;
+                ones x;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    x[i] = (nan_at >> (ch * 8 + i)) & 1 ? 0x3F80 : 0;
+#pragma unroll
+                for (int qt = 0; qt < QT; ++qt) {
+                    ones y;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        y[i] = kv_sees(sight[qt], tree, j0 + 16 * (i >> 2) + 4 * g + (i & 3)) ? 0x3F80 : 0;
+                    const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, y),
+                                                                                f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                    for (int e = 0; e < kEl; ++e)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            o[qt][ch * kEl + e][i] = hit[i] > 0.f ? __uint_as_float(0x7FC00000u) : o[qt][ch * kEl + e][i];
+                }
+            }
+        }
+    };
+
+    // Tiles t_begin + wave, + 4, ...: the next one is asked for before the present one is used.
+    int pages = 0, loaded = 0;
+    auto load = [&](T& t, int tile) {
+        if ((loaded & 31) == 0)
+            pages = kv_pages32<NW>(a, it.b, it.len, tile);
+        const int k = (loaded & 31) * 2;
+        ++loaded;
+        load_tile(t, a.c, it.h, tile * 32, __builtin_amdgcn_readlane(pages, k), __builtin_amdgcn_readlane(pages, k + 1));
+    };
+    int tile = t_begin + wave;
+    if (tile < t_end) {
+        T x, y;
+        load(x, tile);
+        while (true) {
+            if (tile + NW < t_end)
+                load(y, tile + NW);
+            compute(x, tile);
+            tile += NW;
+            if (tile >= t_end)
+                break;
+            if (tile + NW < t_end)
+                load(x, tile + NW);
+            compute(y, tile);
+            tile += NW;
+            if (tile >= t_end)
+                break;
+        }
+    }
+
+    // The four waves' sums meet in the LDS, one chunk of elements at a time; wave i takes row i of the accumulators.
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        l[qt] = sum_of_rows(l[qt]);
+        if (g == 0) {
+            ml[wave][qt][c][0] = m[qt];
+            ml[wave][qt][c][1] = l[qt];
+        }
+    }
+    float* part = a.part + (int64_t)it.slot * kSlot;
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        float f[NW], top = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int ch = 0; ch < kChunks; ++ch) {
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < kEl; ++e)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    comb[wave][e][i][lane] = o[qt][ch * kEl + e][i];
+            __syncthreads();
+            if (ch == 0) {
+#pragma unroll
+                for (int w = 0; w < NW; ++w)
+                    top = fmaxf(top, ml[w][qt][c][0]);
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {
+                    f[w] = ml[w][qt][c][0] == -INFINITY ? 0.f : exp2f((ml[w][qt][c][0] - top) * scale);
+                    // (a wave that has met only NaN scores has no maximum, but its sum says so)
+                    f[w] = ml[w][qt][c][1] != ml[w][qt][c][1] ? __uint_as_float(0x7FC00000u) : f[w];
+                    total += f[w] * ml[w][qt][c][1];
+                }
+            }
+            float r[kEl];
+#pragma unroll
+            for (int e = 0; e < kEl; ++e) {
+                r[e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < NW; ++w)
+                    r[e] += f[w] * comb[w][e][wave][lane];
+            }
+            if (it.S == 1) {
+                if (out_at[qt] >= 0 && (!kPad || ch * T::kChunk + kEl * (4 * g + wave) < 32 * a.c.nb)) {
+                    const float inv = total == 0.f ? 0.f : 1.f / total;
+                    uint16_t* to = a.out.p + out_at[qt] + ch * T::kChunk + kEl * (4 * g + wave);
+                    uint32_t y[kEl / 2];
+#pragma unroll
+                    for (int e = 0; e < kEl; e += 2)
+                        y[e / 2] = f32_to_bf16_rne2(r[e] * inv, r[e + 1] * inv);
+                    __builtin_memcpy(__builtin_assume_aligned(to, kEl * 2), y, kEl * 2);
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < kEl; ++e)
+                    part[((qt * 2 * NB + ch * kEl + e) * 4 + wave) * 64 + lane] = r[e];
+            }
+        }
+        if (wave == 0 && g == 0) {
+            if (it.S > 1) {
+                part[QT * NB * 512 + qt * 32 + c] = top;
+                part[QT * NB * 512 + qt * 32 + 16 + c] = total;
+            } else if (a.lse && out_at[qt] >= 0) {
+                const int row = row0 + qt * 16 + c, i = row / a.group;
+                a.lse[(int64_t)(it.first + i) * (a.group * a.c.heads) + it.h * a.group + row - i * a.group] =
+                    total == 0.f ? -INFINITY : (top * scale + log2f(total)) * kLn2;
+            }
+        }
+    }
+    if (it.S == 1)
+        return;
+
+    // Parts of one row of keys: the workgroup that comes last adds all of them, in their order whoever it is.  Nobody waits.
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0)
+        last = atomicAdd(&a.counters[it.slot0], 1u) == (uint32_t)it.S - 1;
+    __syncthreads();
+    if (!last)
+        return;
+    __threadfence();
+    if (threadIdx.x == 0)
+        a.counters[it.slot0] = 0;
+    const float* parts = a.part + (int64_t)it.slot0 * kSlot;
+    const int64_t step = (int64_t)it.slots * kSlot;
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        float top = -INFINITY, total = 0.f;
+        for (int s = 0; s < it.S; ++s)
+            top = fmaxf(top, parts[s * step + QT * NB * 512 + qt * 32 + c]);
+        float r[2 * NB];
+#pragma unroll
+        for (int e = 0; e < 2 * NB; ++e)
+            r[e] = 0.f;
+#pragma unroll 2
+        for (int s = 0; s < it.S; ++s) {
+            const float* x = parts + s * step;
+            const float ms = x[QT * NB * 512 + qt * 32 + c], ls = x[QT * NB * 512 + qt * 32 + 16 + c];
+            const float f = ls != ls ? __uint_as_float(0x7FC00000u) : ms == -INFINITY ? 0.f : exp2f((ms - top) * scale);
+            total += f * ls;
+#pragma unroll
+            for (int e = 0; e < 2 * NB; ++e)
+                r[e] += f * x[((qt * 2 * NB + e) * 4 + wave) * 64 + lane];
+        }
+        if (out_at[qt] < 0)
+            continue;
+        const float inv = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+        for (int ch = 0; ch < kChunks; ++ch) {
+            if (kPad && ch * T::kChunk + kEl * (4 * g + wave) >= 32 * a.c.nb)
+                continue;
+            uint16_t* to = a.out.p + out_at[qt] + ch * T::kChunk + kEl * (4 * g + wave);
+            uint32_t y[kEl / 2];
+#pragma unroll
+            for (int e = 0; e < kEl; e += 2)
+                y[e / 2] = f32_to_bf16_rne2(r[ch * kEl + e] * inv, r[ch * kEl + e + 1] * inv);
+            __builtin_memcpy(__builtin_assume_aligned(to, kEl * 2), y, kEl * 2);
+        }
+        if (a.lse && wave == 0 && g == 0) {
+            const int row = row0 + qt * 16 + c, i = row / a.group;
+            a.lse[(int64_t)(it.first + i) * (a.group * a.c.heads) + it.h * a.group + row - i * a.group] =
+                total == 0.f ? -INFINITY : (top * scale + log2f(total)) * kLn2;
+        }
+    }
+}
+
+// Query tiles of a workgroup: two where an average sequence has more queries than one tile holds, and the registers hold the
+// sums (8 times the tiles times dim / 32 of them).
+static int query_tiles(int nb, int64_t queries) { return queries <= 16 || nb > 4 ? 1 : 2; }
+
+static int padded(int nb) { return nb == 3 ? 4 : nb == 6 ? 8 : nb; }
+
+// Workgroups that the cutting aims for: as many as run at once.
+static int attend_target(int nb, const DeviceInfo& dev) { return dev.cus * (nb <= 4 ? 2 : 1); }
+
+size_t kv_attend_part_bytes(int nb, int group, int64_t tokens, int64_t rows, const DeviceInfo& dev)
+{
+    const int qt = query_tiles(nb, rows ? (tokens * group + rows - 1) / rows : 0);
+    return (size_t)2 * attend_target(nb, dev) * (qt * padded(nb) * 512 + 32 * qt) * sizeof(float);
+}
+
+template <int NB, bool kPad>
+static hipError_t launch_attend(const KvAttend& a, int qt, int64_t blocks, hipStream_t stream)
+{
+    auto kernel = kv_attend_kernel<NB, 1, kPad>;
+    if constexpr (NB <= 4)
+        if (qt == 2)
+            kernel = kv_attend_kernel<NB, 2, kPad>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_attend(KvAttend a, const DeviceInfo& dev, hipStream_t stream)
+{
+    const int qt = query_tiles(a.c.nb, ((int64_t)a.b.tokens * a.group + a.b.rows - 1) / a.b.rows);
+    a.target = attend_target(a.c.nb, dev);
+    // No more workgroups than shares: target + tiles x heads by the cutting, and no more than the tables' units.
+    const int64_t per = 16 * qt;
+    const int64_t tiles = a.b.starts ? (int64_t)a.b.tokens * a.group / per + a.b.rows : a.b.rows * (((int64_t)a.b.per_row * a.group + per - 1) / per);
+    const int64_t units = (((int64_t)a.b.width << a.c.shift) + 127) / 128;
+    int64_t blocks = tiles * a.c.heads + a.target;
+    if (tiles * a.c.heads * units < blocks)
+        blocks = tiles * a.c.heads * units;
+    if (blocks > 0x7FFFFFFF)
+        return hipErrorInvalidConfiguration;
+    switch (a.c.nb) {
+    case 1: return launch_attend<1, false>(a, qt, blocks, stream);
+    case 2: return launch_attend<2, false>(a, qt, blocks, stream);
+    case 3: return launch_attend<4, true>(a, qt, blocks, stream);
+    case 4: return launch_attend<4, false>(a, qt, blocks, stream);
+    case 6: return launch_attend<8, true>(a, qt, blocks, stream);
+    case 8: return launch_attend<8, false>(a, qt, blocks, stream);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace mxfp4

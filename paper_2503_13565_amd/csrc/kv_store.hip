@@ -1,0 +1,227 @@
+// Into, out of and inside a paged MXFP4 cache for gfx950: the store of new tokens (rotary positions and the cast of
+// arXiv 2503.13565, section 3.4.3, in one launch), the values back out, tokens moved together, pages copied.
+#include "cast_block.h"
+#include "common.h"
+#include "kv.h"
+
+namespace mxfp4 {
+
+// Eight values of one head turned by their positions.  `x`: the head's elements e .. e + 7; the partners of the
+// pairs (i, i + dim / 2) are dim / 2 further or before, another load of the same lines.  Each product is rounded to FP32 on its
+// own (no fused multiply-add), so that the BF16 result does not depend on how a compiler contracts.
+__device__ __forceinline__ u32x4_t turn8(u32x4_t own, const uint16_t* head, int e, const KvRope& rope, int pos)
+{
+#pragma clang fp contract(off)
+    const int half = rope.dim >> 1;
+    const bool second = e >= half;
+    const int i = second ? e - half : e;
+    const u32x4_t other = *reinterpret_cast<const u32x4_t*>(head + (second ? i : i + half));
+    const bool inside = (unsigned)pos < (unsigned)rope.length;
+    const int64_t at = (int64_t)(inside ? pos : 0) * half + i;
+    f32x4_t c[2], s[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        c[j] = *reinterpret_cast<const f32x4_t*>(rope.cos + at + 4 * j);
+        s[j] = *reinterpret_cast<const f32x4_t*>(rope.sin + at + 4 * j);
+    }
+    const float wrong = inside ? 0.f : __uint_as_float(0x7FC00000u);
+    u32x4_t out;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        float r[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const float x = bf16_bits_to_f32(k ? own[j] >> 16 : own[j] & 0xFFFFu);
+            const float y = bf16_bits_to_f32(k ? other[j] >> 16 : other[j] & 0xFFFFu);
+            const float a = x * c[(2 * j + k) >> 2][(2 * j + k) & 3];
+            const float b = y * s[(2 * j + k) >> 2][(2 * j + k) & 3];
+            const float t = second ? a + b : a - b;
+            r[k] = inside ? t : wrong;
+        }
+        out[j] = f32_to_bf16_rne2(r[0], r[1]);
+    }
+    return out;
+}
+
+// A workgroup takes 256 groups of eight elements of one token: the heads of q, then of k, then of v.  A quad of lanes has one
+// 32-element block, as in the cast of a whole tensor.  Bound by latency for a step's few tokens (the token's row, its
+// length and its page are one load behind the other, the elements are asked for in front of them) and by HBM for prompts.
+__global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvBatch b, KvTensor k, KvTensor v, KvTensor q, KvTensor qo,
+                                                        int q_heads, KvRope rope)
+{
+    const int t = blockIdx.x;
+    const int per_head = c.nb * 4;
+    const int g = blockIdx.y * 256 + threadIdx.x;
+    const int head_all = g / per_head, e = (g - head_all * per_head) * 8;
+    const int kv_heads = c.heads;
+    const bool live = head_all < q_heads + 2 * kv_heads;         // the same for a whole quad (per_head is a multiple of four)
+    const int what = head_all < q_heads ? 0 : head_all < q_heads + kv_heads ? 1 : 2;
+    const int head = what == 0 ? head_all : what == 1 ? head_all - q_heads : head_all - q_heads - kv_heads;
+    const KvTensor& in = what == 0 ? q : what == 1 ? k : v;
+    const uint16_t* row = in.p + (int64_t)t * in.token + (int64_t)head * in.head;
+    u32x4_t x = {0, 0, 0, 0};
+    if (live)
+        x = *reinterpret_cast<const u32x4_t*>(row + e);
+    const KvPlace at = kv_place(b, t);           // (with all lanes of the wave)
+    if (!live)
+        return;
+    if (what < 2 && e < rope.dim)
+        x = turn8(x, row, e, rope, rope.positions ? rope.positions[t] : at.at);
+    if (what == 0) {
+        *reinterpret_cast<u32x4_t*>(qo.p + (int64_t)t * qo.token + (int64_t)head * qo.head + e) = x;
+        return;
+    }
+    const int page = kv_page(b.table, b.ldt, b.width, c.shift, c.pages, at.row, at.at);
+    uint32_t packed;
+    int scale;
+    cast_group<true>(x, &packed, &scale);
+    if (page < 0)
+        return;
+    const int slot = (head << c.shift) + (at.at & ((1 << c.shift) - 1));
+    uint8_t* cq = (what == 1 ? c.kq : c.vq) + (int64_t)page * c.psq + (int64_t)slot * (c.nb * 16);
+    uint8_t* cs = (what == 1 ? c.ks : c.vs) + (int64_t)page * c.pss + (int64_t)slot * c.nb;
+    *reinterpret_cast<uint32_t*>(cq + (e >> 1)) = packed;
+    if ((e & 31) == 0)
+        cs[e >> 5] = (uint8_t)scale;
+}
+
+// Eight elements back to BF16 (exact: a code times a power of two), zeros where the token is nowhere.
+__global__ __launch_bounds__(256) void kv_read_kernel(KvView c, KvBatch b, KvTensor k, KvTensor v)
+{
+    const int t = blockIdx.x;
+    const int per_head = c.nb * 4;
+    const int g = blockIdx.y * 256 + threadIdx.x;
+    const int head_all = g / per_head, e = (g - head_all * per_head) * 8;
+    const KvPlace at = kv_place(b, t);
+    const int page = kv_page(b.table, b.ldt, b.width, c.shift, c.pages, at.row, at.at);
+    if (head_all >= 2 * c.heads)
+        return;
+    const bool keys = head_all < c.heads;
+    const int head = keys ? head_all : head_all - c.heads;
+    const KvTensor& out = keys ? k : v;
+    if (!out.p)
+        return;
+    u32x4_t x = {0, 0, 0, 0};
+    if (page >= 0) {
+        const int slot = (head << c.shift) + (at.at & ((1 << c.shift) - 1));
+        const uint32_t w = *reinterpret_cast<const uint32_t*>((keys ? c.kq : c.vq) + (int64_t)page * c.psq +
+                                                              (int64_t)slot * (c.nb * 16) + (e >> 1));
+        const float s = __uint_as_float((uint32_t)((keys ? c.ks : c.vs) + (int64_t)page * c.pss + (int64_t)slot * c.nb)[e >> 5] << 23);
+        x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+        x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+        x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+        x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+    }
+    *reinterpret_cast<u32x4_t*>(out.p + (int64_t)t * out.token + (int64_t)head * out.head + e) = x;
+}
+
+// Tokens of one sequence and one head move together, in place.  256 threads hold 256 / (2 nb) tokens at a time, one block (16
+// bytes of codes and a scale byte) of a key or value each; a step's tokens are all read before any is written.  A step writes below
+// what later steps read (keep ascends, so token j comes from beyond position j), so the steps need no more than that.
+__global__ __launch_bounds__(256) void kv_compact_kernel(KvView c, const int32_t* table, int64_t ldt, int width, const int32_t* base,
+                                                         const int32_t* keep, int ldk, const int32_t* counts)
+{
+    const int row = blockIdx.x, head = blockIdx.y;
+    const int each = 2 * c.nb, at_once = 256 / each;
+    const int tok = threadIdx.x / each, unit = threadIdx.x - tok * each;
+    const bool keys = unit < c.nb;
+    const int block = keys ? unit : unit - c.nb;
+    const int n = min(counts[row], ldk), from0 = base[row];
+    uint8_t* cq = keys ? c.kq : c.vq;
+    uint8_t* cs = keys ? c.ks : c.vs;
+    const int mask = (1 << c.shift) - 1;
+    for (int i0 = 0; i0 < n; i0 += at_once) {
+        const int i = i0 + tok;
+        u32x4_t w = {0, 0, 0, 0};
+        uint8_t s = 0;
+        int to = -1, slot = 0;
+        if (tok < at_once && i < n) {
+            const int k = keep[(int64_t)row * ldk + i];
+            if (k > i && from0 >= 0 && k <= 0x7FFFFFFF - from0) {
+                const int from = kv_page(table, ldt, width, c.shift, c.pages, row, from0 + k);
+                to = from < 0 ? -1 : kv_page(table, ldt, width, c.shift, c.pages, row, from0 + i);
+                const int at = (head << c.shift) + ((from0 + k) & mask);
+                slot = (head << c.shift) + ((from0 + i) & mask);
+                if (to >= 0) {
+                    w = *reinterpret_cast<const u32x4_t*>(cq + (int64_t)from * c.psq + ((int64_t)at * c.nb + block) * 16);
+                    s = cs[(int64_t)from * c.pss + (int64_t)at * c.nb + block];
+                }
+            }
+        }
+        drain_vmem();                            // what this step reads is here before anyone writes
+        __syncthreads();
+        if (to >= 0) {
+            *reinterpret_cast<u32x4_t*>(cq + (int64_t)to * c.psq + ((int64_t)slot * c.nb + block) * 16) = w;
+            cs[(int64_t)to * c.pss + (int64_t)slot * c.nb + block] = s;
+        }
+    }
+}
+
+// Pages (or the slots of them that are in use) copied, one pair per blockIdx.x, 16 bytes at a time; a head's part of a page is
+// a run of its own.
+__global__ __launch_bounds__(256) void kv_copy_kernel(KvView c, const int32_t* src, const int32_t* dst, int pitch, const int32_t* rows,
+                                                      int n_rows, const int32_t* lens, const int32_t* add)
+{
+    const int from = src[(int64_t)blockIdx.x * pitch], to = dst[(int64_t)blockIdx.x * pitch];
+    if ((unsigned)from >= (unsigned)c.pages || (unsigned)to >= (unsigned)c.pages)
+        return;
+    int tokens = 1 << c.shift;
+    if (rows) {
+        const int row = rows[blockIdx.x];
+        if ((unsigned)row >= (unsigned)n_rows)
+            return;
+        tokens = (((lens[row] - add[blockIdx.x]) & (tokens - 1)) + 15) & ~15;
+    }
+    const int q_run = tokens * c.nb, s_run = tokens * c.nb / 16;         // 16-byte pieces of a head
+    const int q_page = c.nb << c.shift, s_page = (c.nb << c.shift) / 16;
+    const int each = 2 * (q_run + s_run), total = each * c.heads;
+    for (int i = blockIdx.y * 256 + threadIdx.x; i < total; i += gridDim.y * 256) {
+        const int head = i / each;
+        int at = i - head * each;
+        const bool keys = at < q_run + s_run;
+        at = keys ? at : at - q_run - s_run;
+        const bool codes = at < q_run;
+        uint8_t* x = codes ? (keys ? c.kq : c.vq) : (keys ? c.ks : c.vs);
+        const int64_t stride = codes ? c.psq : c.pss;
+        const int64_t off = 16 * (codes ? (int64_t)head * q_page + at : (int64_t)head * s_page + at - q_run);
+        *reinterpret_cast<u32x4_t*>(x + (int64_t)to * stride + off) = *reinterpret_cast<const u32x4_t*>(x + (int64_t)from * stride + off);
+    }
+}
+
+hipError_t launch_kv_append(const KvView& c, const KvBatch& b, const KvTensor& k, const KvTensor& v, const KvTensor& q,
+                            const KvTensor& qo, int q_heads, const KvRope& rope, hipStream_t stream)
+{
+    const int64_t groups = (int64_t)(q_heads + 2 * c.heads) * c.nb * 4;
+    hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)b.tokens, (unsigned)((groups + 255) / 256)), dim3(256), 0, stream, c, b, k, v,
+                       q, qo, q_heads, rope);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const KvView& c, const KvBatch& b, const KvTensor& k, const KvTensor& v, hipStream_t stream)
+{
+    const int64_t groups = (int64_t)2 * c.heads * c.nb * 4;
+    hipLaunchKernelGGL(kv_read_kernel, dim3((unsigned)b.tokens, (unsigned)((groups + 255) / 256)), dim3(256), 0, stream, c, b, k, v);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_compact(const KvView& c, const int32_t* table, int64_t ldt, int width, const int32_t* base,
+                             const int32_t* keep, int ldk, const int32_t* counts, int rows, hipStream_t stream)
+{
+    hipLaunchKernelGGL(kv_compact_kernel, dim3((unsigned)rows, (unsigned)c.heads), dim3(256), 0, stream, c, table, ldt, width, base, keep,
+                       ldk, counts);
+    return hipGetLastError();
+}
+
+hipError_t launch_kv_copy(const KvView& c, const int32_t* src, const int32_t* dst, int pitch, int count, const int32_t* rows,
+                          int n_rows, const int32_t* lens, const int32_t* add, hipStream_t stream)
+{
+    const int64_t pieces = (int64_t)2 * c.heads * ((c.nb << c.shift) + (c.nb << c.shift) / 16);
+    int64_t blocks = (pieces + 1023) / 1024;
+    const int64_t most = 4096 / count + 1;           // enough to fill the device, four pieces or more for each thread
+    blocks = blocks < most ? blocks : most;
+    hipLaunchKernelGGL(kv_copy_kernel, dim3((unsigned)count, (unsigned)blocks), dim3(256), 0, stream, c, src, dst, pitch, rows, n_rows, lens,
+                       add);
+    return hipGetLastError();
+}
+
+}  // namespace mxfp4

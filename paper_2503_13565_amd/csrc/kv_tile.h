@@ -1,0 +1,307 @@
+// What the attention kernels over a paged MXFP4 cache share: how the work of a batch is cut into workgroups, and how 32
+// cached tokens become operands of the matrix instructions in registers.
+#pragma once
+
+#include "common.h"
+#include "kv.h"
+
+namespace mxfp4 {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// Maximum over the four lanes that hold one query's scores (l, l + 16, l + 32, l + 48), in all of them.
+__device__ __forceinline__ float max_of_rows(float v)
+{
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+    v = fmaxf(__int_as_float(p[0]), __int_as_float(p[1]));
+    p = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return fmaxf(__int_as_float(p[0]), __int_as_float(p[1]));
+}
+__device__ __forceinline__ float sum_of_rows(float v)
+{
+    auto p = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
+    v = __int_as_float(p[0]) + __int_as_float(p[1]);
+    p = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
+    return __int_as_float(p[0]) + __int_as_float(p[1]);
+}
+
+// One workgroup's share: key/value head h, query tile `tile` and part s of S of sequence b.
+struct KvItem {
+    int b, h, tile, s, S;
+    int slot, slot0, slots;          // its partial result, that of part 0, and the step from one part to the next
+    int n, len, first;               // new tokens, cached tokens, first packed token of the sequence
+};
+
+__device__ __forceinline__ int wave_scan(int v)
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int u = __shfl_up(v, d);
+        v += lane >= d ? u : 0;
+    }
+    return v;
+}
+
+// A row's new tokens, its length (both held to what the tables can hold) and where its keys begin to count.
+struct KvRow {
+    int n, len, first, lo;
+};
+__device__ __forceinline__ KvRow kv_row(const KvAttend& a, int b)
+{
+    KvRow r;
+    if (a.b.starts) {
+        r.first = min(max(a.b.starts[b], 0), a.b.tokens);
+        r.n = min(max(a.b.starts[b + 1], r.first), a.b.tokens) - r.first;
+    } else {
+        r.first = b * a.b.per_row;
+        r.n = a.b.per_row;
+    }
+    r.len = min(max(a.b.lens[b], 0), a.b.width << a.c.shift);
+    r.lo = a.window > 0 ? max(0, min(r.len, r.len - r.n + 1 - a.window)) & ~31 : 0;
+    return r;
+}
+
+// The cutting.  A sequence's range of keys counts in units of kUnit tokens; with U units in all (every head, every
+// query tile) a part gets L = ceil(U / target) of them, so a row of n units has S = ceil(n / L) parts, and there are at most
+// target + (heads x tiles) workgroups.  Each finds its own share from the lengths, so that one launch fits any lengths, also those that
+// change between replays of a graph, and sequences of different lengths load the device evenly.  Only rows of two parts or more need
+// partial results: at most 2 target of them.
+template <int kUnit>
+__device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_rows, KvItem* out)
+{
+    const int lane = threadIdx.x & 63;
+    int64_t all = 0;
+    for (int base = 0; base < a.b.rows; base += 64) {
+        const int b = base + lane;
+        int64_t u = 0;
+        if (b < a.b.rows) {
+            const KvRow r = kv_row(a, b);
+            u = (int64_t)((r.n * a.group + tile_rows - 1) / tile_rows) * max(1, (r.len - r.lo + kUnit - 1) / kUnit);
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1)
+            u += __shfl_xor(u, d);
+        all += u;
+    }
+    const int each = (int)max((int64_t)1, (all * a.c.heads + a.target - 1) / a.target);
+    int before = 0, slots = 0;
+    for (int base = 0; base < a.b.rows; base += 64) {
+        const int b = base + lane;
+        KvRow r = {0, 0, 0, 0};
+        int parts = 1, tiles = 0;
+        if (b < a.b.rows) {
+            r = kv_row(a, b);
+            tiles = (r.n * a.group + tile_rows - 1) / tile_rows;
+            parts = max(1, ((r.len - r.lo + kUnit - 1) / kUnit + each - 1) / each);
+        }
+        const int mine = tiles * parts * a.c.heads;
+        const int upto = before + wave_scan(mine);
+        const int slots_upto = slots + wave_scan(parts > 1 ? mine : 0);
+        const uint64_t there = __ballot(upto > item);
+        if (there) {
+            const int at = __ffsll((unsigned long long)there) - 1;
+            const int local = item - __builtin_amdgcn_readlane(upto - mine, at);
+            const int S = __builtin_amdgcn_readlane(parts, at), T = __builtin_amdgcn_readlane(tiles, at);
+            out->b = base + at;
+            out->S = S;
+            out->h = local % a.c.heads;                  // neighbouring workgroups: the heads, so that a head's tiles meet in one L2
+            const int rest = local / a.c.heads;
+            out->tile = rest % T;
+            out->s = rest / T;
+            out->slots = T * a.c.heads;
+            out->slot0 = __builtin_amdgcn_readlane(slots_upto - (parts > 1 ? mine : 0), at) + out->tile * a.c.heads + out->h;
+            out->slot = out->slot0 + out->s * out->slots;
+            out->n = __builtin_amdgcn_readlane(r.n, at);
+            out->len = __builtin_amdgcn_readlane(r.len, at);
+            out->first = __builtin_amdgcn_readlane(r.first, at);
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(upto, 63);
+        slots = __builtin_amdgcn_readlane(slots_upto, 63);
+    }
+    return false;
+}
+
+// 32 tokens of one head as a wave loads them.  Keys: lane (r, g) = (lane % 16, lane / 16) has the NB dwords of tokens r and 16 + r
+// that hold elements 8 NB g .. 8 NB (g + 1) - 1, which are its eight elements of each of NB products (the queries are laid out to
+// match).  Values: lane (r, g) has tokens 4 g .. 4 g + 3 and 16 + 4 g .. 16 + 4 g + 3, the tokens whose weights the same lane gets
+// out of the score products; of each token elements kEl r .. kEl (r + 1) - 1 of every chunk of 16 kEl, so that
+// the eight tokens of one element are an operand without any crossing of lanes.
+// NB is 1, 2, 4 or 8; kPad: the head has fewer than 32 NB elements (96 of 128, 192 of 256), the lanes of the missing ones hold zeros.
+template <int NB, bool kPad>
+struct KvTile {
+    static constexpr int kEl = NB >= 4 ? 8 : NB == 2 ? 4 : 2;            // elements of a chunk in one lane
+    static constexpr int kChunk = 16 * kEl, kChunks = NB * 32 / kChunk;
+    static constexpr int kBlocks = kChunk / 32;                          // scale blocks of a chunk
+    static constexpr int kKs = NB == 8 ? 2 : 1;                          // scale blocks of a lane's key elements
+    uint32_t k[2][NB];
+    uint32_t v[2][4][kChunks];
+    uint32_t vs[2][kPad ? 4 * kChunks : NB];                             // four tokens' bytes as they lie, or a byte each
+    uint32_t ks[2][kKs];
+    int page[2];                                                         // of the two halves; -1: not there (uniform)
+};
+
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t* out, const uint8_t* p)
+{
+    if constexpr (N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const u32x4_t w = *reinterpret_cast<const u32x4_t*>(p + 4 * i);
+            out[i] = w[0], out[i + 1] = w[1], out[i + 2] = w[2], out[i + 3] = w[3];
+        }
+    } else if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            const uint2 w = *reinterpret_cast<const uint2*>(p + 4 * i);
+            out[i] = w.x, out[i + 1] = w.y;
+        }
+    } else {
+        out[0] = *reinterpret_cast<const uint32_t*>(p);
+    }
+}
+
+// Page of each half of 32 tiles of a wave, `step` tiles apart: lane 2 i + half has tile i's.  -1 where the table names none.
+template <int kStep>
+__device__ __forceinline__ int kv_pages32(const KvAttend& a, int b, int len, int tile)
+{
+    const int lane = threadIdx.x & 63;
+    const int at = (tile + (lane >> 1) * kStep) * 32 + (lane & 1) * 16;
+    return at < len ? kv_page(a.b.table, a.b.ldt, a.b.width, a.c.shift, a.c.pages, b, at) : -1;
+}
+
+template <int NB, bool kPad>
+__device__ __forceinline__ void load_tile(KvTile<NB, kPad>& t, const KvView& c, int h, int token, int page0, int page1)
+{
+    typedef KvTile<NB, kPad> T;
+    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int nb = kPad ? c.nb : NB;
+    t.page[0] = page0;
+    t.page[1] = page1;
+#pragma unroll
+    for (int a = 0; a < 2; ++a) {
+        const int page = max(t.page[a], 0);              // a half that is not there is read from page 0 and left out
+        const int64_t slot = ((int64_t)h << c.shift) + ((token + 16 * a) & ((1 << c.shift) - 1));
+        const uint8_t* kq = c.kq + (int64_t)page * c.psq + slot * (16 * nb);
+        const uint8_t* vq = c.vq + (int64_t)page * c.psq + slot * (16 * nb);
+        const uint8_t* ks = c.ks + (int64_t)page * c.pss + slot * nb;
+        const uint8_t* vs = c.vs + (int64_t)page * c.pss + slot * nb;
+#pragma unroll
+        for (int b = 0; b < T::kKs; ++b) {
+            const int block = T::kKs * g + b;            // (NB = 1, 2: a quarter, a half of a block in a lane)
+            const bool has = !kPad || block < nb;
+            t.ks[a][b] = 0;
+            if constexpr (NB >= 4) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    t.k[a][4 * b + i] = 0;
+                if (has)
+                    load_words<4>(&t.k[a][4 * b], kq + (r * nb + block) * 16);
+            } else {
+                load_words<NB>(t.k[a], kq + (r * 16 + 4 * g) * NB);
+            }
+            if (has)
+                t.ks[a][b] = ks[r * nb + (NB >= 4 ? block : (NB * g) >> 2)];
+        }
+        if constexpr (!kPad)
+            load_words<NB>(t.vs[a], vs + 4 * g * NB);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int ch = 0; ch < T::kChunks; ++ch) {
+                const uint8_t* p = vq + ((4 * g + i) * 16 * nb + ch * (T::kChunk / 2) + r * (T::kEl / 2));
+                if constexpr (kPad) {
+                    const int block = ch * T::kBlocks + ((r * T::kEl) >> 5);
+                    t.v[a][i][ch] = t.vs[a][i * T::kChunks + ch] = 0;
+                    if (block < nb) {
+                        t.v[a][i][ch] = *reinterpret_cast<const uint32_t*>(p);
+                        t.vs[a][i * T::kChunks + ch] = vs[(4 * g + i) * nb + block];
+                    }
+                } else {
+                    t.v[a][i][ch] = T::kEl == 8 ? *reinterpret_cast<const uint32_t*>(p)
+                                                : T::kEl == 4 ? (uint32_t)*reinterpret_cast<const uint16_t*>(p) : (uint32_t)*p;
+                }
+            }
+    }
+}
+
+// Eight elements of a dword of codes as BF16; byte 255 of the scale is NaN to the convert, 0 is 2^-127.
+__device__ __forceinline__ bf16x8_t eight_of(uint32_t w, uint32_t byte)
+{
+    const float s = __uint_as_float(byte << 23);
+    u32x4_t x;
+    x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+    x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+    x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+    x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+    return __builtin_bit_cast(bf16x8_t, x);
+}
+
+// The lane's eight key elements of product j of half a.
+template <int NB, bool kPad>
+__device__ __forceinline__ bf16x8_t key_operand(const KvTile<NB, kPad>& t, int a, int j)
+{
+    return eight_of(t.k[a][j], t.ks[a][KvTile<NB, kPad>::kKs == 2 ? j >> 2 : 0]);
+}
+
+// The scale byte of token i of half a, chunk ch, in this lane; and the byte made 0 (2^-127: zero codes are zeros with any but NaN).
+template <int NB, bool kPad>
+__device__ __forceinline__ int value_scale_shift(int i, int ch)
+{
+    typedef KvTile<NB, kPad> T;
+    return 8 * ((i * NB + ch * T::kBlocks) & 3) + 8 * (((threadIdx.x & 15) * T::kEl) >> 5);
+}
+template <int NB, bool kPad>
+__device__ __forceinline__ uint32_t value_scale(const KvTile<NB, kPad>& t, int a, int i, int ch)
+{
+    typedef KvTile<NB, kPad> T;
+    if constexpr (kPad)
+        return t.vs[a][i * T::kChunks + ch];
+    else
+        return (t.vs[a][(i * NB + ch * T::kBlocks) >> 2] >> value_scale_shift<NB, kPad>(i, ch)) & 0xFFu;
+}
+template <int NB, bool kPad>
+__device__ __forceinline__ void clear_value(KvTile<NB, kPad>& t, int a, int i, int ch)
+{
+    typedef KvTile<NB, kPad> T;
+    t.v[a][i][ch] = 0;
+    if constexpr (kPad)
+        t.vs[a][i * T::kChunks + ch] = 0;
+    else
+        t.vs[a][(i * NB + ch * T::kBlocks) >> 2] &= ~(0xFFu << value_scale_shift<NB, kPad>(i, ch));
+}
+
+// The lane's operands of one chunk of the values: x[e] holds its eight tokens of element kEl r + e.  Two tokens' converts
+// give pairs of elements; a byte permute each makes pairs of tokens of them (the scale differs from token to token, so the
+// tokens cannot be paired in front of the convert).
+template <int NB, bool kPad>
+__device__ __forceinline__ void value_operands(const KvTile<NB, kPad>& t, int ch, bf16x8_t* x)
+{
+    typedef KvTile<NB, kPad> T;
+    u32x4_t y[T::kEl];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        const int a = m >> 1, i = (m & 1) * 2;
+        const float s0 = __uint_as_float(value_scale(t, a, i, ch) << 23), s1 = __uint_as_float(value_scale(t, a, i + 1, ch) << 23);
+        const uint32_t w0 = t.v[a][i][ch], w1 = t.v[a][i + 1][ch];
+#define MXFP4_PAIR(e)                                                                                                     \
+    if constexpr (2 * e < T::kEl) {                                                                                       \
+        const uint32_t c0 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, s0, e));           \
+        const uint32_t c1 = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w1, s1, e));           \
+        y[2 * e][m] = __builtin_amdgcn_perm(c1, c0, 0x05040100u);                                                         \
+        y[2 * e + 1][m] = __builtin_amdgcn_perm(c1, c0, 0x07060302u);                                                     \
+    }
+        MXFP4_PAIR(0)
+        MXFP4_PAIR(1)
+        MXFP4_PAIR(2)
+        MXFP4_PAIR(3)
+#undef MXFP4_PAIR
+    }
+#pragma unroll
+    for (int e = 0; e < T::kEl; ++e)
+        x[e] = __builtin_bit_cast(bf16x8_t, y[e]);
+}
+
+}  // namespace mxfp4

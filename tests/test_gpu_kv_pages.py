@@ -1,0 +1,334 @@
+"""Into, out of and inside the paged MXFP4 cache: stored bits are those of the cast's oracle, tables and counts those of a
+plain model of who holds which page."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2503_13565_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+from helpers import DEV  # noqa: E402
+from kv_plain import Paged, cast, tokens, values  # noqa: E402
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def rotated(x, cos, sin, at):
+    """BF16 [t, h, d] turned as the header says: products and sums in FP32, each rounded, then BF16."""
+    half = cos.shape[1]
+    c, s = cos[at][:, None].numpy(), sin[at][:, None].numpy()
+    f = x.float().numpy()
+    a, b = f[..., :half], f[..., half: 2 * half]
+    out = np.concatenate([a * c - b * s, b * c + a * s, f[..., 2 * half:]], axis=-1)
+    return torch.from_numpy(out.astype(np.float32)).to(torch.bfloat16)
+
+
+def tables(length, d):
+    angle = torch.arange(length, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(d // 2, dtype=torch.float64) / (d // 2))
+    return angle.cos().float(), angle.sin().float()
+
+
+@pytest.mark.parametrize("dim,hq,hkv,page,rotary", [
+    (128, 4, 4, 16, 128), (128, 8, 1, 64, 64), (64, 2, 2, 32, 16), (32, 3, 1, 16, 32), (96, 5, 5, 16, 96), (192, 2, 1, 1024, 32),
+    (256, 1, 1, 128, 256), (64, 70, 3, 16, 0),
+])
+@pytest.mark.parametrize("ragged", [False, True])
+def test_append_and_read(dim, hq, hkv, page, rotary, ragged):
+    news = [3, 1, 0, 40, 9] if ragged else [5] * 5
+    p = Paged([max(n, m) for n, m in zip(news, [3, 50, 17, 40, 1000])], hkv, page, dim, seed=dim + page)
+    gen = torch.Generator().manual_seed(dim)
+    total = sum(news)
+    qkv = tokens(gen, total, hq + 2 * hkv, dim)
+    qkv[0, hq, :32] = 0.0                                             # a block of zeros, one with a NaN, one with an infinity
+    qkv[1, hq + hkv, 5] = float("nan")
+    qkv[1, hq + hkv - 1, dim - 1] = float("inf")
+    q, k, v = qkv.split([hq, hkv, hkv], dim=1)
+    at = np.concatenate([np.arange(n - m, n) for n, m in zip(p.lens, news)]).astype(np.int64)
+    row = np.repeat(np.arange(5), news)
+    rope = tables(1100, rotary) if rotary else None
+    cache, (table, lens) = p.cache(DEV), p.batch(DEV)
+    starts = ints([0, *np.cumsum(news)]) if ragged else None
+    g = qkv.to(DEV)
+    gq, gk, gv = g.split([hq, hkv, hkv], dim=1)
+    back = binding.mxfp4_kv_append(cache, gk, gv, table, lens, starts=starts, q=gq, rope=None if rope is None else tuple(x.to(DEV) for x in rope))
+    torch.cuda.synchronize()
+    turn = (lambda x: rotated(x, *rope, torch.from_numpy(at))) if rotary else (lambda x: x)
+    assert torch.equal(back.cpu().view(torch.int16), turn(q).contiguous().view(torch.int16))
+    pages, slots = p.table[row, at // page], at % page
+    for x, code, scale in ((turn(k), p.kq, p.ks), (v, p.vq, p.vs)):
+        code[pages, :, slots], scale[pages, :, slots] = cast(x)
+    for got, want in zip(cache, (p.kq, p.ks, p.vq, p.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+    rk, rv = binding.mxfp4_kv_read(cache, table, lens, total, starts=starts)
+    for got, code, scale in ((rk, p.kq, p.ks), (rv, p.vq, p.vs)):
+        assert np.array_equal(got.double().cpu().numpy(), values(code[pages, :, slots], scale[pages, :, slots]), equal_nan=True)
+
+
+def test_append_without_queries_with_positions_and_with_strides():
+    p = Paged([20, 9], 2, 16, 64, seed=1)
+    gen = torch.Generator().manual_seed(3)
+    k, v = tokens(gen, 8, 2, 64), tokens(gen, 8, 2, 64)
+    cos, sin = tables(40, 64)
+    where = [30, 31, 31, 32, 0, 39, 40, -1]                           # the last two are outside the tables
+    cache, (table, lens) = p.cache(DEV), p.batch(DEV)
+    wide = torch.zeros((8, 4, 2, 72), dtype=torch.bfloat16, device=DEV)
+    wide[:, 1, :, :64], wide[:, 3, :, 8:72] = k.to(DEV), v.to(DEV)
+    assert binding.mxfp4_kv_append(cache, wide[:, 1, :, :64], wide[:, 3, :, 8:72], table, lens, rope=(cos.to(DEV), sin.to(DEV)),
+                                   positions=ints(where)) is None
+    turned = rotated(k[:6], cos, sin, torch.tensor(where[:6]))
+    rk, rv = (x.double().cpu().numpy() for x in binding.mxfp4_kv_read(cache, table, lens, 8))
+    q, s = cast(turned)
+    assert np.array_equal(rk[:6], values(q, s)) and np.isnan(rk[6:]).all()
+    q, s = cast(v)
+    assert np.array_equal(rv, values(q, s))
+
+
+def test_tokens_without_a_place_are_left_out():
+    p = Paged([20, 9, 30], 1, 16, 64, seed=2)
+    before = [x.copy() for x in (p.kq, p.ks, p.vq, p.vs)]
+    cache, (table, lens) = p.cache(DEV), p.batch(DEV)
+    gen = torch.Generator().manual_seed(3)
+    k, v = tokens(gen, 6, 1, 64).to(DEV), tokens(gen, 6, 1, 64).to(DEV)
+    table[0, 1], table[1, 0] = -1, p.pages
+    lens[2] = 1                                                       # its first new token would stand at -1
+    binding.mxfp4_kv_append(cache, k, v, table, lens)
+    rk, rv = binding.mxfp4_kv_read(cache, table, lens, 6)
+    torch.cuda.synchronize()
+    page = p.table[2, 0]
+    for got, want in zip(cache, before):
+        got = got.cpu().numpy()
+        got[page, :, 0], want[page, :, 0] = 0, 0
+        assert np.array_equal(got, want)
+    assert not rk[:5].any() and not rv[:5].any() and rk[5].any()
+    lens[2] = 1 << 30                                                 # past the table
+    binding.mxfp4_kv_append(cache, k, v, table, lens)
+    for starts in ([5, 2, 9, -3], [0, 0, 0, 0], [-7, 100, 3, 1]):
+        binding.mxfp4_kv_append(cache, k, v, table, lens, starts=ints(starts))
+        binding.mxfp4_kv_read(cache, table, lens, 6, starts=ints(starts))
+    torch.cuda.synchronize()
+
+
+def test_many_rows_find_their_tokens():
+    rows = 300
+    rng = np.random.RandomState(0)
+    news = rng.randint(0, 4, rows)
+    news[5] = 70
+    p = Paged([int(n) + int(rng.randint(0, 40)) for n in news], 1, 16, 32, seed=3)
+    total = int(news.sum())
+    gen = torch.Generator().manual_seed(3)
+    k, v = tokens(gen, total, 1, 32), tokens(gen, total, 1, 32)
+    cache, (table, lens) = p.cache(DEV), p.batch(DEV)
+    starts = ints([0, *np.cumsum(news)])
+    binding.mxfp4_kv_append(cache, k.to(DEV), v.to(DEV), table, lens, starts=starts)
+    rk, rv = binding.mxfp4_kv_read(cache, table, lens, total, starts=starts)
+    assert np.array_equal(rk.double().cpu().numpy(), values(*cast(k))) and np.array_equal(rv.double().cpu().numpy(), values(*cast(v)))
+    at = np.concatenate([np.arange(n - m, n) for n, m in zip(p.lens, news)]).astype(np.int64)
+    row = np.repeat(np.arange(rows), news)
+    got = cache.kq.cpu().numpy()[p.table[row, at // 16], :, at % 16]
+    assert np.array_equal(got, cast(k)[0])
+
+
+class Model:
+    """Who holds which page, in plain Python."""
+
+    def __init__(self, pages, page, rows, width):
+        self.pages, self.page, self.width = pages, page, width
+        self.refs, self.table, self.lens = [0] * pages, [[] for _ in range(rows)], [0] * rows
+
+    def free(self):
+        return [p for p in range(self.pages) if self.refs[p] == 0]
+
+    def fork(self, src, dst):
+        for s, d in zip(src, dst):
+            self.table[d], self.lens[d] = list(self.table[s]), self.lens[s]
+            for p in self.table[d]:
+                self.refs[p] += 1
+
+    def extend(self, rows, add):
+        """(copies, missing)"""
+        plan, free, refs = [], self.free(), list(self.refs)
+        for r, a in zip(rows, add):
+            if self.lens[r] + a > self.width * self.page:
+                return None, -1
+        copies, lacking = [], 0
+        for r, a in zip(rows, add):
+            table, copy = list(self.table[r]), (-1, -1)
+            need = -(-(self.lens[r] + a) // self.page) - len(table)
+            if a and self.lens[r] % self.page and refs[table[-1]] > 1:
+                refs[table[-1]] -= 1
+                if free:
+                    copy = (table[-1], free.pop(0))
+                    refs[copy[1]] = 1
+                    table[-1] = copy[1]
+                else:
+                    lacking += 1
+            for _ in range(need):
+                if free:
+                    table.append(free.pop(0))
+                    refs[table[-1]] = 1
+                else:
+                    lacking += 1
+            copies.append(copy)
+            plan.append((r, table, self.lens[r] + a))
+        if lacking:
+            return None, lacking
+        self.refs = refs
+        for r, table, n in plan:
+            self.table[r], self.lens[r] = table, n
+        return copies, 0
+
+    def release(self, rows, keep):
+        for r, k in zip(rows, keep):
+            n = min(self.lens[r], max(k, 0))
+            for p in self.table[r][-(-n // self.page):]:
+                self.refs[p] -= 1
+            self.table[r], self.lens[r] = self.table[r][: -(-n // self.page)], n
+
+    def same(self, pool, table, lens):
+        assert lens.tolist() == self.lens
+        assert pool.refs.tolist() == self.refs
+        want = [t + [-1] * (self.width - len(t)) for t in self.table]
+        assert table.tolist() == want
+        bits = [(int(w) & 0xFFFFFFFF) >> i & 1 for w in pool.free.tolist() for i in range(32)]
+        assert bits[: self.pages] == [int(r == 0) for r in self.refs] and not any(bits[self.pages:])
+
+
+@pytest.mark.parametrize("pages,page,rows,width,seed", [(40, 16, 6, 5, 0), (33, 16, 9, 4, 1), (64, 32, 5, 20, 2), (70000, 16, 80, 40, 3), (31, 64, 4, 9, 4)])
+def test_pages_change_hands_as_in_the_model(pages, page, rows, width, seed):
+    rng = np.random.RandomState(seed)
+    m = Model(pages, page, rows, width)
+    pool = binding.mxfp4_kv_pool(pages, DEV)
+    cache = binding.mxfp4_kv_cache(pages, 1, page, 32, device=DEV)
+    cache.kq.copy_(torch.from_numpy(rng.randint(0, 256, cache.kq.shape).astype(np.uint8)))
+    table, lens = torch.full((rows, width), -1, dtype=torch.int32, device=DEV), torch.zeros(rows, dtype=torch.int32, device=DEV)
+    m.same(pool, table, lens)
+    for step in range(60):
+        what = rng.randint(3)
+        some = rng.permutation(rows)[: rng.randint(1, rows + 1)]
+        if what == 0:
+            empty = [r for r in range(rows) if m.lens[r] == 0]
+            full = [r for r in range(rows) if m.lens[r]]
+            if not full or not empty:
+                continue
+            dst = empty[: rng.randint(1, len(empty) + 1)]
+            src = [int(full[rng.randint(len(full))]) for _ in dst]
+            binding.mxfp4_kv_fork(pool, cache, table, lens, ints(src), ints(dst))
+            m.fork(src, dst)
+        elif what == 1:
+            add = rng.randint(0, 2 * page, len(some))
+            old = cache.kq.clone()
+            before, held = list(m.lens), dict(zip(some.tolist(), add.tolist()))
+            missing = binding.mxfp4_kv_extend(pool, cache, table, lens, ints(some), ints(add))
+            copies, lacking = m.extend(some.tolist(), add.tolist())
+            assert int(missing) == lacking, (step, int(missing), lacking)
+            for i, (a, b) in enumerate(copies or []):
+                if a >= 0:
+                    n = before[some[i]] % page
+                    assert torch.equal(cache.kq[b, :, :n], old[a, :, :n])
+                    old[b] = cache.kq[b]
+            assert torch.equal(old, cache.kq)
+        else:
+            keep = [int(rng.randint(-1, m.lens[r] + page)) if rng.rand() < 0.5 else 0 for r in some]
+            binding.mxfp4_kv_release(pool, cache, table, lens, ints(some), ints(keep))
+            m.release(some.tolist(), keep)
+        m.same(pool, table, lens)
+
+
+def test_rows_outside_and_full_pools_change_nothing():
+    pool, cache = binding.mxfp4_kv_pool(4, DEV), binding.mxfp4_kv_cache(4, 1, 16, 32, device=DEV)
+    table, lens = torch.full((3, 8), -1, dtype=torch.int32, device=DEV), torch.zeros(3, dtype=torch.int32, device=DEV)
+    m = Model(4, 16, 3, 8)
+    assert int(binding.mxfp4_kv_extend(pool, cache, table, lens, ints([0, 7, -1]), ints([40, 16, 16]))) == 0
+    m.extend([0], [40])
+    m.same(pool, table, lens)
+    assert int(binding.mxfp4_kv_extend(pool, cache, table, lens, ints([1, 2]), ints([16, 33]))) == 3
+    assert int(binding.mxfp4_kv_extend(pool, cache, table, lens, ints([0]), ints([89]))) == -1
+    assert int(binding.mxfp4_kv_extend(pool, cache, table, lens, ints([0, 1]), ints([-4, 0]))) == 0
+    binding.mxfp4_kv_fork(pool, cache, table, lens, ints([0, 9, 0]), ints([5, 1, -1]))
+    binding.mxfp4_kv_release(pool, cache, table, lens, ints([3, -1]), ints([0, 0]))
+    m.same(pool, table, lens)
+    binding.mxfp4_kv_fork(pool, cache, table, lens, ints([])[:0], ints([])[:0])
+
+
+@pytest.mark.parametrize("dim,heads,page", [(128, 4, 16), (64, 3, 32), (96, 2, 16), (256, 1, 64), (32, 5, 16), (192, 2, 128)])
+def test_compact(dim, heads, page):
+    rng = np.random.RandomState(dim)
+    lens, base = [500, 90, 40, 33, 5], [100, 17, 40, 0, 3]
+    p = Paged(lens, heads, page, dim, seed=dim)
+    counts = [300, 60, 0, 33, 1]
+    keep = np.zeros((5, 320), dtype=np.int32)
+    for b in range(5):
+        keep[b, : counts[b]] = np.sort(rng.permutation(lens[b] - base[b])[: counts[b]])
+    cache, (table, _) = p.cache(DEV), p.batch(DEV)
+    binding.mxfp4_kv_compact(cache, table, ints(base), torch.from_numpy(keep).to(DEV), ints(counts))
+    torch.cuda.synchronize()
+    for x in (p.kq, p.ks, p.vq, p.vs):
+        old = x.copy()
+        for b in range(5):
+            at = base[b] + keep[b, : counts[b]]
+            to = base[b] + np.arange(counts[b])
+            x[p.table[b, to // page], :, to % page] = old[p.table[b, at // page], :, at % page]
+    for got, want in zip(cache, (p.kq, p.ks, p.vq, p.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+    # numbers that name no token move nothing
+    bad = torch.full((5, 4), 1 << 30, dtype=torch.int32, device=DEV)
+    binding.mxfp4_kv_compact(cache, table, ints(base), bad, ints([4, 100, -3, 2, 1]))
+    binding.mxfp4_kv_compact(cache, table, ints([-9, 1 << 30, 5, 5, 0x7FFFFFFF]), bad, ints([4] * 5))
+    for got, want in zip(cache, (p.kq, p.ks, p.vq, p.vs)):
+        assert np.array_equal(got.cpu().numpy(), want)
+
+
+def test_copy_pages_and_layers():
+    rng = np.random.RandomState(0)
+    cache = binding.mxfp4_kv_cache(30, 2, 16, 96, layers=3, device=DEV)
+    for x in cache:
+        x.copy_(torch.from_numpy(rng.randint(0, 256, tuple(x.shape)).astype(np.uint8)))
+    want = [x.clone() for x in cache]
+    src, dst = [3, 4, -1, 29, 30, 7], [10, 11, 12, 0, 13, -2]
+    binding.mxfp4_kv_copy_pages(binding.mxfp4_kv_all_layers(cache), ints(src), ints(dst))
+    for x, y in zip(cache, want):
+        y[10], y[11], y[0] = y[3].clone(), y[4].clone(), y[29].clone()
+        assert torch.equal(x, y)
+
+
+def test_a_step_in_a_graph():
+    # fork, make room, store, attend, keep some, drop the rest: replayed with the eager calls between
+    def make():
+        gen = torch.Generator().manual_seed(0)
+        cache, pool = binding.mxfp4_kv_cache(64, 2, 16, 64, device=DEV), binding.mxfp4_kv_pool(64, DEV)
+        table, lens = torch.full((6, 16), -1, dtype=torch.int32, device=DEV), torch.zeros(6, dtype=torch.int32, device=DEV)
+        binding.mxfp4_kv_extend(pool, cache, table, lens, ints([0, 1]), ints([50, 37]))
+        k, v = tokens(gen, 87, 2, 64).to(DEV), tokens(gen, 87, 2, 64).to(DEV)
+        binding.mxfp4_kv_append(cache, k, v, table[:2], lens[:2], starts=ints([0, 50, 87]))
+        return dict(cache=cache, pool=pool, table=table, lens=lens, k=tokens(gen, 16, 2, 64).to(DEV), q=tokens(gen, 16, 4, 64).to(DEV),
+                    src=ints([0, 0, 1, 1]), dst=ints([2, 3, 4, 5]), four=ints([4] * 4), none=ints([0] * 4), zero=ints([0, 1]), two=ints([2, 3]),
+                    keep=ints([[0, 2, 3, 0]] * 4), counts=ints([3] * 4), base=torch.zeros(4, dtype=torch.int32, device=DEV))
+
+    def step(s):
+        b, args = binding, (s["pool"], s["cache"], s["table"], s["lens"])
+        b.mxfp4_kv_release(*args, s["dst"], s["none"])
+        b.mxfp4_kv_fork(*args, s["src"], s["dst"])
+        s["base"].copy_(s["lens"][2:])
+        missing = b.mxfp4_kv_extend(*args, s["dst"], s["four"])
+        b.mxfp4_kv_append(s["cache"], s["k"], s["k"], s["table"][2:], s["lens"][2:])
+        out = b.mxfp4_kv_attention(s["q"], s["cache"], s["table"][2:], s["lens"][2:])
+        b.mxfp4_kv_compact(s["cache"], s["table"][2:], s["base"], s["keep"], s["counts"])
+        b.mxfp4_kv_release(*args, s["dst"], s["base"] + s["counts"])
+        return out, missing
+
+    a, e = make(), make()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(a)
+    for i in range(4):
+        a["q"].mul_(0.5)
+        e["q"].mul_(0.5)
+        graph.replay()
+        want = step(e)
+        torch.cuda.synchronize()
+        assert int(got[1]) == 0 and int(want[1]) == 0 and torch.equal(got[0], want[0]), i
+        for x, y in zip([*a["cache"], *a["pool"], a["table"], a["lens"]], [*e["cache"], *e["pool"], e["table"], e["lens"]]):
+            assert torch.equal(x, y)
