@@ -65,6 +65,19 @@ def _cast(w):
     return _cast(w)
 
 
+class _Kv:
+    """The extension's calls of the paged cache; None from them as from the three above."""
+    append = read = attention = pages = compact = staticmethod(lambda *args: None)
+
+
+_kv = None
+
+
+def _kv_host():
+    load()
+    return _kv
+
+
 class GemmDesc(ctypes.Structure):
     """``mxfp4_gemm_desc`` of the header, field for field."""
     _fields_ = [("x_bf16", ctypes.c_void_p), ("M", ctypes.c_int64), ("ldx", ctypes.c_int64),
@@ -125,7 +138,7 @@ class Mxfp4Error(RuntimeError):
 
 def load() -> ctypes.CDLL:
     """Load the HIP library (torch first, so that both share one HIP runtime)."""
-    global _lib, _product, _verify, _cast
+    global _lib, _product, _verify, _cast, _kv
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -246,7 +259,7 @@ def load() -> ctypes.CDLL:
         getattr(lib, name).restype = i32
     lib.mxfp4_last_error.restype = ctypes.c_char_p
     lib.mxfp4_version.restype = ctypes.c_char_p
-    _product, _verify, _cast = _host_calls()
+    _product, _verify, _cast, _kv = _host_calls()
     _lib = lib
     return lib
 
@@ -261,9 +274,12 @@ def _host_calls():
     except ImportError as e:
         warnings.warn("the extension module _host cannot be used (%s): calls go through ctypes, which takes more host time; "
                       "build it with `python -m paper_2503_13565_amd.build`" % e, RuntimeWarning, stacklevel=3)
-        return (lambda *args: None,) * 3
+        return (*(lambda *args: None,) * 3, _Kv)
     _host.on_failure(_check)
-    return _host.product, _host.verify, _host.cast
+
+    class kv(_Kv):
+        append, read, attention, pages, compact = _host.kv_append, _host.kv_read, _host.kv_attention, _host.kv_pages, _host.kv_compact
+    return _host.product, _host.verify, _host.cast, kv
 
 
 def _check(rc: int) -> None:
@@ -1109,6 +1125,10 @@ def mxfp4_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, table: tor
     ends of their lengths ``lens`` int32 ``[rows]`` (which count them already).  ``rope``: (cos, sin) float32 ``[length, d/2]``
     turns the first d elements of ``k``, and of ``q`` into the tensor that is returned, at the tokens' places or at
     ``positions`` int32 ``[tokens]``.  ``starts`` int32 ``[rows + 1]``: whose rows are whose; None: the same number each."""
+    if q_out is None:
+        got = (_kv or _kv_host()).append(cache, k, v, table, lens, starts, q, rope, positions)
+        if got is not None:
+            return got if q is not None else None
     c = _kv_cache_desc(cache)
     dev, tokens = cache.kq.device, k.shape[0]
     b = _kv_rows_desc(table, lens, starts, tokens, dev)
@@ -1135,6 +1155,10 @@ def mxfp4_kv_append(cache: KvCache, k: torch.Tensor, v: torch.Tensor, table: tor
 def mxfp4_kv_read(cache: KvCache, table: torch.Tensor, lens: torch.Tensor, tokens: int, starts: Optional[torch.Tensor] = None,
                   out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """The last tokens of the sequences, ``tokens`` in all, as the values that the cache holds: (k, v) BF16 ``[tokens, heads, dim]``."""
+    if out is None:
+        out = (_kv or _kv_host()).read(cache, table, lens, tokens, starts)
+        if out is not None:
+            return out
     c = _kv_cache_desc(cache)
     dev = cache.kq.device
     b = _kv_rows_desc(table, lens, starts, tokens, dev)
@@ -1154,9 +1178,10 @@ _kv_workspaces = {}
 def _kv_workspace(device: torch.device, stream: int, need: int) -> torch.Tensor:
     if torch.cuda.is_current_stream_capturing():
         return torch.zeros((need,), dtype=torch.uint8, device=device)
-    ws = _kv_workspaces.get((device.index, stream))
+    key = stream * 64 + device.index
+    ws = _kv_workspaces.get(key)
     if ws is None or ws.numel() < need:
-        ws = _kv_workspaces[device.index, stream] = torch.zeros((need,), dtype=torch.uint8, device=device)
+        ws = _kv_workspaces[key] = torch.zeros((need,), dtype=torch.uint8, device=device)
     return ws
 
 
@@ -1174,6 +1199,10 @@ def mxfp4_kv_attention(q: torch.Tensor, cache: KvCache, table: torch.Tensor, len
     that the query sees new token m of its sequence, in place of the causal rule.  Returns BF16 ``[tokens, q_heads, dim]``, with
     ``return_lse`` also the logarithms of the softmax sums, float32 ``[tokens, q_heads]``.  ``workspace``: None takes the one that the binding
     keeps for the current stream."""
+    if out is None and workspace is None:
+        got = (_kv or _kv_host()).attention(q, cache, table, lens, starts, scale, causal, window, tree, return_lse, _kv_workspaces)
+        if got is not None:
+            return got
     c = _kv_cache_desc(cache)
     dev = cache.kq.device
     tokens = q.shape[0]
@@ -1214,6 +1243,8 @@ def _kv_two_lists(a: torch.Tensor, b: torch.Tensor, names: str, device) -> int:
 
 def mxfp4_kv_fork(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) -> None:
     """Sequence ``dst[i]`` (empty) becomes a second owner of what sequence ``src[i]`` holds; nothing is copied."""
+    if (_kv or _kv_host()).pages(0, *pool, cache, table, lens, src, dst):
+        return
     p, n = _kv_pool_desc(pool, cache, table, lens), _kv_two_lists(src, dst, "src and dst", pool.refs.device)
     with _on(pool.refs.device):
         _check(load().mxfp4_kv_fork(p, _ptr(src), _ptr(dst), n, _stream()))
@@ -1224,6 +1255,9 @@ def mxfp4_kv_extend(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: tor
     """Room for ``add[i]`` more tokens of sequence ``rows[i]``: pages are taken, a shared last page becomes a copy, ``lens`` grows.
     ``cache``: its pages hold all that belongs to a token (all layers).  Returns int32 ``[1]`` on the device: 0, or what is missing
     (pages, or -1 for a table that is too narrow); then nothing has changed."""
+    got = (_kv or _kv_host()).pages(2, *pool, cache, table, lens, rows, add)
+    if got is not None:
+        return got
     dev = pool.refs.device
     p, n = _kv_pool_desc(pool, cache, table, lens), _kv_two_lists(rows, add, "rows and add", dev)
     got = torch.empty((2 * n + 1,), dtype=torch.int32, device=dev)
@@ -1234,6 +1268,8 @@ def mxfp4_kv_extend(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: tor
 
 def mxfp4_kv_release(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: torch.Tensor, rows: torch.Tensor, keep: torch.Tensor) -> None:
     """Sequence ``rows[i]`` is cut down to its first ``keep[i]`` tokens (0: all of it is given up); pages that nobody holds any more are free."""
+    if (_kv or _kv_host()).pages(1, *pool, cache, table, lens, rows, keep):
+        return
     p, n = _kv_pool_desc(pool, cache, table, lens), _kv_two_lists(rows, keep, "rows and keep", pool.refs.device)
     with _on(pool.refs.device):
         _check(load().mxfp4_kv_release(p, _ptr(rows), _ptr(keep), n, _stream()))
@@ -1241,6 +1277,8 @@ def mxfp4_kv_release(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: to
 
 def mxfp4_kv_compact(cache: KvCache, table: torch.Tensor, base: torch.Tensor, keep: torch.Tensor, counts: torch.Tensor) -> None:
     """Token ``base[b] + keep[b, i]`` of sequence b moves to ``base[b] + i`` for i below ``counts[b]``; ``keep`` ascends."""
+    if (_kv or _kv_host()).compact(cache, table, base, keep, counts):
+        return
     c, dev = _kv_cache_desc(cache), cache.kq.device
     ldt, rows = _kv_table(table, dev), table.shape[0]
     _kv_ints(base, dev, "base", rows)

@@ -21,6 +21,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmxfp4_hip.so")
 HOST = os.path.join(HERE, "_host.so")
 SOURCES = ["api.hip", "cast.hip", "gemv.hip", "gemv_reg.hip", "gemv_short.hip", "chain.hip", "mfma.hip", "mfma_tile.hip", "bf16.hip", "e4m3.hip", "e2m3.hip", "mxfmt.hip", "gemm_t.hip", "gemv_tile.hip", "gemm_wide.hip", "gemm_wide_fmt.hip", "gemm_wide_bf16.hip", "kv_api.hip", "kv_store.hip", "kv_pages.hip", "kv_attend.hip"]
+HOST_SOURCES = ["host.cpp", "host_kv.cpp"]
 # packed FP32 instructions are disabled on purpose: see the build notes of this project
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -51,26 +52,26 @@ def _compile(src: str, verbose: bool, defines=()) -> str:
     return obj
 
 
-def _compile_host(verbose: bool) -> str:
+def _compile_host(src: str, verbose: bool) -> str:
     """The extension module behind the binding: host code against torch's headers."""
-    obj, at = os.path.join(BUILD, "host.o"), os.path.join(os.path.dirname(torch.__file__), "include")
+    obj, at = os.path.join(BUILD, os.path.splitext(src)[0] + ".o"), os.path.join(os.path.dirname(torch.__file__), "include")
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, '-DMXFP4_TORCH_VERSION="%s"' % torch.__version__,
            "-isystem", at, "-isystem",
            os.path.join(at, "torch", "csrc", "api", "include"), "-isystem", "/opt/rocm/include", "-isystem",
-           sysconfig.get_paths()["include"], "-c", os.path.join(CSRC, "host.cpp"), "-o", obj]
+           sysconfig.get_paths()["include"], "-c", os.path.join(CSRC, src), "-o", obj]
     if verbose:
         print(" ".join(cmd), flush=True)
     proc = subprocess.run(cmd, capture_output=True, text=True)
     if proc.returncode != 0:
-        raise RuntimeError("g++ failed on host.cpp:\n%s" % proc.stderr)
+        raise RuntimeError("g++ failed on %s:\n%s" % (src, proc.stderr))
     return obj
 
 
-def _link_host(obj: str, verbose: bool) -> None:
+def _link_host(objs, verbose: bool) -> None:
     """Linked against the library beside it, which the binding has loaded by then."""
     tmp, at = HOST + ".tmp.%d" % os.getpid(), os.path.join(os.path.dirname(torch.__file__), "lib")
-    cmd = ["g++", "-shared", "-o", tmp, obj, "-L" + HERE, "-l:" + os.path.basename(LIB), "-L" + at, "-ltorch_python",
+    cmd = ["g++", "-shared", "-o", tmp, *objs, "-L" + HERE, "-l:" + os.path.basename(LIB), "-L" + at, "-ltorch_python",
            "-ltorch_cpu", "-ltorch_hip", "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN"]
     if verbose:
         print(" ".join(cmd), flush=True)
@@ -84,7 +85,7 @@ def build(verbose: bool = True, jobs: int = 8, knobs: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     defines = ("-DMXFP4_MEASUREMENT_KNOBS",) if knobs else ()
     with ThreadPoolExecutor(max_workers=jobs) as ex:
-        host = ex.submit(_compile_host, verbose)
+        host = [ex.submit(_compile_host, src, verbose) for src in HOST_SOURCES]
         objs = list(ex.map(lambda s: _compile(s, verbose, defines), SOURCES))
     tmp = LIB + ".tmp.%d" % os.getpid()
     cmd = [_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp, *objs]
@@ -92,7 +93,7 @@ def build(verbose: bool = True, jobs: int = 8, knobs: bool = False) -> str:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
     os.replace(tmp, LIB)
-    _link_host(host.result(), verbose)
+    _link_host([h.result() for h in host], verbose)
     return LIB
 
 

@@ -6,39 +6,14 @@
 // allocation and the marshalling of the Python form took longer than the launch (2.4 us of a call's host time here).  us of host
 // time per call, Python form -> here: one row 6.9 -> 3.5, fused 7.7 -> 3.8, BF16 weights 7.0 -> 3.7, tile-major 6.9 -> 3.6,
 // verification (two launches) 14.2 -> 7.6, a cast (two outputs) 7.5 -> 4.4.
-#include <ATen/ATen.h>
-#include <c10/core/impl/TorchDispatchModeTLS.h>
-#include <c10/hip/HIPFunctions.h>
-#include <c10/hip/HIPStream.h>
-#include <ATen/PythonTorchFunctionTLS.h>
-#include <ATen/hip/EmptyTensor.h>
-#include <c10/core/impl/LocalDispatchKeySet.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/python_variable.h>
-
-#include "../../include/mxfp4.h"
+#include "host.h"
 
 namespace {
 
-PyObject* g_failed = nullptr;                       // raises the error of a status code
+using namespace mxfp4_host;
 
 // The kinds of binding.py: 0 MXFP4, 1 E4M3, 2 E2M3, 3 BF16, 4 the tile-major copy, 16 + id the formats chosen by id.
 enum { kMx = 0, kE4m3 = 1, kE2m3 = 2, kBf16 = 3, kTiled = 4, kFmt = 16 };
-
-// A tensor whose memory and sizes are what they say: exactly torch.Tensor (or Parameter) and no transform, mode or lazy bit.
-const at::Tensor* plain(PyObject* o, at::ScalarType type, c10::Device device)
-{
-    static const uint64_t allowed =
-        c10::DispatchKeySet({c10::DispatchKey::CUDA, c10::DispatchKey::AutogradCUDA, c10::DispatchKey::ADInplaceOrView,
-                             c10::DispatchKey::AutocastCUDA}).raw_repr();
-    if (!THPVariable_CheckExact(o))
-        return nullptr;
-    const at::Tensor& t = THPVariable_Unpack(o);
-    if (!t.defined() || (t.key_set().raw_repr() & ~allowed) != 0 || t.scalar_type() != type || t.device() != device ||
-        !t.has_storage())
-        return nullptr;
-    return &t;
-}
 
 const at::Tensor* rows_of(PyObject* o, c10::Device device)       // [rows, columns] BF16, columns side by side
 {
@@ -107,32 +82,6 @@ bool operands(PyObject* const* args, int* kind, Operands* o)
     return true;
 }
 
-// A new tensor on the device: from the allocator behind torch.empty, without the way through the dispatcher, unless something on this
-// thread wants to see it there (a transform; autocast and the keys that every thread has do not).  One row of
-// 4096 x 4096, which the host bounds: 4.35 -> 4.17 us from call to call.
-at::Tensor fresh(at::IntArrayRef size, at::ScalarType type, c10::Device device)
-{
-    static const uint64_t usual = (c10::default_included_set | c10::autocast_dispatch_keyset).raw_repr();
-    if ((c10::impl::tls_local_dispatch_key_set().included_.raw_repr() & ~usual) != 0)
-        return at::empty(size, at::TensorOptions().dtype(type).device(device));
-    return at::Tensor(at::detail::empty_cuda(size, type, device, std::nullopt));
-}
-
-// What the binding's own checks take over: also a number that is none or too large, whose error they raise in their words.
-PyObject* left()
-{
-    PyErr_Clear();
-    Py_RETURN_NONE;
-}
-
-bool small(PyObject* o, int* v)                     // an int of the C interface as it stands
-{
-    int over = 0;
-    const long long wide = PyLong_Check(o) ? PyLong_AsLongLongAndOverflow(o, &over) : 0;
-    *v = (int)wide;
-    return PyLong_Check(o) && over == 0 && wide == *v;
-}
-
 struct Scratch {
     void* at = nullptr;
     size_t bytes = 0;
@@ -149,36 +98,6 @@ bool scratch(PyObject* o, c10::Device device, Scratch* s)
     s->bytes = (size_t)t->numel();
     return true;
 }
-
-PyObject* finish(int rc, PyObject* (*wrap)(const at::Tensor*), const at::Tensor* out)
-{
-    if (rc == 0)
-        return wrap(out);
-    PyObject* raised = PyObject_CallFunction(g_failed, "i", rc);
-    Py_XDECREF(raised);
-    if (!PyErr_Occurred())
-        PyErr_SetString(PyExc_RuntimeError, "mxfp4: status without an error");
-    return nullptr;
-}
-
-PyObject* wrap_one(const at::Tensor* t) { return THPVariable_Wrap(t[0]); }
-
-PyObject* wrap_list(const at::Tensor* t, int count)
-{
-    PyObject* tuple = PyTuple_New(count);
-    for (int i = 0; tuple && i < count; ++i) {
-        PyObject* item = THPVariable_Wrap(t[i]);
-        if (!item) {
-            Py_DECREF(tuple);
-            return nullptr;
-        }
-        PyTuple_SET_ITEM(tuple, i, item);
-    }
-    return tuple;
-}
-
-PyObject* wrap_three(const at::Tensor* t) { return wrap_list(t, 3); }
-PyObject* wrap_two(const at::Tensor* t) { return wrap_list(t, 2); }
 
 // product(kind, x, q, s, n, k, fused, bias, act, residual, path, workspace) -> y, or None
 PyObject* product(PyObject*, PyObject* const* args, Py_ssize_t count)
@@ -333,7 +252,8 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_host", nullptr, -1, kMethods, nu
 PyMODINIT_FUNC PyInit__host()
 {
     PyObject* module = PyModule_Create(&kModule);
-    if (module && PyModule_AddStringConstant(module, "torch_version", MXFP4_TORCH_VERSION) < 0) {
+    if (module && (PyModule_AddFunctions(module, mxfp4_host::kv_methods) < 0 ||
+                   PyModule_AddStringConstant(module, "torch_version", MXFP4_TORCH_VERSION) < 0)) {
         Py_DECREF(module);
         return nullptr;
     }

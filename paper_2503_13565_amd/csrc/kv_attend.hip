@@ -28,12 +28,18 @@ __device__ __forceinline__ bool kv_sees(const KvSight& s, bool tree, int j)
     return ok;
 }
 
+// Stores and loads that all dies of the device see alike.
+__device__ __forceinline__ void put_through(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get_through(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
 template <int NB, int QT, bool kPad>
 __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAttend a)
 {
     typedef KvTile<NB, kPad> T;
     constexpr int NW = 4, kRows = 16 * QT, kEl = T::kEl, kChunks = T::kChunks;
+    constexpr int kDepth = QT == 1 ? 3 : 2;
     constexpr int kSlot = QT * NB * 512 + 32 * QT;                     // floats of a partial result
+    constexpr int kJoin = 8, kFinal = 8192;                            // parts added at a time; where the counters of the last sums begin
     __shared__ __align__(16) float comb[NW][kEl][4][64];
     __shared__ float ml[NW][QT][16][2];
     __shared__ int last;
@@ -194,7 +200,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
         }
     };
 
-    // Tiles t_begin + wave, + 4, ...: the next one is asked for before the present one is used.
+    // Tiles t_begin + wave, + 4, ...: kDepth - 1 of them are on their way while one is used.
     int pages = 0, loaded = 0;
     auto load = [&](T& t, int tile) {
         if ((loaded & 31) == 0)
@@ -205,21 +211,22 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     };
     int tile = t_begin + wave;
     if (tile < t_end) {
-        T x, y;
-        load(x, tile);
-        while (true) {
-            if (tile + NW < t_end)
-                load(y, tile + NW);
-            compute(x, tile);
-            tile += NW;
-            if (tile >= t_end)
-                break;
-            if (tile + NW < t_end)
-                load(x, tile + NW);
-            compute(y, tile);
-            tile += NW;
-            if (tile >= t_end)
-                break;
+        T t[kDepth];
+#pragma unroll
+        for (int d = 0; d < kDepth - 1; ++d)
+            if (tile + d * NW < t_end)
+                load(t[d], tile + d * NW);
+        for (bool more = true; more;) {
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                if (tile + (kDepth - 1) * NW < t_end)
+                    load(t[(d + kDepth - 1) % kDepth], tile + (kDepth - 1) * NW);
+                compute(t[d], tile);
+                tile += NW;
+                more = tile < t_end;
+                if (!more)
+                    break;
+            }
         }
     }
 
@@ -232,7 +239,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
             ml[wave][qt][c][1] = l[qt];
         }
     }
-    float* part = a.part + (int64_t)it.slot * kSlot;
+    float* part = a.part + (int64_t)(it.slot0 + it.s * it.slots) * kSlot;
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         float f[NW], top = -INFINITY, total = 0.f;
@@ -275,16 +282,16 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                         y[e / 2] = f32_to_bf16_rne2(r[e] * inv, r[e + 1] * inv);
                     __builtin_memcpy(__builtin_assume_aligned(to, kEl * 2), y, kEl * 2);
                 }
-            } else {
+            } else if (out_at[qt] >= 0) {
 #pragma unroll
                 for (int e = 0; e < kEl; ++e)
-                    part[((qt * 2 * NB + ch * kEl + e) * 4 + wave) * 64 + lane] = r[e];
+                    put_through(&part[((qt * 2 * NB + ch * kEl + e) * 4 + wave) * 64 + lane], r[e]);
             }
         }
         if (wave == 0 && g == 0) {
             if (it.S > 1) {
-                part[QT * NB * 512 + qt * 32 + c] = top;
-                part[QT * NB * 512 + qt * 32 + 16 + c] = total;
+                put_through(&part[QT * NB * 512 + qt * 32 + c], top);
+                put_through(&part[QT * NB * 512 + qt * 32 + 16 + c], total);
             } else if (a.lse && out_at[qt] >= 0) {
                 const int row = row0 + qt * 16 + c, i = row / a.group;
                 a.lse[(int64_t)(it.first + i) * (a.group * a.c.heads) + it.h * a.group + row - i * a.group] =
@@ -295,57 +302,108 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     if (it.S == 1)
         return;
 
-    // Parts of one row of keys: the workgroup that comes last adds all of them, in their order whoever it is.  Nobody waits.
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0)
-        last = atomicAdd(&a.counters[it.slot0], 1u) == (uint32_t)it.S - 1;
-    __syncthreads();
-    if (!last)
-        return;
-    __threadfence();
-    if (threadIdx.x == 0)
-        a.counters[it.slot0] = 0;
+    // Parts of one row of keys: of every kJoin parts the workgroup that comes last adds them, of these the one that comes last
+    // again, in the order of the parts whoever it is.  Nobody waits.  The parts go past the L2 (each die has its own) with coherent stores,
+    // which have arrived when the wave's counter of stores is at zero, so that the count needs no write-back of a whole L2 in front of
+    // it: with __threadfence() in that place 1024 workgroups took 245 us over 131071 tokens instead of 123.
     const float* parts = a.part + (int64_t)it.slot0 * kSlot;
-    const int64_t step = (int64_t)it.slots * kSlot;
+    int first = it.s - it.s % kJoin, count = min(kJoin, it.S - first), step = 1;
+    bool done = it.S <= kJoin;
+    uint32_t* counter = &a.counters[it.slot0 + first * it.slots];
+    while (true) {
+        drain_vmem();
+        __syncthreads();
+        if (threadIdx.x == 0)
+            last = __hip_atomic_fetch_add(counter, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)count - 1;
+        __syncthreads();
+        if (!last)
+            return;
+        if (threadIdx.x == 0)
+            __hip_atomic_store(counter, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        const float* from = parts + (int64_t)first * it.slots * kSlot;
+        const int64_t pitch = (int64_t)step * it.slots * kSlot;
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-        float top = -INFINITY, total = 0.f;
-        for (int s = 0; s < it.S; ++s)
-            top = fmaxf(top, parts[s * step + QT * NB * 512 + qt * 32 + c]);
-        float r[2 * NB];
-#pragma unroll
-        for (int e = 0; e < 2 * NB; ++e)
-            r[e] = 0.f;
-#pragma unroll 2
-        for (int s = 0; s < it.S; ++s) {
-            const float* x = parts + s * step;
-            const float ms = x[QT * NB * 512 + qt * 32 + c], ls = x[QT * NB * 512 + qt * 32 + 16 + c];
-            const float f = ls != ls ? __uint_as_float(0x7FC00000u) : ms == -INFINITY ? 0.f : exp2f((ms - top) * scale);
-            total += f * ls;
+        for (int qt = 0; qt < QT; ++qt) {
+            const bool live = out_at[qt] >= 0;
+            float top = -INFINITY, total = 0.f;
+            float r[2 * NB];
 #pragma unroll
             for (int e = 0; e < 2 * NB; ++e)
-                r[e] += f * x[((qt * 2 * NB + e) * 4 + wave) * 64 + lane];
-        }
-        if (out_at[qt] < 0)
-            continue;
-        const float inv = total == 0.f ? 0.f : 1.f / total;
+                r[e] = 0.f;
+            if (live) {
+                for (int s = 0; s < count; s += kJoin) {               // (more than kJoin only for the last sum of very many parts)
+                    float ms[kJoin], ls[kJoin], x[kJoin][2 * NB];
 #pragma unroll
-        for (int ch = 0; ch < kChunks; ++ch) {
-            if (kPad && ch * T::kChunk + kEl * (4 * g + wave) >= 32 * a.c.nb)
+                    for (int k = 0; k < kJoin; ++k) {
+                        const float* p = from + min(s + k, count - 1) * pitch;
+                        ms[k] = get_through(&p[QT * NB * 512 + qt * 32 + c]);
+                        ls[k] = get_through(&p[QT * NB * 512 + qt * 32 + 16 + c]);
+#pragma unroll
+                        for (int e = 0; e < 2 * NB; ++e)
+                            x[k][e] = get_through(&p[((qt * 2 * NB + e) * 4 + wave) * 64 + lane]);
+                    }
+                    float now = top;
+#pragma unroll
+                    for (int k = 0; k < kJoin; ++k)
+                        now = fmaxf(now, ms[k]);
+                    const float old = top == -INFINITY ? 0.f : exp2f((top - now) * scale);
+                    total *= old;
+#pragma unroll
+                    for (int e = 0; e < 2 * NB; ++e)
+                        r[e] *= old;
+                    top = now;
+#pragma unroll
+                    for (int k = 0; k < kJoin; ++k) {
+                        float f = ms[k] == -INFINITY ? 0.f : exp2f((ms[k] - now) * scale);
+                        f = ls[k] != ls[k] ? __uint_as_float(0x7FC00000u) : f;
+                        f = s + k < count ? f : 0.f;
+                        total += f * (s + k < count ? ls[k] : 0.f);
+#pragma unroll
+                        for (int e = 0; e < 2 * NB; ++e)
+                            r[e] += s + k < count ? f * x[k][e] : 0.f;
+                    }
+                }
+            }
+            if (!done) {
+                float* to = const_cast<float*>(from);                  // in the place of the first of them
+                if (live) {
+#pragma unroll
+                    for (int e = 0; e < 2 * NB; ++e)
+                        put_through(&to[((qt * 2 * NB + e) * 4 + wave) * 64 + lane], r[e]);
+                }
+                if (wave == 0 && g == 0) {
+                    put_through(&to[QT * NB * 512 + qt * 32 + c], top);
+                    put_through(&to[QT * NB * 512 + qt * 32 + 16 + c], total);
+                }
                 continue;
-            uint16_t* to = a.out.p + out_at[qt] + ch * T::kChunk + kEl * (4 * g + wave);
-            uint32_t y[kEl / 2];
+            }
+            if (!live)
+                continue;
+            const float inv = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
-            for (int e = 0; e < kEl; e += 2)
-                y[e / 2] = f32_to_bf16_rne2(r[ch * kEl + e] * inv, r[ch * kEl + e + 1] * inv);
-            __builtin_memcpy(__builtin_assume_aligned(to, kEl * 2), y, kEl * 2);
+            for (int ch = 0; ch < kChunks; ++ch) {
+                if (kPad && ch * T::kChunk + kEl * (4 * g + wave) >= 32 * a.c.nb)
+                    continue;
+                uint16_t* to = a.out.p + out_at[qt] + ch * T::kChunk + kEl * (4 * g + wave);
+                uint32_t y[kEl / 2];
+#pragma unroll
+                for (int e = 0; e < kEl; e += 2)
+                    y[e / 2] = f32_to_bf16_rne2(r[ch * kEl + e] * inv, r[ch * kEl + e + 1] * inv);
+                __builtin_memcpy(__builtin_assume_aligned(to, kEl * 2), y, kEl * 2);
+            }
+            if (a.lse && wave == 0 && g == 0) {
+                const int row = row0 + qt * 16 + c, i = row / a.group;
+                a.lse[(int64_t)(it.first + i) * (a.group * a.c.heads) + it.h * a.group + row - i * a.group] =
+                    total == 0.f ? -INFINITY : (top * scale + log2f(total)) * kLn2;
+            }
         }
-        if (a.lse && wave == 0 && g == 0) {
-            const int row = row0 + qt * 16 + c, i = row / a.group;
-            a.lse[(int64_t)(it.first + i) * (a.group * a.c.heads) + it.h * a.group + row - i * a.group] =
-                total == 0.f ? -INFINITY : (top * scale + log2f(total)) * kLn2;
-        }
+        if (done)
+            return;
+        count = (it.S + kJoin - 1) / kJoin;                            // and now the sums of the groups
+        first = 0;
+        step = kJoin;
+        done = true;
+        counter = &a.counters[kFinal + it.slot0];
     }
 }
 
@@ -356,12 +414,25 @@ static int query_tiles(int nb, int64_t queries) { return queries <= 16 || nb > 4
 static int padded(int nb) { return nb == 3 ? 4 : nb == 6 ? 8 : nb; }
 
 // Workgroups that the cutting aims for: as many as run at once.
-static int attend_target(int nb, const DeviceInfo& dev) { return dev.cus * (nb <= 4 ? 2 : 1); }
+static int attend_target(int nb, const DeviceInfo& dev)
+{
+    if (const char* e = knob("MXFP4_KV_TARGET"))                       // measurement only
+        return atoi(e);
+    return dev.cus * (nb <= 4 ? 2 : 1);
+}
+
+// Units of 128 tokens that a part has at least.
+static int attend_least()
+{
+    if (const char* e = knob("MXFP4_KV_LEAST"))                        // measurement only
+        return atoi(e);
+    return 2;
+}
 
 size_t kv_attend_part_bytes(int nb, int group, int64_t tokens, int64_t rows, const DeviceInfo& dev)
 {
     const int qt = query_tiles(nb, rows ? (tokens * group + rows - 1) / rows : 0);
-    return (size_t)2 * attend_target(nb, dev) * (qt * padded(nb) * 512 + 32 * qt) * sizeof(float);
+    return ((size_t)2 * attend_target(nb, dev) + 8) * (qt * padded(nb) * 512 + 32 * qt) * sizeof(float);
 }
 
 template <int NB, bool kPad>
@@ -379,6 +450,7 @@ hipError_t launch_kv_attend(KvAttend a, const DeviceInfo& dev, hipStream_t strea
 {
     const int qt = query_tiles(a.c.nb, ((int64_t)a.b.tokens * a.group + a.b.rows - 1) / a.b.rows);
     a.target = attend_target(a.c.nb, dev);
+    a.least = attend_least();
     // No more workgroups than shares: target + tiles x heads by the cutting, and no more than the tables' units.
     const int64_t per = 16 * qt;
     const int64_t tiles = a.b.starts ? (int64_t)a.b.tokens * a.group / per + a.b.rows : a.b.rows * (((int64_t)a.b.per_row * a.group + per - 1) / per);

@@ -29,18 +29,24 @@ __device__ __forceinline__ float sum_of_rows(float v)
 // One workgroup's share: key/value head h, query tile `tile` and part s of S of sequence b.
 struct KvItem {
     int b, h, tile, s, S;
-    int slot, slot0, slots;          // its partial result, that of part 0, and the step from one part to the next
+    int slot0, slots;                // the partial result of part 0, and the step from one part to the next
     int n, len, first;               // new tokens, cached tokens, first packed token of the sequence
 };
 
+// Inclusive sums over the wave's lanes, in the vector unit (through the LDS crossbar a step waits for its answer).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_or_zero(int v)
+{
+    return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false);
+}
 __device__ __forceinline__ int wave_scan(int v)
 {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int u = __shfl_up(v, d);
-        v += lane >= d ? u : 0;
-    }
+    v += dpp_or_zero<0x111, 0xF>(v);         // row_shr 1, 2, 4, 8: sums within 16 lanes
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);         // the last lane of rows 0 and 2 to rows 1 and 3
+    v += dpp_or_zero<0x143, 0xC>(v);         // lane 31 to the upper half
     return v;
 }
 
@@ -67,32 +73,32 @@ __device__ __forceinline__ KvRow kv_row(const KvAttend& a, int b)
 // query tile) a part gets L = ceil(U / target) of them, so a row of n units has S = ceil(n / L) parts, and there are at most
 // target + (heads x tiles) workgroups.  Each finds its own share from the lengths, so that one launch fits any lengths, also those that
 // change between replays of a graph, and sequences of different lengths load the device evenly.  Only rows of two parts or more need
-// partial results: at most 2 target of them.
+// partial results: at most 2 target of them (U is summed in FP32, which all workgroups do alike; a few more for its rounding).  A part
+// has at least `least` units: below that the joining costs more than the walk.
 template <int kUnit>
 __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_rows, KvItem* out)
 {
     const int lane = threadIdx.x & 63;
-    int64_t all = 0;
+    KvRow r0 = {0, 0, 0, 0};
+    float all = 0.f;
     for (int base = 0; base < a.b.rows; base += 64) {
-        const int b = base + lane;
-        int64_t u = 0;
-        if (b < a.b.rows) {
-            const KvRow r = kv_row(a, b);
-            u = (int64_t)((r.n * a.group + tile_rows - 1) / tile_rows) * max(1, (r.len - r.lo + kUnit - 1) / kUnit);
+        float u = 0.f;
+        if (base + lane < a.b.rows) {
+            const KvRow r = kv_row(a, base + lane);
+            u = (float)((r.n * a.group + tile_rows - 1) / tile_rows) * (float)max(1, (r.len - r.lo + kUnit - 1) / kUnit);
+            if (base == 0)
+                r0 = r;
         }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1)
-            u += __shfl_xor(u, d);
-        all += u;
+        all += wave_sum(u);
     }
-    const int each = (int)max((int64_t)1, (all * a.c.heads + a.target - 1) / a.target);
+    const int each = (int)fminf(fmaxf((float)a.least, ceilf(all * (float)a.c.heads / (float)a.target)), 1e9f);
     int before = 0, slots = 0;
     for (int base = 0; base < a.b.rows; base += 64) {
-        const int b = base + lane;
-        KvRow r = {0, 0, 0, 0};
+        KvRow r = r0;
         int parts = 1, tiles = 0;
-        if (b < a.b.rows) {
-            r = kv_row(a, b);
+        if (base + lane < a.b.rows) {
+            if (base)
+                r = kv_row(a, base + lane);
             tiles = (r.n * a.group + tile_rows - 1) / tile_rows;
             parts = max(1, ((r.len - r.lo + kUnit - 1) / kUnit + each - 1) / each);
         }
@@ -112,7 +118,6 @@ __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_ro
             out->s = rest / T;
             out->slots = T * a.c.heads;
             out->slot0 = __builtin_amdgcn_readlane(slots_upto - (parts > 1 ? mine : 0), at) + out->tile * a.c.heads + out->h;
-            out->slot = out->slot0 + out->s * out->slots;
             out->n = __builtin_amdgcn_readlane(r.n, at);
             out->len = __builtin_amdgcn_readlane(r.len, at);
             out->first = __builtin_amdgcn_readlane(r.first, at);
@@ -183,11 +188,9 @@ __device__ __forceinline__ void load_tile(KvTile<NB, kPad>& t, const KvView& c, 
 #pragma unroll
     for (int a = 0; a < 2; ++a) {
         const int page = max(t.page[a], 0);              // a half that is not there is read from page 0 and left out
-        const int64_t slot = ((int64_t)h << c.shift) + ((token + 16 * a) & ((1 << c.shift) - 1));
-        const uint8_t* kq = c.kq + (int64_t)page * c.psq + slot * (16 * nb);
-        const uint8_t* vq = c.vq + (int64_t)page * c.psq + slot * (16 * nb);
-        const uint8_t* ks = c.ks + (int64_t)page * c.pss + slot * nb;
-        const uint8_t* vs = c.vs + (int64_t)page * c.pss + slot * nb;
+        const int slot = (h << c.shift) + ((token + 16 * a) & ((1 << c.shift) - 1));
+        const int64_t at_q = (int64_t)page * c.psq + (int64_t)slot * (16 * nb), at_s = (int64_t)page * c.pss + (int64_t)slot * nb;
+        const uint8_t *kq = c.kq + at_q, *vq = c.vq + at_q, *ks = c.ks + at_s, *vs = c.vs + at_s;
 #pragma unroll
         for (int b = 0; b < T::kKs; ++b) {
             const int block = T::kKs * g + b;            // (NB = 1, 2: a quarter, a half of a block in a lane)
