@@ -50,7 +50,7 @@ struct KvAttend {
     int group, causal;                       // query heads per key/value head
     int window;                              // 0: none
     float scale;                             // times log2(e)
-    int target, least;                       // workgroups that the cutting of long rows aims for; units of a part at least
+    int target;                              // workgroups that the cutting of long rows aims for
     uint32_t* counters;
     float* part;
 };

@@ -39,7 +39,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     constexpr int NW = 4, kRows = 16 * QT, kEl = T::kEl, kChunks = T::kChunks;
     constexpr int kDepth = QT == 1 ? 3 : 2;
     constexpr int kSlot = QT * NB * 512 + 32 * QT;                     // floats of a partial result
-    constexpr int kJoin = 8, kFinal = 8192;                            // parts added at a time; where the counters of the last sums begin
+    constexpr int kJoin = kKvJoin, kFinal = 8192;                         // parts added at a time; where the counters of the last sums begin
     __shared__ __align__(16) float comb[NW][kEl][4][64];
     __shared__ float ml[NW][QT][16][2];
     __shared__ int last;
@@ -414,25 +414,12 @@ static int query_tiles(int nb, int64_t queries) { return queries <= 16 || nb > 4
 static int padded(int nb) { return nb == 3 ? 4 : nb == 6 ? 8 : nb; }
 
 // Workgroups that the cutting aims for: as many as run at once.
-static int attend_target(int nb, const DeviceInfo& dev)
-{
-    if (const char* e = knob("MXFP4_KV_TARGET"))                       // measurement only
-        return atoi(e);
-    return dev.cus * (nb <= 4 ? 2 : 1);
-}
-
-// Units of 128 tokens that a part has at least.
-static int attend_least()
-{
-    if (const char* e = knob("MXFP4_KV_LEAST"))                        // measurement only
-        return atoi(e);
-    return 2;
-}
+static int attend_target(int nb, const DeviceInfo& dev) { return dev.cus * (nb <= 4 ? 2 : 1); }
 
 size_t kv_attend_part_bytes(int nb, int group, int64_t tokens, int64_t rows, const DeviceInfo& dev)
 {
     const int qt = query_tiles(nb, rows ? (tokens * group + rows - 1) / rows : 0);
-    return ((size_t)2 * attend_target(nb, dev) + 8) * (qt * padded(nb) * 512 + 32 * qt) * sizeof(float);
+    return ((size_t)4 * attend_target(nb, dev) + 8) * (qt * padded(nb) * 512 + 32 * qt) * sizeof(float);
 }
 
 template <int NB, bool kPad>
@@ -450,12 +437,11 @@ hipError_t launch_kv_attend(KvAttend a, const DeviceInfo& dev, hipStream_t strea
 {
     const int qt = query_tiles(a.c.nb, ((int64_t)a.b.tokens * a.group + a.b.rows - 1) / a.b.rows);
     a.target = attend_target(a.c.nb, dev);
-    a.least = attend_least();
-    // No more workgroups than shares: target + tiles x heads by the cutting, and no more than the tables' units.
+    // No more workgroups than shares: 2 target + tiles x heads by the cutting, and no more than the tables' units.
     const int64_t per = 16 * qt;
     const int64_t tiles = a.b.starts ? (int64_t)a.b.tokens * a.group / per + a.b.rows : a.b.rows * (((int64_t)a.b.per_row * a.group + per - 1) / per);
     const int64_t units = (((int64_t)a.b.width << a.c.shift) + 127) / 128;
-    int64_t blocks = tiles * a.c.heads + a.target;
+    int64_t blocks = tiles * a.c.heads + 2 * a.target;
     if (tiles * a.c.heads * units < blocks)
         blocks = tiles * a.c.heads * units;
     if (blocks > 0x7FFFFFFF)

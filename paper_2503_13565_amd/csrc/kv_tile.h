@@ -18,6 +18,13 @@ __device__ __forceinline__ float max_of_rows(float v)
     p = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
     return fmaxf(__int_as_float(p[0]), __int_as_float(p[1]));
 }
+__device__ __forceinline__ float max_of_wave(float v)
+{
+    v = fmaxf(v, dpp_f32<0xB1>(v));
+    v = fmaxf(v, dpp_f32<0x4E>(v));
+    v = fmaxf(v, dpp_f32<0x141>(v));
+    return max_of_rows(fmaxf(v, dpp_f32<0x140>(v)));
+}
 __device__ __forceinline__ float sum_of_rows(float v)
 {
     auto p = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
@@ -70,28 +77,40 @@ __device__ __forceinline__ KvRow kv_row(const KvAttend& a, int b)
 }
 
 // The cutting.  A sequence's range of keys counts in units of kUnit tokens; with U units in all (every head, every
-// query tile) a part gets L = ceil(U / target) of them, so a row of n units has S = ceil(n / L) parts, and there are at most
-// target + (heads x tiles) workgroups.  Each finds its own share from the lengths, so that one launch fits any lengths, also those that
+// query tile) a part gets about L = U / target of them, so a row of n units has ceil(n / L) parts, and there are at most
+// 2 target + (heads x tiles) workgroups.  Each finds its own share from the lengths, so that one launch fits any lengths, also those that
 // change between replays of a graph, and sequences of different lengths load the device evenly.  Only rows of two parts or more need
-// partial results: at most 2 target of them (U is summed in FP32, which all workgroups do alike; a few more for its rounding).  A part
-// has at least `least` units: below that the joining costs more than the walk.
+// partial results: at most 4 target of them (U is summed in FP32, which all workgroups do alike; a few more for its rounding).
+// What the parts aim for (64 query heads on 8, dim 128, us):
+//   long parts   `target` of them, all at once (16 rows of 32000 tokens: 112; twice as many 119), but twice as many where the
+//                longest row is over the mean by a quarter, and parts of one length do not come out (64 rows of 500 to 16384 tokens: 81, not 86)
+//   short ones   (up to `brief` units: 16 with one query tile, 8 with two) half of `target`, because joining costs more than it
+//                saves (4 rows of 16000 tokens: 21.6, not 23.3)
+//   a row alone  no more than the kJoin parts that are joined at a time, unless that leaves a part over four units
+//                (one row of 2000 tokens: 9.1, and 10.7 with parts of one unit); whole up to six units (32 heads, 500 tokens: 7.8, not 10.1)
+constexpr int kKvJoin = 8;
 template <int kUnit>
 __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_rows, KvItem* out)
 {
+    const int brief = tile_rows <= 16 ? 16 : 8;
     const int lane = threadIdx.x & 63;
     KvRow r0 = {0, 0, 0, 0};
-    float all = 0.f;
+    float all = 0.f, longest = 0.f;
     for (int base = 0; base < a.b.rows; base += 64) {
         float u = 0.f;
         if (base + lane < a.b.rows) {
             const KvRow r = kv_row(a, base + lane);
             u = (float)((r.n * a.group + tile_rows - 1) / tile_rows) * (float)max(1, (r.len - r.lo + kUnit - 1) / kUnit);
+            longest = fmaxf(longest, u);
             if (base == 0)
                 r0 = r;
         }
         all += wave_sum(u);
     }
-    const int each = (int)fminf(fmaxf((float)a.least, ceilf(all * (float)a.c.heads / (float)a.target)), 1e9f);
+    longest = max_of_wave(longest);
+    const float even = ceilf(all * (float)a.c.heads / (float)a.target);
+    const float full = longest * (float)a.b.rows > 1.25f * all && even > (float)brief ? ceilf(0.5f * even) : even;
+    const int each = (int)fminf(fmaxf(full, fminf(2.f * even, (float)brief)), 1e9f);
     int before = 0, slots = 0;
     for (int base = 0; base < a.b.rows; base += 64) {
         KvRow r = r0;
@@ -100,7 +119,9 @@ __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_ro
             if (base)
                 r = kv_row(a, base + lane);
             tiles = (r.n * a.group + tile_rows - 1) / tile_rows;
-            parts = max(1, ((r.len - r.lo + kUnit - 1) / kUnit + each - 1) / each);
+            const int units = max(1, (r.len - r.lo + kUnit - 1) / kUnit);
+            const int mine = max(each, units <= 6 ? units : min((units + kKvJoin - 1) / kKvJoin, 4));
+            parts = (units + mine - 1) / mine;
         }
         const int mine = tiles * parts * a.c.heads;
         const int upto = before + wave_scan(mine);
