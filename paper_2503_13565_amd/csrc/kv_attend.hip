@@ -13,25 +13,6 @@
 
 namespace mxfp4 {
 
-// What a query may see, for the lane's column of query tile qt.
-struct KvSight {
-    int lo, hi;                      // positions lo .. hi - 1
-    uint64_t tree;                   // and, from `base` on, the bits that are set
-    int base;
-};
-
-__device__ __forceinline__ bool kv_sees(const KvSight& s, bool tree, int j)
-{
-    bool ok = j >= s.lo && j < s.hi;
-    if (tree && j >= s.base)
-        ok = ok && j - s.base < 64 && ((s.tree >> (j - s.base)) & 1);
-    return ok;
-}
-
-// Stores and loads that all dies of the device see alike.
-__device__ __forceinline__ void put_through(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ float get_through(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-
 template <int NB, int QT, bool kPad>
 __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAttend a)
 {
@@ -46,7 +27,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     KvItem it;
-    if (!kv_find<NW * 32>(a, blockIdx.x, kRows, &it))
+    if (!kv_find<NW * 32>(a, blockIdx.x, kRows, QT == 1 ? 16 : 8, QT == 1 ? 3 : 4, &it))
         return;                                                        // (the whole workgroup)
     const int rows = it.n * a.group, row0 = it.tile * kRows;
     const int i0 = row0 / a.group, i1 = min((row0 + kRows - 1) / a.group, it.n - 1);
@@ -54,24 +35,21 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     const int hi = causal ? max(0, min(it.len, it.len - it.n + i1 + 1)) : it.len;
     const int lo = a.window > 0 ? max(0, it.len - it.n + i0 + 1 - a.window) & ~31 : 0;
     const int tiles = max(0, (hi - lo + 31) >> 5);
-    const int t_begin = (lo >> 5) + (int)((int64_t)tiles * it.s / it.S), t_end = (lo >> 5) + (int)((int64_t)tiles * (it.s + 1) / it.S);
+    const int t_begin = (lo >> 5) + part_begin(tiles, it.s, it.S), t_end = (lo >> 5) + part_begin(tiles, it.s + 1, it.S);
     // tiles from `plain_lo` on and up to `plain_hi` need no mask: every query of this workgroup sees all of their tokens
     const int plain_hi = causal ? it.len - it.n + i0 + 1 : tree ? it.len - it.n : it.len;
     const int plain_lo = a.window > 0 ? it.len - it.n + i1 + 1 - a.window : 0;
 
     bf16x8_t q[QT][NB];
-    KvSight sight[QT];
+    const KvSight sight = {it.len - it.n, a.window, causal, tree};
+    int at_q[QT];                                                      // the positions of the lane's queries
     int64_t out_at[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const int row = row0 + qt * 16 + c;
         const int i = row / a.group, head = it.h * a.group + row - i * a.group;
         const bool live = row < rows;
-        const int p = it.len - it.n + i;
-        sight[qt].lo = a.window > 0 ? p - a.window + 1 : 0;
-        sight[qt].hi = !live ? 0 : causal ? p + 1 : it.len;
-        sight[qt].base = it.len - it.n;
-        sight[qt].tree = tree && live ? a.tree[it.first + i] : 0;
+        at_q[qt] = live ? it.len - it.n + i : kNobody;
         out_at[qt] = live ? (int64_t)(it.first + i) * a.out.token + (int64_t)head * a.out.head : -1;
         const uint16_t* from = a.q.p + (int64_t)(it.first + (live ? i : 0)) * a.q.token + (int64_t)(live ? head : it.h * a.group) * a.q.head;
 #pragma unroll
@@ -111,6 +89,10 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
             }
         uint32_t nan_at = 0;                                           // bit (chunk, half, token): a NaN block, taken out of the values
         if (masked) {
+            uint64_t word[QT];
+#pragma unroll
+            for (int qt = 0; qt < QT; ++qt)
+                word[qt] = sight.word(a, it, at_q[qt]);
             // Tokens behind the end and pages that are not there: whatever lies in the memory must not reach the sums.
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -121,7 +103,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                     const bool there = 4 * g + i < here;
 #pragma unroll
                     for (int qt = 0; qt < QT; ++qt)
-                        s[qt][h][i] = there && kv_sees(sight[qt], tree, j) ? s[qt][h][i] : -INFINITY;
+                        s[qt][h][i] = there && sight.sees(at_q[qt], word[qt], j) ? s[qt][h][i] : -INFINITY;
 #pragma unroll
                     for (int ch = 0; ch < kChunks; ++ch) {
                         const bool bad = value_scale(t, h, i, ch) == 0xFFu;
@@ -136,31 +118,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
         bf16x8_t p[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
-            float top = fmaxf(fmaxf(fmaxf(s[qt][0][0], s[qt][0][1]), fmaxf(s[qt][0][2], s[qt][0][3])),
-                              fmaxf(fmaxf(s[qt][1][0], s[qt][1][1]), fmaxf(s[qt][1][2], s[qt][1][3])));
-            top = max_of_rows(top);
-            // The sums move to a new maximum only when it is 2^8 above the old one: the weights then stay below 2^8, which FP32 sums and
-            // BF16 weights hold as well as weights up to 1.
-            if (__ballot((top - m[qt]) * scale > 8.f || (m[qt] == -INFINITY && top > -INFINITY))) {
-                const float now = fmaxf(m[qt], top);
-                const float f = now == -INFINITY ? 1.f : exp2f((m[qt] - now) * scale);
-                m[qt] = now;
-                l[qt] *= f;
-#pragma unroll
-                for (int e = 0; e < 2 * NB; ++e)
-                    o[qt][e] *= f;
-            }
-            const float off = m[qt] == -INFINITY ? 0.f : -m[qt] * scale;
-            float w[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                w[i] = __builtin_amdgcn_exp2f(fmaf(s[qt][i >> 2][i & 3], scale, off));
-                l[qt] += w[i];
-            }
-            // rounded to BF16 (the type of the values' product; half a step, 2^-8 of a weight at most, and the weights' errors average out)
-            typedef __attribute__((ext_vector_type(4))) uint32_t words;
-            p[qt] = __builtin_bit_cast(bf16x8_t, (words{f32_to_bf16_rne2(w[0], w[1]), f32_to_bf16_rne2(w[2], w[3]),
-                                                        f32_to_bf16_rne2(w[4], w[5]), f32_to_bf16_rne2(w[6], w[7])}));
+            p[qt] = softmax_step<2 * NB>(s[qt], scale, &m[qt], &l[qt], o[qt]);
         }
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
@@ -185,16 +143,11 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
 #pragma unroll
                 for (int qt = 0; qt < QT; ++qt) {
                     ones y;
+                    const uint64_t word = sight.word(a, it, at_q[qt]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        y[i] = kv_sees(sight[qt], tree, j0 + 16 * (i >> 2) + 4 * g + (i & 3)) ? 0x3F80 : 0;
-                    const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, y),
-                                                                                f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                    for (int e = 0; e < kEl; ++e)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            o[qt][ch * kEl + e][i] = hit[i] > 0.f ? __uint_as_float(0x7FC00000u) : o[qt][ch * kEl + e][i];
+                        y[i] = sight.sees(at_q[qt], word, j0 + 16 * (i >> 2) + 4 * g + (i & 3)) ? 0x3F80 : 0;
+                    mark_nan<kEl>(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, y), &o[qt][ch * kEl]);
                 }
             }
         }

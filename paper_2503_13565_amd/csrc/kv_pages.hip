@@ -48,106 +48,125 @@ __global__ __launch_bounds__(256) void kv_release_kernel(KvPool p, const int32_t
     }
 }
 
-// Inclusive sum over the workgroup's 1024 threads, in thread order; `sums` holds a number per wave.
-__device__ __forceinline__ int block_scan(int v, int* sums)
+// Inclusive sums over a wave's lanes, in the vector unit.
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int shifted_or_zero(int v)
+{
+    return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false);
+}
+__device__ __forceinline__ int scan_of_wave(int v)
+{
+    v += shifted_or_zero<0x111, 0xF>(v);
+    v += shifted_or_zero<0x112, 0xF>(v);
+    v += shifted_or_zero<0x114, 0xF>(v);
+    v += shifted_or_zero<0x118, 0xF>(v);
+    v += shifted_or_zero<0x142, 0xA>(v);
+    v += shifted_or_zero<0x143, 0xC>(v);
+    return v;
+}
+
+// Inclusive sum over the workgroup's 1024 threads, in thread order, and the sum of all; `sums` holds a number per wave.
+__device__ __forceinline__ int block_scan(int v, int* sums, int* all)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int u = __shfl_up(v, d);
-        v += lane >= d ? u : 0;
-    }
+    v = scan_of_wave(v);
     __syncthreads();                             // (the last scan's sums are read)
     if (lane == 63)
         sums[wave] = v;
     __syncthreads();
-    int before = 0;
-    for (int w = 0; w < 16; ++w)
-        before += w < wave ? sums[w] : 0;
-    return v + before;
+    const int upto = scan_of_wave(lane < 16 ? sums[lane] : 0);
+    *all = __builtin_amdgcn_readlane(upto, 15);
+    const int before = __builtin_amdgcn_readlane(upto, max(__builtin_amdgcn_readfirstlane(wave) - 1, 0));
+    return v + (wave ? before : 0);
 }
 
 // One workgroup of 1024 threads: the rows are scanned for what each needs, the free bits for the pages of the lowest numbers.
 // Free pages are dealt out 1024 words (32768 pages) at a time: their numbers go to a list in the LDS in order, then every
 // page finds its row by bisection among the rows' sums.  Latency-bound: a chain of some twelve loads, scans and barriers.
+// kEach: rows of a thread, 1 up to 1024 rows, 4 up to 4096.
+template <int kEach>
 __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t* rows, const int32_t* add, int count, int32_t* copies,
                                                          int32_t* missing)
 {
-    extern __shared__ int lds[];
-    int* sum = lds;                              // needs of rows 0 .. i together
-    int* mine = sum + kKvMaxRows;                // the page that a row would leave, or -1
-    int* first = mine + kKvMaxRows;              // where a row's first new page goes
-    uint16_t* list = reinterpret_cast<uint16_t*>(first + kKvMaxRows);
-    __shared__ int sums[16], bad, found;
-    constexpr int kEach = kKvMaxRows / 1024;
+    extern __shared__ __align__(16) int lds[];
+    constexpr int kRows = 1024 * kEach;
+    int* mine = lds;                             // the page that a row would leave, or -1
+    int* sum = mine + kRows;                     // needs of rows 0 .. i together
+    int* first = sum + kRows;                    // where a row's first new page goes
+    uint16_t* list = reinterpret_cast<uint16_t*>(first + kRows);
+    __shared__ int sums[16], bad;
     const int tid = threadIdx.x;
     if (tid == 0)
-        bad = found = 0;
+        bad = 0;
+    const int words = (p.pages + 31) >> 5;
+    const uint32_t word0 = tid < words ? p.bits[tid] : 0u;             // (asked for before the rows' chain of loads)
     int n[kEach], a[kEach], row[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         const int i = tid * kEach + j;
         row[j] = i < count ? rows[i] : -1;
+        a[j] = i < count ? max(add[i], 0) : 0;
         if ((unsigned)row[j] >= (unsigned)p.rows)
             row[j] = -1;
         n[j] = row[j] < 0 ? 0 : max(p.lens[row[j]], 0);
-        a[j] = row[j] < 0 ? 0 : max(add[i], 0);
+        a[j] = row[j] < 0 ? 0 : a[j];
     }
+    int have = __popc(word0);
+    for (int w = 1024 + tid; w < words; w += 1024)
+        have += __popc(p.bits[w]);
     __syncthreads();
+    int refs[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        const int i = tid * kEach + j;
         int page = -1;
+        refs[j] = 0;
         if ((int64_t)n[j] + a[j] > ((int64_t)p.width << p.shift)) {
             bad = 1;
             n[j] = a[j] = 0;
         } else if (a[j] > 0 && (n[j] & ((1 << p.shift) - 1))) {
             page = p.table[(int64_t)row[j] * p.ldt + (n[j] >> p.shift)];
-            if ((unsigned)page >= (unsigned)p.pages || p.refs[page] < 2)
+            if ((unsigned)page < (unsigned)p.pages)
+                refs[j] = p.refs[page];
+            if (refs[j] < 2)
                 page = -1;
         }
-        mine[i] = page;
+        mine[tid * kEach + j] = page;
     }
-    __syncthreads();
+    int free_pages;
+    block_scan(have, sums, &free_pages);         // (its barriers also show everybody `mine`)
     int need[kEach], own = 0;
     bool copy[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        const int i = tid * kEach + j;
+        const int i = tid * kEach + j, page = mine[i];
         copy[j] = false;
-        if (mine[i] >= 0) {
+        if (page >= 0) {
             int before = 0;                      // rows in front of this one that leave the same page
-            for (int k = 0; k < i; ++k)
-                before += mine[k] == mine[i];
-            copy[j] = p.refs[mine[i]] - before > 1;
+            const int4* at = reinterpret_cast<const int4*>(mine);
+            for (int k = 0; k < i >> 2; ++k)
+                before += (at[k].x == page) + (at[k].y == page) + (at[k].z == page) + (at[k].w == page);
+            for (int k = i & ~3; k < i; ++k)
+                before += mine[k] == page;
+            copy[j] = refs[j] - before > 1;
         }
         const int w = pages_of(n[j], p.shift);
         need[j] = pages_of(n[j] + a[j], p.shift) - w + copy[j];
         first[i] = w - copy[j];
         own += need[j];
     }
-    const int all = block_scan(own, sums);
-    int at = all - own;
+    int total;
+    int at = block_scan(own, sums, &total) - own;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
+        const int i = tid * kEach + j;
         at += need[j];
-        sum[tid * kEach + j] = at;
+        sum[i] = at;
         if (!copy[j])
-            mine[tid * kEach + j] = -1;          // (everybody has counted: the scan above has barriers)
+            mine[i] = -1;                        // (everybody has counted: the scan above has barriers)
     }
-    __syncthreads();
-    const int total = sum[kKvMaxRows - 1];
-    const int words = (p.pages + 31) >> 5;
-    int have = 0;
-    for (int w = tid; w < words; w += 1024)
-        have += __popc(p.bits[w]);
-    have = block_scan(have, sums);
-    if (tid == 1023)
-        found = have;
-    __syncthreads();
-    if (bad || found < total) {                  // the same for all: nothing is changed
+    if (bad || free_pages < total) {             // the same for all: nothing is changed
         if (tid == 0)
-            *missing = bad ? -1 : total - found;
+            *missing = bad ? -1 : total - free_pages;
         for (int i = tid; i < count; i += 1024)
             copies[2 * i] = copies[2 * i + 1] = -1;
         return;
@@ -166,11 +185,10 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
     }
     int done = 0;
     for (int w0 = 0; done < total; w0 += 1024) {
-        const uint32_t word = w0 + tid < words ? p.bits[w0 + tid] : 0u;
+        const uint32_t word = w0 == 0 ? word0 : w0 + tid < words ? p.bits[w0 + tid] : 0u;
         const int c = __popc(word);
-        const int upto = block_scan(c, sums);
-        if (tid == 1023)
-            found = upto;
+        int found;
+        const int upto = block_scan(c, sums, &found);
         const int left = total - done;           // of this tile's free pages, the first `left` are taken
         int k = upto - c;
         uint32_t rest = word;
@@ -185,7 +203,7 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
         const int got = min(found, left);
         for (int r = tid; r < got; r += 1024) {
             const int rank = done + r, page = w0 * 32 + list[r];
-            int lo = 0, hi = kKvMaxRows - 1;     // the first row whose sum passes the rank
+            int lo = 0, hi = kRows - 1;          // the first row whose sum passes the rank
             while (lo < hi) {
                 const int m = (lo + hi) >> 1;
                 if (sum[m] > rank)
@@ -194,10 +212,9 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
                     lo = m + 1;
             }
             const int k2 = rank - (lo ? sum[lo - 1] : 0);
-            const int r2 = rows[lo];
             const int w = first[lo] + k2;
             p.refs[page] = 1;
-            p.table[(int64_t)r2 * p.ldt + w] = page;
+            p.table[(int64_t)rows[lo] * p.ldt + w] = page;
             if (k2 == 0 && mine[lo] >= 0) {      // the first one takes the place of the page that others hold too
                 copies[2 * lo] = mine[lo];
                 copies[2 * lo + 1] = page;
@@ -218,12 +235,14 @@ hipError_t launch_kv_fork(const KvPool& p, const int32_t* src, const int32_t* ds
 hipError_t launch_kv_extend(const KvPool& p, const int32_t* rows, const int32_t* add, int count, int32_t* copies,
                             int32_t* missing, hipStream_t stream)
 {
-    constexpr int kBytes = 3 * kKvMaxRows * 4 + 1024 * 32 * 2;
-    static LdsLimit limit;
-    const hipError_t e = limit.raise(reinterpret_cast<const void*>(kv_extend_kernel), kBytes);
+    const bool few = count <= 1024;
+    auto kernel = few ? kv_extend_kernel<1> : kv_extend_kernel<4>;
+    const int bytes = 3 * 4 * (few ? 1024 : kKvMaxRows) + 1024 * 32 * 2;
+    static LdsLimit limit[2];
+    const hipError_t e = limit[few].raise(reinterpret_cast<const void*>(kernel), bytes);
     if (e != hipSuccess)
         return e;
-    hipLaunchKernelGGL(kv_extend_kernel, dim3(1), dim3(1024), kBytes, stream, p, rows, add, count, copies, missing);
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(1024), bytes, stream, p, rows, add, count, copies, missing);
     return hipGetLastError();
 }
 

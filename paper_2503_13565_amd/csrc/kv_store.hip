@@ -6,93 +6,144 @@
 
 namespace mxfp4 {
 
-// Eight values of one head turned by their positions.  `x`: the head's elements e .. e + 7; the partners of the
-// pairs (i, i + dim / 2) are dim / 2 further or before, another load of the same lines.  Each product is rounded to FP32 on its
-// own (no fused multiply-add), so that the BF16 result does not depend on how a compiler contracts.
-__device__ __forceinline__ u32x4_t turn8(u32x4_t own, const uint16_t* head, int e, const KvRope& rope, int pos)
+// Eight pairs of elements turned by eight angles: (x, y) -> (x cos - y sin, y cos + x sin).  Each product is rounded to FP32 on its
+// own (no fused multiply-add), so that the BF16 result does not depend on how a compiler contracts.  kFirst, kSecond: which
+// of the two is wanted.
+template <bool kFirst, bool kSecond>
+__device__ __forceinline__ void turn8(u32x4_t* x, u32x4_t* y, const KvRope& rope, int pos, int i)
 {
 #pragma clang fp contract(off)
-    const int half = rope.dim >> 1;
-    const bool second = e >= half;
-    const int i = second ? e - half : e;
-    const u32x4_t other = *reinterpret_cast<const u32x4_t*>(head + (second ? i : i + half));
     const bool inside = (unsigned)pos < (unsigned)rope.length;
-    const int64_t at = (int64_t)(inside ? pos : 0) * half + i;
+    const int64_t at = (int64_t)(inside ? pos : 0) * (rope.dim >> 1) + i;
     f32x4_t c[2], s[2];
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
         c[j] = *reinterpret_cast<const f32x4_t*>(rope.cos + at + 4 * j);
         s[j] = *reinterpret_cast<const f32x4_t*>(rope.sin + at + 4 * j);
     }
-    const float wrong = inside ? 0.f : __uint_as_float(0x7FC00000u);
-    u32x4_t out;
+    const float wrong = __uint_as_float(0x7FC00000u);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        float r[2];
+        float r[2], t[2];
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            const float x = bf16_bits_to_f32(k ? own[j] >> 16 : own[j] & 0xFFFFu);
-            const float y = bf16_bits_to_f32(k ? other[j] >> 16 : other[j] & 0xFFFFu);
-            const float a = x * c[(2 * j + k) >> 2][(2 * j + k) & 3];
-            const float b = y * s[(2 * j + k) >> 2][(2 * j + k) & 3];
-            const float t = second ? a + b : a - b;
-            r[k] = inside ? t : wrong;
+            const float u = bf16_bits_to_f32(k ? (*x)[j] >> 16 : (*x)[j] & 0xFFFFu);
+            const float v = bf16_bits_to_f32(k ? (*y)[j] >> 16 : (*y)[j] & 0xFFFFu);
+            const float co = c[(2 * j + k) >> 2][(2 * j + k) & 3], si = s[(2 * j + k) >> 2][(2 * j + k) & 3];
+            const float uc = u * co, vs = v * si, vc = v * co, us = u * si;
+            r[k] = inside ? uc - vs : wrong;
+            t[k] = inside ? vc + us : wrong;
         }
-        out[j] = f32_to_bf16_rne2(r[0], r[1]);
+        if (kFirst)
+            (*x)[j] = f32_to_bf16_rne2(r[0], r[1]);
+        if (kSecond)
+            (*y)[j] = f32_to_bf16_rne2(t[0], t[1]);
     }
-    return out;
 }
 
-// A workgroup takes 256 groups of eight elements of one token: the heads of q, then of k, then of v.  A quad of lanes has one
-// 32-element block, as in the cast of a whole tensor.  Bound by latency for a step's few tokens (the token's row, its
-// length and its page are one load behind the other, the elements are asked for in front of them) and by HBM for prompts.
+// A token's place in the cache, for one head.
+struct KvSlot {
+    uint8_t* q;
+    uint8_t* s;
+};
+__device__ __forceinline__ KvSlot kv_slot(const KvView& c, bool keys, int page, int head, int at)
+{
+    const int64_t slot = (head << c.shift) + (at & ((1 << c.shift) - 1));
+    return {(keys ? c.kq : c.vq) + (int64_t)page * c.psq + slot * (c.nb * 16), (keys ? c.ks : c.vs) + (int64_t)page * c.pss + slot * c.nb};
+}
+
+// Eight elements cast and stored; a quad of lanes has one block.  (All four take part, also without a page.)
+__device__ __forceinline__ void kv_put(const u32x4_t x, const KvSlot& to, bool there, int e)
+{
+    uint32_t packed;
+    int scale;
+    cast_group<true>(x, &packed, &scale);
+    if (!there)
+        return;
+    *reinterpret_cast<uint32_t*>(to.q + (e >> 1)) = packed;
+    if ((e & 31) == 0)
+        to.s[e >> 5] = (uint8_t)scale;
+}
+
+// Heads whose elements i and i + dim / 2 are turned together (or not at all), with whole blocks in either half: a thread takes
+// eight of each half of a head of q, then of k, then of v, so that the angles are loaded once and every element once.
+// Bound by latency for a step's few tokens (the token's row, its length and its page are one load behind the other, the
+// elements are asked for in front of them) and by HBM for prompts.
+__global__ __launch_bounds__(256) void kv_append_halves_kernel(KvView c, KvBatch b, KvTensor k, KvTensor v, KvTensor q, KvTensor qo,
+                                                               int q_heads, KvRope rope)
+{
+    const int t = blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
+    const int half = c.nb * 2;                                         // groups of eight in half a head; a multiple of four
+    const int head_all = (int)((unsigned)g / (unsigned)half), e = (g - head_all * half) * 8, e2 = e + half * 8;
+    const bool live = head_all < q_heads + 2 * c.heads;                // the same for a whole quad
+    const int what = head_all < q_heads ? 0 : head_all < q_heads + c.heads ? 1 : 2;
+    const int head = what == 0 ? head_all : what == 1 ? head_all - q_heads : head_all - q_heads - c.heads;
+    const KvTensor& in = what == 0 ? q : what == 1 ? k : v;
+    const uint16_t* row = in.p + (int64_t)t * in.token + (int64_t)head * in.head;
+    u32x4_t x = {0, 0, 0, 0}, y = {0, 0, 0, 0};
+    if (live) {
+        x = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + e));
+        y = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + e2));
+    }
+    const KvPlace at = kv_place(b, t);                                 // (with all lanes of the wave)
+    if (!live)
+        return;
+    if (what < 2 && rope.dim)
+        turn8<true, true>(&x, &y, rope, rope.positions ? rope.positions[t] : at.at, e);
+    if (what == 0) {
+        uint16_t* to = qo.p + (int64_t)t * qo.token + (int64_t)head * qo.head;
+        *reinterpret_cast<u32x4_t*>(to + e) = x;                       // (the attention behind this call reads them)
+        *reinterpret_cast<u32x4_t*>(to + e2) = y;
+        return;
+    }
+    const int page = kv_page(b.table, b.ldt, b.width, c.shift, c.pages, at.row, at.at);
+    const KvSlot to = kv_slot(c, what == 1, max(page, 0), head, at.at);
+    kv_put(x, to, page >= 0, e);
+    kv_put(y, to, page >= 0, e2);
+}
+
+// Any head and any rotary dim: 256 groups of eight elements of one token, the partner of a turned element by another load.
 __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvBatch b, KvTensor k, KvTensor v, KvTensor q, KvTensor qo,
                                                         int q_heads, KvRope rope)
 {
-    const int t = blockIdx.x;
+    const int t = blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
     const int per_head = c.nb * 4;
-    const int g = blockIdx.y * 256 + threadIdx.x;
     const int head_all = g / per_head, e = (g - head_all * per_head) * 8;
-    const int kv_heads = c.heads;
-    const bool live = head_all < q_heads + 2 * kv_heads;         // the same for a whole quad (per_head is a multiple of four)
-    const int what = head_all < q_heads ? 0 : head_all < q_heads + kv_heads ? 1 : 2;
-    const int head = what == 0 ? head_all : what == 1 ? head_all - q_heads : head_all - q_heads - kv_heads;
+    const bool live = head_all < q_heads + 2 * c.heads;                // the same for a whole quad (per_head is a multiple of four)
+    const int what = head_all < q_heads ? 0 : head_all < q_heads + c.heads ? 1 : 2;
+    const int head = what == 0 ? head_all : what == 1 ? head_all - q_heads : head_all - q_heads - c.heads;
     const KvTensor& in = what == 0 ? q : what == 1 ? k : v;
     const uint16_t* row = in.p + (int64_t)t * in.token + (int64_t)head * in.head;
     u32x4_t x = {0, 0, 0, 0};
     if (live)
         x = *reinterpret_cast<const u32x4_t*>(row + e);
-    const KvPlace at = kv_place(b, t);           // (with all lanes of the wave)
+    const KvPlace at = kv_place(b, t);                                 // (with all lanes of the wave)
     if (!live)
         return;
-    if (what < 2 && e < rope.dim)
-        x = turn8(x, row, e, rope, rope.positions ? rope.positions[t] : at.at);
+    if (what < 2 && e < rope.dim) {
+        const int half = rope.dim >> 1, pos = rope.positions ? rope.positions[t] : at.at;
+        u32x4_t other = *reinterpret_cast<const u32x4_t*>(row + (e < half ? e + half : e - half));
+        if (e < half)
+            turn8<true, false>(&x, &other, rope, pos, e);
+        else
+            turn8<false, true>(&other, &x, rope, pos, e - half);
+    }
     if (what == 0) {
         *reinterpret_cast<u32x4_t*>(qo.p + (int64_t)t * qo.token + (int64_t)head * qo.head + e) = x;
         return;
     }
     const int page = kv_page(b.table, b.ldt, b.width, c.shift, c.pages, at.row, at.at);
-    uint32_t packed;
-    int scale;
-    cast_group<true>(x, &packed, &scale);
-    if (page < 0)
-        return;
-    const int slot = (head << c.shift) + (at.at & ((1 << c.shift) - 1));
-    uint8_t* cq = (what == 1 ? c.kq : c.vq) + (int64_t)page * c.psq + (int64_t)slot * (c.nb * 16);
-    uint8_t* cs = (what == 1 ? c.ks : c.vs) + (int64_t)page * c.pss + (int64_t)slot * c.nb;
-    *reinterpret_cast<uint32_t*>(cq + (e >> 1)) = packed;
-    if ((e & 31) == 0)
-        cs[e >> 5] = (uint8_t)scale;
+    kv_put(x, kv_slot(c, what == 1, max(page, 0), head, at.at), page >= 0, e);
 }
 
-// Eight elements back to BF16 (exact: a code times a power of two), zeros where the token is nowhere.
+// Codes back to BF16 (exact: a code times a power of two), zeros where the token is nowhere.  Bound by the writes, four bytes
+// for one that is read; they are not read again soon and go past the L2's order of use.
 __global__ __launch_bounds__(256) void kv_read_kernel(KvView c, KvBatch b, KvTensor k, KvTensor v)
 {
-    const int t = blockIdx.x;
-    const int per_head = c.nb * 4;
-    const int g = blockIdx.y * 256 + threadIdx.x;
-    const int head_all = g / per_head, e = (g - head_all * per_head) * 8;
-    const KvPlace at = kv_place(b, t);
+    const int t = blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
+    const int per_head = c.nb * 4;                                     // groups of eight elements
+    const int head_all = (int)((unsigned)g / (unsigned)per_head), e = (g - head_all * per_head) * 8;
+    const KvPlace at = kv_place(b, t);                                 // (with all lanes of the wave)
     const int page = kv_page(b.table, b.ldt, b.width, c.shift, c.pages, at.row, at.at);
     if (head_all >= 2 * c.heads)
         return;
@@ -103,16 +154,15 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView c, KvBatch b, KvTen
         return;
     u32x4_t x = {0, 0, 0, 0};
     if (page >= 0) {
-        const int slot = (head << c.shift) + (at.at & ((1 << c.shift) - 1));
-        const uint32_t w = *reinterpret_cast<const uint32_t*>((keys ? c.kq : c.vq) + (int64_t)page * c.psq +
-                                                              (int64_t)slot * (c.nb * 16) + (e >> 1));
-        const float s = __uint_as_float((uint32_t)((keys ? c.ks : c.vs) + (int64_t)page * c.pss + (int64_t)slot * c.nb)[e >> 5] << 23);
+        const KvSlot from = kv_slot(c, keys, page, head, at.at);
+        const uint32_t w = *reinterpret_cast<const uint32_t*>(from.q + (e >> 1));
+        const float s = __uint_as_float((uint32_t)from.s[e >> 5] << 23);
         x[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
         x[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
         x[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
         x[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
     }
-    *reinterpret_cast<u32x4_t*>(out.p + (int64_t)t * out.token + (int64_t)head * out.head + e) = x;
+    __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t*>(out.p + (int64_t)t * out.token + (int64_t)head * out.head + e));
 }
 
 // Tokens of one sequence and one head move together, in place.  256 threads hold 256 / (2 nb) tokens at a time, one block (16
@@ -191,8 +241,9 @@ __global__ __launch_bounds__(256) void kv_copy_kernel(KvView c, const int32_t* s
 hipError_t launch_kv_append(const KvView& c, const KvBatch& b, const KvTensor& k, const KvTensor& v, const KvTensor& q,
                             const KvTensor& qo, int q_heads, const KvRope& rope, hipStream_t stream)
 {
-    const int64_t groups = (int64_t)(q_heads + 2 * c.heads) * c.nb * 4;
-    hipLaunchKernelGGL(kv_append_kernel, dim3((unsigned)b.tokens, (unsigned)((groups + 255) / 256)), dim3(256), 0, stream, c, b, k, v,
+    const bool halves = c.nb % 2 == 0 && (rope.dim == 0 || rope.dim == c.nb * 32);
+    const int64_t groups = (int64_t)(q_heads + 2 * c.heads) * c.nb * (halves ? 2 : 4);
+    hipLaunchKernelGGL(halves ? kv_append_halves_kernel : kv_append_kernel, dim3((unsigned)b.tokens, (unsigned)((groups + 255) / 256)), dim3(256), 0, stream, c, b, k, v,
                        q, qo, q_heads, rope);
     return hipGetLastError();
 }

@@ -81,36 +81,56 @@ __device__ __forceinline__ KvRow kv_row(const KvAttend& a, int b)
 // 2 target + (heads x tiles) workgroups.  Each finds its own share from the lengths, so that one launch fits any lengths, also those that
 // change between replays of a graph, and sequences of different lengths load the device evenly.  Only rows of two parts or more need
 // partial results: at most 4 target of them (U is summed in FP32, which all workgroups do alike; a few more for its rounding).
-// What the parts aim for (64 query heads on 8, dim 128, us):
-//   long parts   `target` of them, all at once (16 rows of 32000 tokens: 112; twice as many 119), but twice as many where the
-//                longest row is over the mean by a quarter, and parts of one length do not come out (64 rows of 500 to 16384 tokens: 81, not 86)
-//   short ones   (up to `brief` units: 16 with one query tile, 8 with two) half of `target`, because joining costs more than it
-//                saves (4 rows of 16000 tokens: 21.6, not 23.3)
-//   a row alone  no more than the kJoin parts that are joined at a time, unless that leaves a part over four units
+// What the parts aim for (dim 128, us):
+//   as they are  rows whose longest ends no later than parts would, the joining (`joint` units' time) with them
+//   one round    with few rows of one length, the shortest parts that `target` workgroups hold at once (16 rows of 32000 tokens, 64 query heads on 8:
+//                112; twice as many parts 119)
+//   several      with many rows of different lengths, parts of half a workgroup's share, since parts of one length do not come out
+//                (64 rows of 500 to 16384 tokens: 81, not 86)
+//   short parts  (up to `brief` units) half of `target`, because joining costs more than it saves (4 rows of 16000 tokens: 21.6,
+//                not 23.3)
+//   a row alone  no more than the kKvJoin parts that are joined at a time, unless that leaves a part over four units
 //                (one row of 2000 tokens: 9.1, and 10.7 with parts of one unit); whole up to six units (32 heads, 500 tokens: 7.8, not 10.1)
 constexpr int kKvJoin = 8;
 template <int kUnit>
-__device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_rows, KvItem* out)
+__device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_rows, int brief, int joint, KvItem* out)
 {
-    const int brief = tile_rows <= 16 ? 16 : 8;
     const int lane = threadIdx.x & 63;
     KvRow r0 = {0, 0, 0, 0};
-    float all = 0.f, longest = 0.f;
+    float all = 0.f, longest = 0.f, whole = 0.f;    // units, those of the longest row, rows of keys
     for (int base = 0; base < a.b.rows; base += 64) {
-        float u = 0.f;
+        float u = 0.f, t = 0.f;
         if (base + lane < a.b.rows) {
             const KvRow r = kv_row(a, base + lane);
-            u = (float)((r.n * a.group + tile_rows - 1) / tile_rows) * (float)max(1, (r.len - r.lo + kUnit - 1) / kUnit);
-            longest = fmaxf(longest, u);
+            const float tiles = (float)((r.n * a.group + tile_rows - 1) / tile_rows), units = (float)max(1, (r.len - r.lo + kUnit - 1) / kUnit);
+            u = tiles * units;
+            t = tiles;
+            longest = fmaxf(longest, tiles > 0.f ? units : 0.f);
             if (base == 0)
                 r0 = r;
         }
         all += wave_sum(u);
+        whole += wave_sum(t);
     }
     longest = max_of_wave(longest);
-    const float even = ceilf(all * (float)a.c.heads / (float)a.target);
-    const float full = longest * (float)a.b.rows > 1.25f * all && even > (float)brief ? ceilf(0.5f * even) : even;
-    const int each = (int)fminf(fmaxf(full, fminf(2.f * even, (float)brief)), 1e9f);
+    all *= (float)a.c.heads;
+    whole *= (float)a.c.heads;
+    const float target = (float)a.target, even = ceilf(all / target);
+    float aim = even;
+    if (fmaxf(longest, all / target + 0.5f * longest) <= 1.5f * all / target + (float)joint) {
+        aim = 1e9f;
+    } else if (2.f * whole <= target && longest * whole <= 1.05f * all && a.b.rows <= 64) {
+        const int tiles = (r0.n * a.group + tile_rows - 1) / tile_rows * a.c.heads, units = max(1, (r0.len - r0.lo + kUnit - 1) / kUnit);
+        for (int i = 0; i < 4; ++i) {
+            aim = ceilf(even * (1.f + 0.25f * (float)i));
+            const int parts = (units + (int)aim - 1) / (int)aim;
+            if (wave_sum(lane < a.b.rows ? (float)tiles * (float)parts : 0.f) <= target)
+                break;
+        }
+    } else if (even > (float)brief && longest * whole > 1.25f * all) {
+        aim = ceilf(0.5f * even);
+    }
+    const int each = (int)fminf(fmaxf(aim, fminf(2.f * even, (float)brief)), 1e9f);
     int before = 0, slots = 0;
     for (int base = 0; base < a.b.rows; base += 64) {
         KvRow r = r0;
@@ -135,7 +155,7 @@ __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_ro
             out->S = S;
             out->h = local % a.c.heads;                  // neighbouring workgroups: the heads, so that a head's tiles meet in one L2
             const int rest = local / a.c.heads;
-            out->tile = rest % T;
+            out->tile = T - 1 - rest % T;                // causal: the tiles with the most keys first
             out->s = rest / T;
             out->slots = T * a.c.heads;
             out->slot0 = __builtin_amdgcn_readlane(slots_upto - (parts > 1 ? mine : 0), at) + out->tile * a.c.heads + out->h;
@@ -222,26 +242,27 @@ __device__ __forceinline__ void load_tile(KvTile<NB, kPad>& t, const KvView& c, 
                 for (int i = 0; i < 4; ++i)
                     t.k[a][4 * b + i] = 0;
                 if (has)
-                    load_words<4>(&t.k[a][4 * b], kq + (r * nb + block) * 16);
+                    load_words<4>(&t.k[a][4 * b], kq + (uint32_t)((r * nb + block) * 16));
             } else {
-                load_words<NB>(t.k[a], kq + (r * 16 + 4 * g) * NB);
+                load_words<NB>(t.k[a], kq + (uint32_t)((r * 16 + 4 * g) * NB));
             }
             if (has)
-                t.ks[a][b] = ks[r * nb + (NB >= 4 ? block : (NB * g) >> 2)];
+                t.ks[a][b] = ks[(uint32_t)(r * nb + (NB >= 4 ? block : (NB * g) >> 2))];
         }
         if constexpr (!kPad)
-            load_words<NB>(t.vs[a], vs + 4 * g * NB);
+            load_words<NB>(t.vs[a], vs + (uint32_t)(4 * g * NB));
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int ch = 0; ch < T::kChunks; ++ch) {
-                const uint8_t* p = vq + ((4 * g + i) * 16 * nb + ch * (T::kChunk / 2) + r * (T::kEl / 2));
+                // (32-bit offsets without a sign: the base stays in scalar registers)
+                const uint8_t* p = vq + (uint32_t)((4 * g + i) * 16 * nb + ch * (T::kChunk / 2) + r * (T::kEl / 2));
                 if constexpr (kPad) {
                     const int block = ch * T::kBlocks + ((r * T::kEl) >> 5);
                     t.v[a][i][ch] = t.vs[a][i * T::kChunks + ch] = 0;
                     if (block < nb) {
                         t.v[a][i][ch] = *reinterpret_cast<const uint32_t*>(p);
-                        t.vs[a][i * T::kChunks + ch] = vs[(4 * g + i) * nb + block];
+                        t.vs[a][i * T::kChunks + ch] = vs[(uint32_t)((4 * g + i) * nb + block)];
                     }
                 } else {
                     t.v[a][i][ch] = T::kEl == 8 ? *reinterpret_cast<const uint32_t*>(p)
@@ -327,5 +348,77 @@ __device__ __forceinline__ void value_operands(const KvTile<NB, kPad>& t, int ch
     for (int e = 0; e < T::kEl; ++e)
         x[e] = __builtin_bit_cast(bf16x8_t, y[e]);
 }
+
+// What the queries of a stretch see: query at position p (kNobody: no query) sees position j.
+constexpr int kNobody = -0x40000000;
+struct KvSight {
+    int base, window;                // position of the sequence's first new token; 0: all before
+    bool causal, tree;
+    __device__ __forceinline__ bool sees(int p, uint64_t word, int j) const
+    {
+        bool ok = p != kNobody && (!causal || j <= p) && (window == 0 || j > p - window);
+        if (tree && j >= base)
+            ok = ok && j - base < 64 && ((word >> (j - base)) & 1);
+        return ok;
+    }
+    __device__ __forceinline__ uint64_t word(const KvAttend& a, const KvItem& it, int p) const
+    {
+        return tree && p != kNobody ? a.tree[it.first + p - base] : 0;
+    }
+};
+
+// Where part s of S begins among n.
+__device__ __forceinline__ int part_begin(int n, int s, int S)
+{
+    const int each = n / S;
+    return s * each + min(s, n - each * S);
+}
+
+// One query tile's scores of 32 tokens (lane (query, g): tokens 4 g + i of either half) become weights: the running maximum m,
+// the lane's share l of the sum, the sums o, and the weights as the right operand of the values' product.
+template <int kSums>
+__device__ __forceinline__ bf16x8_t softmax_step(const f32x4_t* s, float scale, float* m, float* l, f32x4_t* o)
+{
+    float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
+    top = max_of_rows(top);
+    // The sums move to a new maximum only when it is 2^8 above the old one: the weights then stay below 2^8, which FP32 sums and
+    // BF16 weights hold as well as weights up to 1.
+    if (__ballot((top - *m) * scale > 8.f || (*m == -INFINITY && top > -INFINITY))) {
+        const float now = fmaxf(*m, top);
+        const float f = now == -INFINITY ? 1.f : exp2f((*m - now) * scale);
+        *m = now;
+        *l *= f;
+#pragma unroll
+        for (int e = 0; e < kSums; ++e)
+            o[e] *= f;
+    }
+    const float off = *m == -INFINITY ? 0.f : -*m * scale;
+    float w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale, off));
+        *l += w[i];
+    }
+    // rounded to BF16 (the type of the values' product; half a step, 2^-8 of a weight at most, and the weights' errors average out)
+    return __builtin_bit_cast(bf16x8_t, (u32x4_t{f32_to_bf16_rne2(w[0], w[1]), f32_to_bf16_rne2(w[2], w[3]),
+                                                 f32_to_bf16_rne2(w[4], w[5]), f32_to_bf16_rne2(w[6], w[7])}));
+}
+
+// NaN blocks among values that not every query sees: counted for each query that sees one, by the values' product with ones in
+// the places of the blocks (x) and of what is seen (y); the sums of the lane's elements that it hits become NaN.
+template <int kSums>
+__device__ __forceinline__ void mark_nan(bf16x8_t x, bf16x8_t y, f32x4_t* o)
+{
+    const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < kSums; ++e)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            o[e][i] = hit[i] > 0.f ? __uint_as_float(0x7FC00000u) : o[e][i];
+}
+
+// Stores and loads that all dies of the device see alike.
+__device__ __forceinline__ void put_through(float* p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get_through(const float* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 }  // namespace mxfp4

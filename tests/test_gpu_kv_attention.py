@@ -281,3 +281,69 @@ def test_starts_that_make_no_sense_stay_in_bounds():
         binding.mxfp4_kv_attention(q, p.cache(DEV), table, lens, starts=torch.tensor(starts, dtype=torch.int32, device=DEV))
     binding.mxfp4_kv_attention(q, p.cache(DEV), table, torch.tensor([-4, 1 << 30, 60], dtype=torch.int32, device=DEV))
     torch.cuda.synchronize()
+
+
+# Many queries for a key/value head: several tiles of them.
+
+@pytest.mark.parametrize("window", [0, 1, 33, 64, 200])
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+def test_many_queries(dim, window):
+    p = Paged([400, 33, 64, 1, 129, 0], 2, 32, dim, seed=window + dim)
+    check(p, [9, 33, 1, 1, 70, 0], 32, window=window, what="dim %d window %d" % (dim, window))
+    check(p, [30, 2, 64, 0, 128, 0], 32, window=window, causal=False, what="dim %d window %d, not causal" % (dim, window))
+
+
+@pytest.mark.parametrize("page", [16, 64, 1024])
+def test_many_queries_over_long_rows_are_joined(page):
+    p = Paged([9000, 700, 5000], 1, page, 128, seed=page)
+    check(p, [20, 3, 65], 8)
+    first = run(p, [20, 3, 65], 8)[0]
+    for _ in range(5):
+        assert torch.equal(run(p, [20, 3, 65], 8)[0].view(torch.int16), first.view(torch.int16))
+
+
+def test_many_queries_in_trees():
+    rng = np.random.RandomState(0)
+    lens, nodes = [64, 65, 700, 159], 64
+    trees = []
+    for b in range(4):
+        words = []
+        for i in range(nodes):
+            words.append((words[rng.randint(i)] if i else 0) | 1 << i)
+        trees.append(words)
+    trees[0][5] = 0
+    p = Paged(lens, 1, 16, 128, seed=2)
+    check(p, [nodes] * 4, 4, trees=trees)
+
+
+def test_many_queries_more_than_tokens_and_missing_pages():
+    p = Paged([3, 0, 40, 100], 1, 16, 64, seed=2)
+    check(p, [5, 2, 41, 30], 16)
+    p.table[3, 2] = -1
+    keep = np.ones(100, bool)
+    keep[32:48] = False
+    out, lse, q = run(p, [0, 0, 0, 30], 16)
+    sees = p.sees(3, 30)[:, keep]
+    ref, ref_lse, room, off = attention(q.double().numpy(), p.k[3][keep], p.v[3][keep], sees, 64 ** -0.5)
+    assert (np.abs(out.double().cpu().numpy() - ref) <= tolerance(ref, room, off, 100)).all()
+    assert np.allclose(lse.double().cpu().numpy(), ref_lse, atol=1e-4)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_many_queries_and_nan_blocks(dim):
+    p = Paged([200, 90], 1, 16, dim, seed=4)
+    blocks = dim // 32
+    p.vs[p.table[0, 195 // 16], 0, 195 % 16, blocks - 1] = 255
+    p.vs[p.table[0, 20 // 16], 0, 20 % 16, 0] = 255
+    p.ks[p.table[1, 80 // 16], 0, 80 % 16, blocks - 1] = 255
+    for causal, window in ((True, 0), (True, 100), (False, 0)):
+        out = run(p, [30, 30], 8, causal=causal, window=window)[0].float().cpu().numpy()
+        new = np.arange(30)
+        last = np.broadcast_to((not causal) | (170 + new >= 195), 30)
+        first = np.broadcast_to(170 + new - window < 20 if window else True, 30)
+        nan = np.isnan(out)
+        want = np.zeros(nan.shape, bool)
+        want[:30, :, dim - 32:] |= last[:, None, None]
+        want[:30, :, :32] |= first[:, None, None]
+        want[30:] |= np.broadcast_to((not causal) | (60 + new >= 80), 30)[:, None, None]
+        assert np.array_equal(nan, want), (causal, window)
