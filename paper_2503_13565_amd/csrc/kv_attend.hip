@@ -19,10 +19,10 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     typedef KvTile<NB, kPad> T;
     constexpr int NW = 4, kRows = 16 * QT, kEl = T::kEl, kChunks = T::kChunks;
     constexpr int kDepth = QT == 1 ? 3 : 2;
-    constexpr int kSlot = QT * NB * 512 + 32 * QT;                     // floats of a partial result
+    constexpr int kSlot = QT * NB * 512 + 48 * QT;                     // floats of a partial result
     constexpr int kJoin = kKvJoin, kFinal = 8192;                         // parts added at a time; where the counters of the last sums begin
     __shared__ __align__(16) float comb[NW][kEl][4][64];
-    __shared__ float ml[NW][QT][16][2];
+    __shared__ float ml[NW][QT][16][3];                                // maximum, sum, exact sum
     __shared__ int last;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
@@ -43,14 +43,12 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     bf16x8_t q[QT][NB];
     const KvSight sight = {it.len - it.n, a.window, causal, tree};
     int at_q[QT];                                                      // the positions of the lane's queries
-    int64_t out_at[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         const int row = row0 + qt * 16 + c;
         const int i = row / a.group, head = it.h * a.group + row - i * a.group;
         const bool live = row < rows;
         at_q[qt] = live ? it.len - it.n + i : kNobody;
-        out_at[qt] = live ? (int64_t)(it.first + i) * a.out.token + (int64_t)head * a.out.head : -1;
         const uint16_t* from = a.q.p + (int64_t)(it.first + (live ? i : 0)) * a.q.token + (int64_t)(live ? head : it.h * a.group) * a.q.head;
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
@@ -62,17 +60,20 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     }
 
     f32x4_t o[QT][2 * NB];
-    float m[QT], l[QT];
+    float m[QT], exact[QT];
+    f32x4_t l[QT];
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
         m[qt] = -INFINITY;
-        l[qt] = 0.f;
+        l[qt] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        exact[qt] = 0.f;
 #pragma unroll
         for (int e = 0; e < 2 * NB; ++e)
             o[qt][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
 
     const float scale = a.scale;
+    const bool wanted = a.lse != nullptr;                              // the logarithm of the sums
     auto compute = [&](T& t, int tile) {
         const int j0 = tile * 32;
         const bool whole = t.page[0] >= 0 && t.page[1] >= 0 && j0 + 32 <= it.len;
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
         bf16x8_t p[QT];
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
-            p[qt] = softmax_step<2 * NB>(s[qt], scale, &m[qt], &l[qt], o[qt]);
+            p[qt] = softmax_step<2 * NB>(s[qt], scale, wanted, &m[qt], &l[qt], &exact[qt], o[qt]);
         }
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
@@ -183,19 +184,26 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
         }
     }
 
+    int64_t out_at[QT];                                                // where the lane's queries' results go, -1: no query
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+        const int row = row0 + qt * 16 + c, i = row / a.group;
+        out_at[qt] = row < rows ? (int64_t)(it.first + i) * a.out.token + (int64_t)(it.h * a.group + row - i * a.group) * a.out.head : -1;
+    }
     // The four waves' sums meet in the LDS, one chunk of elements at a time; wave i takes row i of the accumulators.
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        l[qt] = sum_of_rows(l[qt]);
+        const float sum = wanted ? sum_of_rows(exact[qt]) : 0.f;
         if (g == 0) {
             ml[wave][qt][c][0] = m[qt];
-            ml[wave][qt][c][1] = l[qt];
+            ml[wave][qt][c][1] = l[qt][0];
+            ml[wave][qt][c][2] = sum;
         }
     }
     float* part = a.part + (int64_t)(it.slot0 + it.s * it.slots) * kSlot;
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
-        float f[NW], top = -INFINITY, total = 0.f;
+        float f[NW], top = -INFINITY, total = 0.f, precise = 0.f;
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
             __syncthreads();
@@ -215,6 +223,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                     // (a wave that has met only NaN scores has no maximum, but its sum says so)
                     f[w] = ml[w][qt][c][1] != ml[w][qt][c][1] ? __uint_as_float(0x7FC00000u) : f[w];
                     total += f[w] * ml[w][qt][c][1];
+                    precise += f[w] * ml[w][qt][c][2];
                 }
             }
             float r[kEl];
@@ -243,12 +252,13 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
         }
         if (wave == 0 && g == 0) {
             if (it.S > 1) {
-                put_through(&part[QT * NB * 512 + qt * 32 + c], top);
-                put_through(&part[QT * NB * 512 + qt * 32 + 16 + c], total);
+                put_through(&part[QT * NB * 512 + qt * 48 + c], top);
+                put_through(&part[QT * NB * 512 + qt * 48 + 16 + c], total);
+                put_through(&part[QT * NB * 512 + qt * 48 + 32 + c], precise);
             } else if (a.lse && out_at[qt] >= 0) {
                 const int row = row0 + qt * 16 + c, i = row / a.group;
                 a.lse[(int64_t)(it.first + i) * (a.group * a.c.heads) + it.h * a.group + row - i * a.group] =
-                    total == 0.f ? -INFINITY : (top * scale + log2f(total)) * kLn2;
+                    precise == 0.f ? -INFINITY : (top * scale + log2f(precise)) * kLn2;
             }
         }
     }
@@ -278,19 +288,20 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
 #pragma unroll
         for (int qt = 0; qt < QT; ++qt) {
             const bool live = out_at[qt] >= 0;
-            float top = -INFINITY, total = 0.f;
+            float top = -INFINITY, total = 0.f, precise = 0.f;
             float r[2 * NB];
 #pragma unroll
             for (int e = 0; e < 2 * NB; ++e)
                 r[e] = 0.f;
             if (live) {
                 for (int s = 0; s < count; s += kJoin) {               // (more than kJoin only for the last sum of very many parts)
-                    float ms[kJoin], ls[kJoin], x[kJoin][2 * NB];
+                    float ms[kJoin], ls[kJoin], es[kJoin], x[kJoin][2 * NB];
 #pragma unroll
                     for (int k = 0; k < kJoin; ++k) {
                         const float* p = from + min(s + k, count - 1) * pitch;
-                        ms[k] = get_through(&p[QT * NB * 512 + qt * 32 + c]);
-                        ls[k] = get_through(&p[QT * NB * 512 + qt * 32 + 16 + c]);
+                        ms[k] = get_through(&p[QT * NB * 512 + qt * 48 + c]);
+                        ls[k] = get_through(&p[QT * NB * 512 + qt * 48 + 16 + c]);
+                        es[k] = get_through(&p[QT * NB * 512 + qt * 48 + 32 + c]);
 #pragma unroll
                         for (int e = 0; e < 2 * NB; ++e)
                             x[k][e] = get_through(&p[((qt * 2 * NB + e) * 4 + wave) * 64 + lane]);
@@ -301,6 +312,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                         now = fmaxf(now, ms[k]);
                     const float old = top == -INFINITY ? 0.f : exp2f((top - now) * scale);
                     total *= old;
+                    precise *= old;
 #pragma unroll
                     for (int e = 0; e < 2 * NB; ++e)
                         r[e] *= old;
@@ -311,6 +323,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                         f = ls[k] != ls[k] ? __uint_as_float(0x7FC00000u) : f;
                         f = s + k < count ? f : 0.f;
                         total += f * (s + k < count ? ls[k] : 0.f);
+                        precise += f * (s + k < count ? es[k] : 0.f);
 #pragma unroll
                         for (int e = 0; e < 2 * NB; ++e)
                             r[e] += s + k < count ? f * x[k][e] : 0.f;
@@ -325,8 +338,9 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                         put_through(&to[((qt * 2 * NB + e) * 4 + wave) * 64 + lane], r[e]);
                 }
                 if (wave == 0 && g == 0) {
-                    put_through(&to[QT * NB * 512 + qt * 32 + c], top);
-                    put_through(&to[QT * NB * 512 + qt * 32 + 16 + c], total);
+                    put_through(&to[QT * NB * 512 + qt * 48 + c], top);
+                    put_through(&to[QT * NB * 512 + qt * 48 + 16 + c], total);
+                    put_through(&to[QT * NB * 512 + qt * 48 + 32 + c], precise);
                 }
                 continue;
             }
@@ -347,7 +361,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
             if (a.lse && wave == 0 && g == 0) {
                 const int row = row0 + qt * 16 + c, i = row / a.group;
                 a.lse[(int64_t)(it.first + i) * (a.group * a.c.heads) + it.h * a.group + row - i * a.group] =
-                    total == 0.f ? -INFINITY : (top * scale + log2f(total)) * kLn2;
+                    precise == 0.f ? -INFINITY : (top * scale + log2f(precise)) * kLn2;
             }
         }
         if (done)
@@ -372,7 +386,7 @@ static int attend_target(int nb, const DeviceInfo& dev) { return dev.cus * (nb <
 size_t kv_attend_part_bytes(int nb, int group, int64_t tokens, int64_t rows, const DeviceInfo& dev)
 {
     const int qt = query_tiles(nb, rows ? (tokens * group + rows - 1) / rows : 0);
-    return ((size_t)4 * attend_target(nb, dev) + 8) * (qt * padded(nb) * 512 + 32 * qt) * sizeof(float);
+    return ((size_t)4 * attend_target(nb, dev) + 8) * (qt * padded(nb) * 512 + 48 * qt) * sizeof(float);
 }
 
 template <int NB, bool kPad>

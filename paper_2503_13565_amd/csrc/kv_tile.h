@@ -11,12 +11,16 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // Maximum over the four lanes that hold one query's scores (l, l + 16, l + 32, l + 48), in all of them.
+__device__ __forceinline__ float max_of_three(float a, float b, float c)
+{
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);      // (one instruction; a NaN is the maximum)
+}
 __device__ __forceinline__ float max_of_rows(float v)
 {
     auto p = __builtin_amdgcn_permlane16_swap(__float_as_int(v), __float_as_int(v), false, false);
-    v = fmaxf(__int_as_float(p[0]), __int_as_float(p[1]));
+    v = __builtin_elementwise_maximum(__int_as_float(p[0]), __int_as_float(p[1]));
     p = __builtin_amdgcn_permlane32_swap(__float_as_int(v), __float_as_int(v), false, false);
-    return fmaxf(__int_as_float(p[0]), __int_as_float(p[1]));
+    return __builtin_elementwise_maximum(__int_as_float(p[0]), __int_as_float(p[1]));
 }
 __device__ __forceinline__ float max_of_wave(float v)
 {
@@ -305,7 +309,7 @@ __device__ __forceinline__ uint32_t value_scale(const KvTile<NB, kPad>& t, int a
     if constexpr (kPad)
         return t.vs[a][i * T::kChunks + ch];
     else
-        return (t.vs[a][(i * NB + ch * T::kBlocks) >> 2] >> value_scale_shift<NB, kPad>(i, ch)) & 0xFFu;
+        return __builtin_amdgcn_ubfe(t.vs[a][(i * NB + ch * T::kBlocks) >> 2], value_scale_shift<NB, kPad>(i, ch), 8);
 }
 template <int NB, bool kPad>
 __device__ __forceinline__ void clear_value(KvTile<NB, kPad>& t, int a, int i, int ch)
@@ -374,20 +378,24 @@ __device__ __forceinline__ int part_begin(int n, int s, int S)
     return s * each + min(s, n - each * S);
 }
 
-// One query tile's scores of 32 tokens (lane (query, g): tokens 4 g + i of either half) become weights: the running maximum m,
-// the lane's share l of the sum, the sums o, and the weights as the right operand of the values' product.
+// One query tile's scores of 32 tokens (lane (query, g): tokens 4 g + i of either half) become weights, the right operand of the
+// values' product.  The running maximum m and the sums move with it: o of the values, l of the weights as the values' product has
+// them, rounded (in all four registers, as the matrix instruction leaves it), and, if it is wanted, `exact` of the lane's weights
+// as they are, for the logarithm, in which a single weight's rounding would show.  A NaN score makes `top` NaN (the maximum here is
+// the one that carries it on), which moves nothing, and a NaN weight, which makes the query's sums NaN.
 template <int kSums>
-__device__ __forceinline__ bf16x8_t softmax_step(const f32x4_t* s, float scale, float* m, float* l, f32x4_t* o)
+__device__ __forceinline__ bf16x8_t softmax_step(const f32x4_t* s, float scale, bool wanted, float* m, f32x4_t* l, float* exact, f32x4_t* o)
 {
-    float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-    top = max_of_rows(top);
+    float top = max_of_three(max_of_three(max_of_three(s[0][0], s[0][1], s[0][2]), s[0][3], s[1][0]), s[1][1], s[1][2]);
+    top = max_of_rows(max_of_three(top, s[1][3], s[1][3]));
     // The sums move to a new maximum only when it is 2^8 above the old one: the weights then stay below 2^8, which FP32 sums and
     // BF16 weights hold as well as weights up to 1.
     if (__ballot((top - *m) * scale > 8.f || (*m == -INFINITY && top > -INFINITY))) {
-        const float now = fmaxf(*m, top);
+        const float now = top > *m ? top : *m;
         const float f = now == -INFINITY ? 1.f : exp2f((*m - now) * scale);
         *m = now;
         *l *= f;
+        *exact *= f;
 #pragma unroll
         for (int e = 0; e < kSums; ++e)
             o[e] *= f;
@@ -395,13 +403,17 @@ __device__ __forceinline__ bf16x8_t softmax_step(const f32x4_t* s, float scale, 
     const float off = *m == -INFINITY ? 0.f : -*m * scale;
     float w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 8; ++i)
         w[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale, off));
-        *l += w[i];
-    }
     // rounded to BF16 (the type of the values' product; half a step, 2^-8 of a weight at most, and the weights' errors average out)
-    return __builtin_bit_cast(bf16x8_t, (u32x4_t{f32_to_bf16_rne2(w[0], w[1]), f32_to_bf16_rne2(w[2], w[3]),
-                                                 f32_to_bf16_rne2(w[4], w[5]), f32_to_bf16_rne2(w[6], w[7])}));
+    const bf16x8_t p = __builtin_bit_cast(bf16x8_t, (u32x4_t{f32_to_bf16_rne2(w[0], w[1]), f32_to_bf16_rne2(w[2], w[3]),
+                                                             f32_to_bf16_rne2(w[4], w[5]), f32_to_bf16_rne2(w[6], w[7])}));
+    if (wanted)
+        *exact += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    // Their sum by one product with ones: the matrix pipe has room, the vector unit has not.
+    const bf16x8_t ones = __builtin_bit_cast(bf16x8_t, (u32x4_t{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}));
+    *l = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p, *l, 0, 0, 0);
+    return p;
 }
 
 // NaN blocks among values that not every query sees: counted for each query that sees one, by the values' product with ones in
