@@ -243,7 +243,7 @@ int mxfp4_woq_gemm_t(const void* x_bf16, int64_t M, int64_t ldx,
  * Position p of sequence b is slot p % page of page table[b * ldt + p / page].  A page number outside
  * [0, pages) and a position outside [0, width * page) name no token: nothing is stored or moved
  * there, nothing is read, and attention leaves it out.  No call reads or writes out of bounds for any contents of
- * table, lens, starts, keep, counts, src or dst.
+ * table, lens, starts, keep, counts, src, dst, refs or free_bits.
  */
 typedef struct mxfp4_kv_cache {
     void* kq;
@@ -348,7 +348,7 @@ int mxfp4_kv_attention(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, 
 
 /*
  * Who holds which page.  refs int32 [pages]: how many table entries name the page; free_bits uint32
- * [(pages + 31) / 32]: bit p % 32 of word p / 32 is set where refs[p] is 0 (bits past the last page are clear).  Both are device arrays that
+ * [(pages + 31) / 32]: bit p % 32 of word p / 32 is set where refs[p] is 0 (bits past the last page do not count).  Both are device arrays that
  * the calls below keep; an empty cache has all refs 0.  `table` [any rows][ldt] and `lens` cover every sequence,
  * `rows_list` (device, `count` distinct numbers in [0, rows)) names those that a call is about; entries outside
  * are left out.  A row's first ceil(lens / page) entries are its pages, the others are -1.

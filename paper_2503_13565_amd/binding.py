@@ -1169,19 +1169,21 @@ def mxfp4_kv_read(cache: KvCache, table: torch.Tensor, lens: torch.Tensor, token
     return k, v
 
 
-# One workspace for each stream that attention has run on, as a program would keep it: zeroed when it is made, left with its
-# counters at zero by every call, and used by calls that the stream runs one after the other.  Under graph capture a call gets one of
+# One workspace for each stream that attention has run on, as a program would keep it: its counters zeroed when it is made, left at
+# zero by every call, and used by calls that the stream runs one after the other.  Under graph capture a call gets one of
 # its own, which belongs to the graph.
 _kv_workspaces = {}
 
 
 def _kv_workspace(device: torch.device, stream: int, need: int) -> torch.Tensor:
-    if torch.cuda.is_current_stream_capturing():
-        return torch.zeros((need,), dtype=torch.uint8, device=device)
     key = stream * 64 + device.index
-    ws = _kv_workspaces.get(key)
+    capturing = torch.cuda.is_current_stream_capturing()
+    ws = None if capturing else _kv_workspaces.get(key)
     if ws is None or ws.numel() < need:
-        ws = _kv_workspaces[key] = torch.zeros((need,), dtype=torch.uint8, device=device)
+        ws = torch.empty((need,), dtype=torch.uint8, device=device)
+        ws[:4 * KV_COUNTERS].zero_()
+        if not capturing:
+            _kv_workspaces[key] = ws
     return ws
 
 

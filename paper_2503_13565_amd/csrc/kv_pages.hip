@@ -80,6 +80,15 @@ __device__ __forceinline__ int block_scan(int v, int* sums, int* all)
     return v + (wave ? before : 0);
 }
 
+// A word of the free bits; bits past the last page name no page, whatever they hold.
+__device__ __forceinline__ uint32_t free_word(const KvPool& p, int words, int w)
+{
+    if (w >= words)
+        return 0u;
+    const int last = p.pages & 31;
+    return p.bits[w] & (w == words - 1 && last ? (1u << last) - 1 : 0xFFFFFFFFu);
+}
+
 // One workgroup of 1024 threads: the rows are scanned for what each needs, the free bits for the pages of the lowest numbers.
 // Free pages are dealt out 1024 words (32768 pages) at a time: their numbers go to a list in the LDS in order, then every
 // page finds its row by bisection among the rows' sums.  Latency-bound: a chain of some twelve loads, scans and barriers.
@@ -99,7 +108,7 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
     if (tid == 0)
         bad = 0;
     const int words = (p.pages + 31) >> 5;
-    const uint32_t word0 = tid < words ? p.bits[tid] : 0u;             // (asked for before the rows' chain of loads)
+    const uint32_t word0 = free_word(p, words, tid);                   // (asked for before the rows' chain of loads)
     int n[kEach], a[kEach], row[kEach];
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
@@ -113,7 +122,7 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
     }
     int have = __popc(word0);
     for (int w = 1024 + tid; w < words; w += 1024)
-        have += __popc(p.bits[w]);
+        have += __popc(free_word(p, words, w));
     __syncthreads();
     int refs[kEach];
 #pragma unroll
@@ -185,7 +194,7 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
     }
     int done = 0;
     for (int w0 = 0; done < total; w0 += 1024) {
-        const uint32_t word = w0 == 0 ? word0 : w0 + tid < words ? p.bits[w0 + tid] : 0u;
+        const uint32_t word = w0 == 0 ? word0 : free_word(p, words, w0 + tid);
         const int c = __popc(word);
         int found;
         const int upto = block_scan(c, sums, &found);

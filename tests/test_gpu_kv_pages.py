@@ -253,6 +253,20 @@ def test_rows_outside_and_full_pools_change_nothing():
     binding.mxfp4_kv_fork(pool, cache, table, lens, ints([])[:0], ints([])[:0])
 
 
+@pytest.mark.parametrize("pages", [1, 31, 33, 40, 1055])
+def test_free_bits_past_the_last_page_name_no_page(pages):
+    cache = binding.mxfp4_kv_cache(pages, 1, 16, 32, device=DEV)
+    pool = binding.mxfp4_kv_pool(pages, device=DEV)
+    pool.free.fill_(-1)
+    table, lens = torch.full((2, 2048), -1, dtype=torch.int32, device=DEV), ints([0, 0])
+    more = binding.mxfp4_kv_extend(pool, cache, table, lens, ints([0]), ints([16 * pages + 1]))
+    assert int(more) == 1 and lens.tolist() == [0, 0] and not pool.refs.any()
+    assert int(binding.mxfp4_kv_extend(pool, cache, table, lens, ints([0]), ints([16 * pages]))) == 0
+    assert table[0, :pages].tolist() == list(range(pages)) and (table[0, pages:] == -1).all() and (pool.refs == 1).all()
+    assert int(binding.mxfp4_kv_extend(pool, cache, table, lens, ints([1]), ints([1]))) == 1
+    assert not pool.free.any()
+
+
 @pytest.mark.parametrize("dim,heads,page", [(128, 4, 16), (64, 3, 32), (96, 2, 16), (256, 1, 64), (32, 5, 16), (192, 2, 128)])
 def test_compact(dim, heads, page):
     rng = np.random.RandomState(dim)
