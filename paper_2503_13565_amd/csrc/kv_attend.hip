@@ -88,6 +88,14 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                 for (int qt = 0; qt < QT; ++qt)
                     s[qt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[qt][j], j ? s[qt][h] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
             }
+        // Converts between the products, four for each operand: the matrix pipe works beside them in one wave's stream better than blocks of
+        // either do in two waves' (5001 tokens of a prompt: 311 us, 316 in the compiler's order).
+        __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * NB * QT; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x2, 4 / QT, 0);
+        }
         uint32_t nan_at = 0;                                           // bit (chunk, half, token): a NaN block, taken out of the values
         if (masked) {
             uint64_t word[QT];
@@ -244,7 +252,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                         y[e / 2] = f32_to_bf16_rne2(r[e] * inv, r[e + 1] * inv);
                     __builtin_memcpy(__builtin_assume_aligned(to, kEl * 2), y, kEl * 2);
                 }
-            } else if (out_at[qt] >= 0) {
+            } else {
 #pragma unroll
                 for (int e = 0; e < kEl; ++e)
                     put_through(&part[((qt * 2 * NB + ch * kEl + e) * 4 + wave) * 64 + lane], r[e]);
@@ -269,6 +277,8 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     // again, in the order of the parts whoever it is.  Nobody waits.  The parts go past the L2 (each die has its own) with coherent stores,
     // which have arrived when the wave's counter of stores is at zero, so that the count needs no write-back of a whole L2 in front of
     // it: with __threadfence() in that place 1024 workgroups took 245 us over 131071 tokens instead of 123.
+    // Lanes without a query store and load as well, so that lines are whole and nothing branches (one token, 32 heads of their own, 2000
+    // tokens: 10.4 us, 12.4 with those lanes left out).
     const float* parts = a.part + (int64_t)it.slot0 * kSlot;
     int first = it.s - it.s % kJoin, count = min(kJoin, it.S - first), step = 1;
     bool done = it.S <= kJoin;
@@ -293,50 +303,46 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
 #pragma unroll
             for (int e = 0; e < 2 * NB; ++e)
                 r[e] = 0.f;
-            if (live) {
-                for (int s = 0; s < count; s += kJoin) {               // (more than kJoin only for the last sum of very many parts)
-                    float ms[kJoin], ls[kJoin], es[kJoin], x[kJoin][2 * NB];
+            for (int s = 0; s < count; s += kJoin) {                   // (more than kJoin only for the last sum of very many parts)
+                float ms[kJoin], ls[kJoin], es[kJoin], x[kJoin][2 * NB];
 #pragma unroll
-                    for (int k = 0; k < kJoin; ++k) {
-                        const float* p = from + min(s + k, count - 1) * pitch;
-                        ms[k] = get_through(&p[QT * NB * 512 + qt * 48 + c]);
-                        ls[k] = get_through(&p[QT * NB * 512 + qt * 48 + 16 + c]);
-                        es[k] = get_through(&p[QT * NB * 512 + qt * 48 + 32 + c]);
-#pragma unroll
-                        for (int e = 0; e < 2 * NB; ++e)
-                            x[k][e] = get_through(&p[((qt * 2 * NB + e) * 4 + wave) * 64 + lane]);
-                    }
-                    float now = top;
-#pragma unroll
-                    for (int k = 0; k < kJoin; ++k)
-                        now = fmaxf(now, ms[k]);
-                    const float old = top == -INFINITY ? 0.f : exp2f((top - now) * scale);
-                    total *= old;
-                    precise *= old;
+                for (int k = 0; k < kJoin; ++k) {
+                    const float* p = from + min(s + k, count - 1) * pitch;
+                    ms[k] = get_through(&p[QT * NB * 512 + qt * 48 + c]);
+                    ls[k] = get_through(&p[QT * NB * 512 + qt * 48 + 16 + c]);
+                    es[k] = get_through(&p[QT * NB * 512 + qt * 48 + 32 + c]);
 #pragma unroll
                     for (int e = 0; e < 2 * NB; ++e)
-                        r[e] *= old;
-                    top = now;
+                        x[k][e] = get_through(&p[((qt * 2 * NB + e) * 4 + wave) * 64 + lane]);
+                }
+                float now = top;
 #pragma unroll
-                    for (int k = 0; k < kJoin; ++k) {
-                        float f = ms[k] == -INFINITY ? 0.f : exp2f((ms[k] - now) * scale);
-                        f = ls[k] != ls[k] ? __uint_as_float(0x7FC00000u) : f;
-                        f = s + k < count ? f : 0.f;
-                        total += f * (s + k < count ? ls[k] : 0.f);
-                        precise += f * (s + k < count ? es[k] : 0.f);
+                for (int k = 0; k < kJoin; ++k)
+                    now = fmaxf(now, ms[k]);
+                const float old = top == -INFINITY ? 0.f : exp2f((top - now) * scale);
+                total *= old;
+                precise *= old;
 #pragma unroll
-                        for (int e = 0; e < 2 * NB; ++e)
-                            r[e] += s + k < count ? f * x[k][e] : 0.f;
-                    }
+                for (int e = 0; e < 2 * NB; ++e)
+                    r[e] *= old;
+                top = now;
+#pragma unroll
+                for (int k = 0; k < kJoin; ++k) {
+                    float f = ms[k] == -INFINITY ? 0.f : exp2f((ms[k] - now) * scale);
+                    f = ls[k] != ls[k] ? __uint_as_float(0x7FC00000u) : f;
+                    f = s + k < count ? f : 0.f;
+                    total += f * (s + k < count ? ls[k] : 0.f);
+                    precise += f * (s + k < count ? es[k] : 0.f);
+#pragma unroll
+                    for (int e = 0; e < 2 * NB; ++e)
+                        r[e] += s + k < count ? f * x[k][e] : 0.f;
                 }
             }
             if (!done) {
                 float* to = const_cast<float*>(from);                  // in the place of the first of them
-                if (live) {
 #pragma unroll
-                    for (int e = 0; e < 2 * NB; ++e)
-                        put_through(&to[((qt * 2 * NB + e) * 4 + wave) * 64 + lane], r[e]);
-                }
+                for (int e = 0; e < 2 * NB; ++e)
+                    put_through(&to[((qt * 2 * NB + e) * 4 + wave) * 64 + lane], r[e]);
                 if (wave == 0 && g == 0) {
                     put_through(&to[QT * NB * 512 + qt * 48 + c], top);
                     put_through(&to[QT * NB * 512 + qt * 48 + 16 + c], total);
