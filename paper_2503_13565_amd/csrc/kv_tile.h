@@ -88,13 +88,13 @@ __device__ __forceinline__ KvRow kv_row(const KvAttend& a, int b)
 // What the parts aim for (dim 128, us):
 //   as they are  rows whose longest ends no later than parts would, the joining (`joint` units' time) with them
 //   one round    with few rows of one length, the shortest parts that `target` workgroups hold at once (16 rows of 32000 tokens, 64 query heads on 8:
-//                112; twice as many parts 119)
+//                113; twice as many parts 118)
 //   several      with many rows of different lengths, parts of half a workgroup's share, since parts of one length do not come out
-//                (64 rows of 500 to 16384 tokens: 81, not 86)
-//   short parts  (up to `brief` units) half of `target`, because joining costs more than it saves (4 rows of 16000 tokens: 21.6,
-//                not 23.3)
+//                (64 rows of 500 to 16384 tokens: 85, not 87.5)
+//   short parts  (up to `brief` units) half of `target`, because joining costs more than it saves (4 rows of 16000 tokens: 22.9,
+//                not 24.3)
 //   a row alone  no more than the kKvJoin parts that are joined at a time, unless that leaves a part over four units
-//                (one row of 2000 tokens: 9.1, and 10.7 with parts of one unit); whole up to six units (32 heads, 500 tokens: 7.8, not 10.1)
+//                (one row of 2000 tokens: 9.6, and 11.3 with parts of one unit); whole up to six units (32 heads, 500 tokens: 8.2, not 9.6)
 constexpr int kKvJoin = 8;
 template <int kUnit>
 __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_rows, int brief, int joint, KvItem* out)
