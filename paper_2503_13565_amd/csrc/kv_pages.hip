@@ -65,19 +65,32 @@ __device__ __forceinline__ int scan_of_wave(int v)
     return v;
 }
 
-// Inclusive sum over the workgroup's 1024 threads, in thread order, and the sum of all; `sums` holds a number per wave.
-__device__ __forceinline__ int block_scan(int v, int* sums, int* all)
+// Inclusive sums of two numbers over the workgroup's 1024 threads, in thread order, the sums of all, and that of a third number;
+// `sums` holds three numbers per wave.
+struct Scan {
+    int a, b, all_a, all_b, all_c;
+};
+__device__ __forceinline__ Scan block_scan(int a, int b, int c, int (*sums)[16])
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    v = scan_of_wave(v);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Scan s;
+    s.a = scan_of_wave(a);
+    s.b = scan_of_wave(b);
+    c = scan_of_wave(c);
     __syncthreads();                             // (the last scan's sums are read)
-    if (lane == 63)
-        sums[wave] = v;
+    if (lane == 63) {
+        sums[0][wave] = s.a;
+        sums[1][wave] = s.b;
+        sums[2][wave] = c;
+    }
     __syncthreads();
-    const int upto = scan_of_wave(lane < 16 ? sums[lane] : 0);
-    *all = __builtin_amdgcn_readlane(upto, 15);
-    const int before = __builtin_amdgcn_readlane(upto, max(__builtin_amdgcn_readfirstlane(wave) - 1, 0));
-    return v + (wave ? before : 0);
+    const int upto_a = scan_of_wave(lane < 16 ? sums[0][lane] : 0), upto_b = scan_of_wave(lane < 16 ? sums[1][lane] : 0);
+    s.all_a = __builtin_amdgcn_readlane(upto_a, 15);
+    s.all_b = __builtin_amdgcn_readlane(upto_b, 15);
+    s.all_c = __builtin_amdgcn_readlane(scan_of_wave(lane < 16 ? sums[2][lane] : 0), 15);
+    s.a += wave ? __builtin_amdgcn_readlane(upto_a, max(wave - 1, 0)) : 0;
+    s.b += wave ? __builtin_amdgcn_readlane(upto_b, max(wave - 1, 0)) : 0;
+    return s;
 }
 
 // A word of the free bits; bits past the last page name no page, whatever they hold.
@@ -91,7 +104,7 @@ __device__ __forceinline__ uint32_t free_word(const KvPool& p, int words, int w)
 
 // One workgroup of 1024 threads: the rows are scanned for what each needs, the free bits for the pages of the lowest numbers.
 // Free pages are dealt out 1024 words (32768 pages) at a time: their numbers go to a list in the LDS in order, then every
-// page finds its row by bisection among the rows' sums.  Latency-bound: a chain of some twelve loads, scans and barriers.
+// page finds its row by bisection among the rows' sums.  Latency-bound: a chain of some ten loads, scans and barriers.
 // kEach: rows of a thread, 1 up to 1024 rows, 4 up to 4096.
 template <int kEach>
 __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t* rows, const int32_t* add, int count, int32_t* copies,
@@ -103,7 +116,7 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
     int* sum = mine + kRows;                     // needs of rows 0 .. i together
     int* first = sum + kRows;                    // where a row's first new page goes
     uint16_t* list = reinterpret_cast<uint16_t*>(first + kRows);
-    __shared__ int sums[16], bad;
+    __shared__ int sums[3][16], bad;
     const int tid = threadIdx.x;
     if (tid == 0)
         bad = 0;
@@ -120,9 +133,9 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
         n[j] = row[j] < 0 ? 0 : max(p.lens[row[j]], 0);
         a[j] = row[j] < 0 ? 0 : a[j];
     }
-    int have = __popc(word0);
+    int more = 0;                                // free pages of the words behind
     for (int w = 1024 + tid; w < words; w += 1024)
-        have += __popc(free_word(p, words, w));
+        more += __popc(free_word(p, words, w));
     __syncthreads();
     int refs[kEach];
 #pragma unroll
@@ -141,8 +154,7 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
         }
         mine[tid * kEach + j] = page;
     }
-    int free_pages;
-    block_scan(have, sums, &free_pages);         // (its barriers also show everybody `mine`)
+    __syncthreads();                             // (everybody sees `mine`)
     int need[kEach], own = 0;
     bool copy[kEach];
 #pragma unroll
@@ -163,8 +175,9 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
         first[i] = w - copy[j];
         own += need[j];
     }
-    int total;
-    int at = block_scan(own, sums, &total) - own;
+    Scan scan = block_scan(own, __popc(word0), more, sums);
+    const int total = scan.all_a, free_pages = scan.all_b + scan.all_c;
+    int at = scan.a - own;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
         const int i = tid * kEach + j;
@@ -195,11 +208,10 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
     int done = 0;
     for (int w0 = 0; done < total; w0 += 1024) {
         const uint32_t word = w0 == 0 ? word0 : free_word(p, words, w0 + tid);
-        const int c = __popc(word);
-        int found;
-        const int upto = block_scan(c, sums, &found);
-        const int left = total - done;           // of this tile's free pages, the first `left` are taken
-        int k = upto - c;
+        if (w0)
+            scan = block_scan(0, __popc(word), 0, sums);
+        const int found = scan.all_b, left = total - done;             // of this tile's free pages, the first `left` are taken
+        int k = scan.b - __popc(word);
         uint32_t rest = word;
         while (rest && k < left) {
             const int bit = __ffs(rest) - 1;
@@ -212,7 +224,7 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
         const int got = min(found, left);
         for (int r = tid; r < got; r += 1024) {
             const int rank = done + r, page = w0 * 32 + list[r];
-            int lo = 0, hi = kRows - 1;          // the first row whose sum passes the rank
+            int lo = 0, hi = count - 1;          // the first row whose sum passes the rank
             while (lo < hi) {
                 const int m = (lo + hi) >> 1;
                 if (sum[m] > rank)

@@ -213,15 +213,12 @@ __global__ __launch_bounds__(256) void kv_copy_kernel(KvView c, const int32_t* s
                                                       int n_rows, const int32_t* lens, const int32_t* add)
 {
     const int from = src[(int64_t)blockIdx.x * pitch], to = dst[(int64_t)blockIdx.x * pitch];
-    if ((unsigned)from >= (unsigned)c.pages || (unsigned)to >= (unsigned)c.pages)
+    const int row = rows ? rows[blockIdx.x] : 0, grown = rows ? add[blockIdx.x] : 0;   // (asked for with the pages)
+    if ((unsigned)from >= (unsigned)c.pages || (unsigned)to >= (unsigned)c.pages || (rows && (unsigned)row >= (unsigned)n_rows))
         return;
     int tokens = 1 << c.shift;
-    if (rows) {
-        const int row = rows[blockIdx.x];
-        if ((unsigned)row >= (unsigned)n_rows)
-            return;
-        tokens = (((lens[row] - add[blockIdx.x]) & (tokens - 1)) + 15) & ~15;
-    }
+    if (rows)
+        tokens = (((lens[row] - grown) & (tokens - 1)) + 15) & ~15;
     const int q_run = tokens * c.nb, s_run = tokens * c.nb / 16;         // 16-byte pieces of a head
     const int q_page = c.nb << c.shift, s_page = (c.nb << c.shift) / 16;
     const int each = 2 * (q_run + s_run), total = each * c.heads;
@@ -267,8 +264,10 @@ hipError_t launch_kv_copy(const KvView& c, const int32_t* src, const int32_t* ds
                           int n_rows, const int32_t* lens, const int32_t* add, hipStream_t stream)
 {
     const int64_t pieces = (int64_t)2 * c.heads * ((c.nb << c.shift) + (c.nb << c.shift) / 16);
-    int64_t blocks = (pieces + 1023) / 1024;
-    const int64_t most = 4096 / count + 1;           // enough to fill the device, four pieces or more for each thread
+    // A piece for each thread while that is about a thousand workgroups: eight begun pages of 32 heads then take 3.1 us, not 4.0 with four
+    // pieces each; more workgroups only add to the calls in which few rows have a page to copy.
+    int64_t blocks = (pieces + 255) / 256;
+    const int64_t most = 1024 / count + 1;
     blocks = blocks < most ? blocks : most;
     hipLaunchKernelGGL(kv_copy_kernel, dim3((unsigned)count, (unsigned)blocks), dim3(256), 0, stream, c, src, dst, pitch, rows, n_rows, lens,
                        add);
