@@ -9,6 +9,8 @@
 //   scores   S^T[token][query]  = K . Q^T      keys are the left operand, decoded in registers (kv_tile.h)
 //   values   O^T[element][query] += V^T . P^T   the scores leave the first product in the layout in which the second one takes
 //                                               them as its right operand: no LDS and no crossing of lanes in the loop
+#include <algorithm>
+
 #include "kv_tile.h"
 
 namespace mxfp4 {
@@ -380,9 +382,25 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     }
 }
 
-// Query tiles of a workgroup: two where an average sequence has more queries than one tile holds, and the registers hold the
+// Query tiles of a workgroup at most: two where an average sequence has more queries than one tile holds, and the registers hold the
 // sums (8 times the tiles times dim / 32 of them).
-static int query_tiles(int nb, int64_t queries) { return queries <= 16 || nb > 4 ? 1 : 2; }
+static int most_query_tiles(int nb, int64_t queries) { return queries <= 16 || nb > 4 ? 1 : 2; }
+
+// Two tiles decode a token once for both, one tile loads, combines and joins less in front of the first result: one where the
+// workgroups with one tile run at once and all of them read less than 4096 tokens for each compute unit, as far as the table can
+// tell the lengths (us with one and with two: 4 new tokens, 64 heads on 8, over 1000: 9.6 and 13.2, 4 rows over 16000: 30 and 34, over
+// 32000: 52 and 50, 16 rows over 16000: 95 and 80; prompts of 32 heads of their own, 100 tokens: 6.2 and 8.2, 1000: 39 and 31, 5001: 456 and 311).
+static int query_tiles(const KvAttend& a, const DeviceInfo& dev)
+{
+    const int64_t queries = ((int64_t)a.b.tokens * a.group + a.b.rows - 1) / a.b.rows;
+    if (most_query_tiles(a.c.nb, queries) == 1)
+        return 1;
+    const int64_t tiles = a.b.rows * ((queries + 15) / 16) * a.c.heads;
+    int64_t tokens = (int64_t)a.b.width << a.c.shift;
+    if (a.window > 0)
+        tokens = std::min(tokens, a.window + queries / a.group);
+    return tiles <= 2 * dev.cus && tiles * tokens < (int64_t)dev.cus * 4096 ? 1 : 2;
+}
 
 static int padded(int nb) { return nb == 3 ? 4 : nb == 6 ? 8 : nb; }
 
@@ -391,7 +409,7 @@ static int attend_target(int nb, const DeviceInfo& dev) { return dev.cus * (nb <
 
 size_t kv_attend_part_bytes(int nb, int group, int64_t tokens, int64_t rows, const DeviceInfo& dev)
 {
-    const int qt = query_tiles(nb, rows ? (tokens * group + rows - 1) / rows : 0);
+    const int qt = most_query_tiles(nb, rows ? (tokens * group + rows - 1) / rows : 0);
     return ((size_t)4 * attend_target(nb, dev) + 8) * (qt * padded(nb) * 512 + 48 * qt) * sizeof(float);
 }
 
@@ -408,7 +426,7 @@ static hipError_t launch_attend(const KvAttend& a, int qt, int64_t blocks, hipSt
 
 hipError_t launch_kv_attend(KvAttend a, const DeviceInfo& dev, hipStream_t stream)
 {
-    const int qt = query_tiles(a.c.nb, ((int64_t)a.b.tokens * a.group + a.b.rows - 1) / a.b.rows);
+    const int qt = query_tiles(a, dev);
     a.target = attend_target(a.c.nb, dev);
     // No more workgroups than shares: 2 target + tiles x heads by the cutting, and no more than the tables' units.
     const int64_t per = 16 * qt;
