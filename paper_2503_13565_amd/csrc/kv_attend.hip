@@ -20,7 +20,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
 {
     typedef KvTile<NB, kPad> T;
     constexpr int NW = 4, kRows = 16 * QT, kEl = T::kEl, kChunks = T::kChunks;
-    constexpr int kDepth = QT == 1 ? 3 : 2;
+    constexpr int kDepth = QT == 1 ? 3 : 2;                            // tiles in flight: what the registers hold (one more spills: prompt 372 us, not 311)
     constexpr int kSlot = QT * NB * 512 + 48 * QT;                     // floats of a partial result
     constexpr int kJoin = kKvJoin, kFinal = 8192;                         // parts added at a time; where the counters of the last sums begin
     __shared__ __align__(16) float comb[NW][kEl][4][64];
@@ -404,13 +404,14 @@ static int query_tiles(const KvAttend& a, const DeviceInfo& dev)
 
 static int padded(int nb) { return nb == 3 ? 4 : nb == 6 ? 8 : nb; }
 
-// Workgroups that the cutting aims for: as many as run at once.
-static int attend_target(int nb, const DeviceInfo& dev) { return dev.cus * (nb <= 4 ? 2 : 1); }
+// Workgroups that the cutting aims for: two for each compute unit, as many as run at once up to dim 128. (Of dim 256 one runs at once: 8 rows
+// of 16000 tokens, 16 heads on 2, take 29.1 us all the same, 35.6 with parts of twice the length; 32 rows of up to 8000 91 either way.)
+static int attend_target(const DeviceInfo& dev) { return 2 * dev.cus; }
 
 size_t kv_attend_part_bytes(int nb, int group, int64_t tokens, int64_t rows, const DeviceInfo& dev)
 {
     const int qt = most_query_tiles(nb, rows ? (tokens * group + rows - 1) / rows : 0);
-    return ((size_t)4 * attend_target(nb, dev) + 8) * (qt * padded(nb) * 512 + 48 * qt) * sizeof(float);
+    return ((size_t)4 * attend_target(dev) + 8) * (qt * padded(nb) * 512 + 48 * qt) * sizeof(float);
 }
 
 template <int NB, bool kPad>
@@ -427,7 +428,7 @@ static hipError_t launch_attend(const KvAttend& a, int qt, int64_t blocks, hipSt
 hipError_t launch_kv_attend(KvAttend a, const DeviceInfo& dev, hipStream_t stream)
 {
     const int qt = query_tiles(a, dev);
-    a.target = attend_target(a.c.nb, dev);
+    a.target = attend_target(dev);
     // No more workgroups than shares: 2 target + tiles x heads by the cutting, and no more than the tables' units.
     const int64_t per = 16 * qt;
     const int64_t tiles = a.b.starts ? (int64_t)a.b.tokens * a.group / per + a.b.rows : a.b.rows * (((int64_t)a.b.per_row * a.group + per - 1) / per);
