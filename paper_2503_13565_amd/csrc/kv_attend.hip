@@ -341,7 +341,11 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                 }
             }
             if (!done) {
-                float* to = const_cast<float*>(from);                  // in the place of the first of them
+                // In the place of the first of them, whose maximum and sums all four waves read and wave 0 replaces: no wave stores before
+                // every wave's loads are here.  (`done` and the loops' bounds are the same for the whole workgroup.)
+                drain_vmem();
+                __syncthreads();
+                float* to = const_cast<float*>(from);
 #pragma unroll
                 for (int e = 0; e < 2 * NB; ++e)
                     put_through(&to[((qt * 2 * NB + e) * 4 + wave) * 64 + lane], r[e]);
