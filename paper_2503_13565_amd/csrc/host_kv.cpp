@@ -203,8 +203,8 @@ PyObject* kv_attention(PyObject*, PyObject* const* args, Py_ssize_t count)
             return left();
         a.scale = (float)s;
     }
-    if (args[6] != Py_True && args[6] != Py_False)
-        return left();
+    if ((args[6] != Py_True && args[6] != Py_False) || (args[9] != Py_True && args[9] != Py_False))
+        return left();                                  // (any other truth value is the binding's to read)
     a.causal = args[6] == Py_True;
     a.window = window;
     a.q_heads = q->size(1);
