@@ -257,7 +257,8 @@ int mxfp4_kv_attention(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, 
     a.tree = args->tree;
     a.group = (int)(args->q_heads / cache->heads);
     a.causal = args->causal != 0;
-    a.window = (int)args->window;
+    // Positions lie in [-2^30, 2^30): a wider window hides nothing, and their differences stay within 32 bits.
+    a.window = (int)(args->window < (1 << 30) ? args->window : 1 << 30);
     a.scale = args->scale * 1.4426950408889634f;
     a.counters = static_cast<uint32_t*>(workspace);
     a.part = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + MXFP4_KV_COUNTERS * sizeof(uint32_t));

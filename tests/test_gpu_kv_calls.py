@@ -24,3 +24,19 @@ def test_truth_values_of_attention(yes, no):
             assert isinstance(got, tuple) and torch.equal(got[0], want[c][0]) and torch.equal(got[1], want[c][1])
             alone = binding.mxfp4_kv_attention(q, cache, table, lens, causal=given, return_lse=no)
             assert isinstance(alone, torch.Tensor) and torch.equal(alone, want[c][0])
+
+
+@pytest.mark.parametrize("window", [1 << 20, (1 << 30) - 1, 1 << 30, (1 << 30) + 1, (1 << 31) - 7, (1 << 31) - 1])
+@pytest.mark.parametrize("causal", [True, False])
+def test_windows_wider_than_any_row(window, causal):
+    # more new tokens than cached ones: the first stand at positions below 0, and differences of positions and windows are largest
+    p = Paged([3, 0, 40, 1], 1, 16, 64, seed=2)
+    table, lens = p.batch(DEV)
+    cache = p.cache(DEV)
+    starts = torch.tensor([0, 6, 8, 53, 93], dtype=torch.int32, device=DEV)
+    q = tokens(torch.Generator().manual_seed(1), 93, 2, 64).to(DEV)
+    want = binding.mxfp4_kv_attention(q, cache, table, lens, starts=starts, causal=causal, return_lse=True)
+    got = binding.mxfp4_kv_attention(q, cache, table, lens, starts=starts, causal=causal, window=window, return_lse=True)
+    assert torch.isfinite(want[1]).any()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
