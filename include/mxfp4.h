@@ -376,7 +376,7 @@ int mxfp4_kv_fork(const mxfp4_kv_pool* pool, const int32_t* src, const int32_t* 
  * that order, while others hold it.  `cache` (NULL: no copying, the caller has `copies`): arrays whose pages
  * hold all layers.  copies (device, int32 [count][2]): (from, to) of each row's copied page, -1 where none.
  * missing (device, int32 [1]): 0, or how many pages (or -1: a row would pass its table's width) are missing; then
- * nothing was changed.  count <= 4096; add >= 0.
+ * nothing was changed (needs past 2^31 - 1 pages together count as that many).  count <= 4096; add >= 0.
  */
 int mxfp4_kv_extend(const mxfp4_kv_pool* pool, const mxfp4_kv_cache* cache, const int32_t* rows_list,
                     const int32_t* add, int64_t count, int32_t* copies, int32_t* missing, void* stream);

@@ -65,8 +65,21 @@ __device__ __forceinline__ int scan_of_wave(int v)
     return v;
 }
 
+// The same for numbers below 2^31, whose sums stop there: rows may ask for 2^26 pages each, 2^38 together.
+__device__ __forceinline__ int add_up_to_cap(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, 0x7FFFFFFFu); }
+__device__ __forceinline__ int capped_scan_of_wave(int v)
+{
+    v = add_up_to_cap(v, shifted_or_zero<0x111, 0xF>(v));
+    v = add_up_to_cap(v, shifted_or_zero<0x112, 0xF>(v));
+    v = add_up_to_cap(v, shifted_or_zero<0x114, 0xF>(v));
+    v = add_up_to_cap(v, shifted_or_zero<0x118, 0xF>(v));
+    v = add_up_to_cap(v, shifted_or_zero<0x142, 0xA>(v));
+    v = add_up_to_cap(v, shifted_or_zero<0x143, 0xC>(v));
+    return v;
+}
+
 // Inclusive sums of two numbers over the workgroup's 1024 threads, in thread order, the sums of all, and that of a third number;
-// `sums` holds three numbers per wave.
+// `sums` holds three numbers per wave.  Those of `a` stop at 2^31 - 1.
 struct Scan {
     int a, b, all_a, all_b, all_c;
 };
@@ -74,7 +87,7 @@ __device__ __forceinline__ Scan block_scan(int a, int b, int c, int (*sums)[16])
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Scan s;
-    s.a = scan_of_wave(a);
+    s.a = capped_scan_of_wave(a);
     s.b = scan_of_wave(b);
     c = scan_of_wave(c);
     __syncthreads();                             // (the last scan's sums are read)
@@ -84,11 +97,11 @@ __device__ __forceinline__ Scan block_scan(int a, int b, int c, int (*sums)[16])
         sums[2][wave] = c;
     }
     __syncthreads();
-    const int upto_a = scan_of_wave(lane < 16 ? sums[0][lane] : 0), upto_b = scan_of_wave(lane < 16 ? sums[1][lane] : 0);
+    const int upto_a = capped_scan_of_wave(lane < 16 ? sums[0][lane] : 0), upto_b = scan_of_wave(lane < 16 ? sums[1][lane] : 0);
     s.all_a = __builtin_amdgcn_readlane(upto_a, 15);
     s.all_b = __builtin_amdgcn_readlane(upto_b, 15);
     s.all_c = __builtin_amdgcn_readlane(scan_of_wave(lane < 16 ? sums[2][lane] : 0), 15);
-    s.a += wave ? __builtin_amdgcn_readlane(upto_a, max(wave - 1, 0)) : 0;
+    s.a = add_up_to_cap(s.a, wave ? __builtin_amdgcn_readlane(upto_a, max(wave - 1, 0)) : 0);
     s.b += wave ? __builtin_amdgcn_readlane(upto_b, max(wave - 1, 0)) : 0;
     return s;
 }
@@ -176,6 +189,7 @@ __global__ __launch_bounds__(1024) void kv_extend_kernel(KvPool p, const int32_t
         own += need[j];
     }
     Scan scan = block_scan(own, __popc(word0), more, sums);
+    // (a total at the cap is past every number of pages; below it no sum has stopped)
     const int total = scan.all_a, free_pages = scan.all_b + scan.all_c;
     int at = scan.a - own;
 #pragma unroll

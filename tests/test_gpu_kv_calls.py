@@ -40,3 +40,22 @@ def test_windows_wider_than_any_row(window, causal):
     assert torch.isfinite(want[1]).any()
     for x, y in zip(got, want):
         assert torch.equal(x, y)
+
+
+def test_growing_by_more_pages_than_32_bits_count():
+    # 66 rows of up to 2^26 pages each (the table's memory is asked for and never written)
+    width, rows, pages = 1 << 26, 66, 100
+    pool, cache = binding.mxfp4_kv_pool(pages, DEV), binding.mxfp4_kv_cache(pages, 1, 16, 32, device=DEV)
+    table, lens = torch.empty((rows, width), dtype=torch.int32, device=DEV), torch.zeros(rows, dtype=torch.int32, device=DEV)
+    free = pool.free.clone()
+    full = 16 * width
+    for adds, want in (([full] * 31, 31 * width), ([full] * 32, 32 * width), ([full] * 33, 33 * width), ([full] * 64, 64 * width),
+                       ([full] * 64 + [40], 64 * width + 3), ([40] + [full] * 64, 64 * width + 3), ([full] * 66, 66 * width),
+                       ([full] * 1500, 1500 * width)):                # (rows that are listed again: nothing is changed all the same)
+        some = torch.arange(len(adds), dtype=torch.int32, device=DEV) % rows
+        missing = binding.mxfp4_kv_extend(pool, cache, table, lens, some, torch.tensor(adds, dtype=torch.int32, device=DEV))
+        assert int(missing) == min(want, 2 ** 31 - 1) - pages, (len(adds), int(missing))
+        assert not lens.any() and not pool.refs.any() and torch.equal(pool.free, free), len(adds)
+    some, add = torch.tensor([3, 65], dtype=torch.int32, device=DEV), torch.tensor([16 * 60, 16 * 40], dtype=torch.int32, device=DEV)
+    assert int(binding.mxfp4_kv_extend(pool, cache, table, lens, some, add)) == 0
+    assert table[3, :60].tolist() == list(range(60)) and table[65, :40].tolist() == list(range(60, 100))
