@@ -327,7 +327,8 @@ int mxfp4_kv_read(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, const
  * A token that sees nothing gives zeros and an lse of -infinity.  What a token does not see does not
  * touch its result, NaN blocks included; a NaN block that it sees gives NaN.
  *   workspace     mxfp4_kv_attention_workspace_bytes bytes, 16-byte aligned, the first MXFP4_KV_COUNTERS * 4 of them
- *                 ZERO before the first call; every call leaves them zero.  Calls that overlap in time must not share it.
+ *                 ZERO before the first call; every call leaves them zero, for any contents of lens and starts.  Calls that
+ *                 overlap in time must not share it.
  * q_heads is a multiple of cache->heads.  The summation order follows from the sizes (the table's width among them), the
  * lengths and starts: the same inputs give the same bits.
  */

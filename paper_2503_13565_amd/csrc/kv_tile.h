@@ -64,16 +64,20 @@ __device__ __forceinline__ int wave_scan(int v)
 // A row's new tokens, its length (both held to what the tables can hold) and where its keys begin to count.
 struct KvRow {
     int n, len, first, lo;
+    bool down;                       // its starts descend
 };
 __device__ __forceinline__ KvRow kv_row(const KvAttend& a, int b)
 {
     KvRow r;
     if (a.b.starts) {
-        r.first = min(max(a.b.starts[b], 0), a.b.tokens);
-        r.n = min(max(a.b.starts[b + 1], r.first), a.b.tokens) - r.first;
+        const int from = a.b.starts[b], to = a.b.starts[b + 1];
+        r.first = min(max(from, 0), a.b.tokens);
+        r.n = min(max(to, r.first), a.b.tokens) - r.first;
+        r.down = to < from;
     } else {
         r.first = b * a.b.per_row;
         r.n = a.b.per_row;
+        r.down = false;
     }
     r.len = min(max(a.b.lens[b], 0), a.b.width << a.c.shift);
     r.lo = a.window > 0 ? max(0, min(r.len, r.len - r.n + 1 - a.window)) & ~31 : 0;
@@ -86,7 +90,9 @@ __device__ __forceinline__ KvRow kv_row(const KvAttend& a, int b)
 // change between replays of a graph, and sequences of different lengths load the device evenly.  Only rows of two parts or more need
 // partial results: at most 4 target of them (U is summed in FP32, which all workgroups do alike; a few more for its rounding).
 // What the parts aim for (dim 128, us):
-//   as they are  rows whose longest ends no later than parts would, the joining (`joint` units' time) with them
+//   as they are  rows whose longest ends no later than parts would, the joining (`joint` units' time) with them; and starts that descend
+//                somewhere: the rows then have more shares together than the launch has workgroups, and a row's parts would wait
+//                for some that never come, with their counter above zero
 //   one round    with few rows of one length, the shortest parts that `target` workgroups hold at once (16 rows of 32000 tokens, 64 query heads on 8:
 //                113; twice as many parts 118)
 //   several      with many rows of different lengths, parts of half a workgroup's share, since parts of one length do not come out
@@ -100,7 +106,8 @@ template <int kUnit>
 __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_rows, int brief, int joint, KvItem* out)
 {
     const int lane = threadIdx.x & 63;
-    KvRow r0 = {0, 0, 0, 0};
+    KvRow r0 = {0, 0, 0, 0, false};
+    bool down = false;
     float all = 0.f, longest = 0.f, whole = 0.f;    // units, those of the longest row, rows of keys
     for (int base = 0; base < a.b.rows; base += 64) {
         float u = 0.f, t = 0.f;
@@ -110,6 +117,7 @@ __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_ro
             u = tiles * units;
             t = tiles;
             longest = fmaxf(longest, tiles > 0.f ? units : 0.f);
+            down |= r.down;
             if (base == 0)
                 r0 = r;
         }
@@ -121,7 +129,7 @@ __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_ro
     whole *= (float)a.c.heads;
     const float target = (float)a.target, even = ceilf(all / target);
     float aim = even;
-    if (fmaxf(longest, all / target + 0.5f * longest) <= 1.5f * all / target + (float)joint) {
+    if (__ballot(down) || fmaxf(longest, all / target + 0.5f * longest) <= 1.5f * all / target + (float)joint) {
         aim = 1e9f;
     } else if (2.f * whole <= target && longest * whole <= 1.05f * all && a.b.rows <= 64) {
         const int tiles = (r0.n * a.group + tile_rows - 1) / tile_rows * a.c.heads, units = max(1, (r0.len - r0.lo + kUnit - 1) / kUnit);

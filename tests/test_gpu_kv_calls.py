@@ -59,3 +59,27 @@ def test_growing_by_more_pages_than_32_bits_count():
     some, add = torch.tensor([3, 65], dtype=torch.int32, device=DEV), torch.tensor([16 * 60, 16 * 40], dtype=torch.int32, device=DEV)
     assert int(binding.mxfp4_kv_extend(pool, cache, table, lens, some, add)) == 0
     assert table[3, :60].tolist() == list(range(60)) and table[65, :40].tolist() == list(range(60, 100))
+
+
+@pytest.mark.parametrize("group", [8, 24])                            # (one tile of queries, and two)
+def test_descending_starts_leave_the_counters_at_zero(group):
+    # every other row's starts go back to 0: their tokens together are 256 times those of the batch, and the one long row, which would
+    # be cut, stands where the launch's workgroups end
+    rows, page, heads, long = 512, 64, 4, 20000
+    width = long // page + 1
+    cache = binding.mxfp4_kv_cache(width, heads, page, 64, device=DEV)
+    for x, byte in zip(cache, (0x21, 127, 0x32, 127)):
+        x.fill_(byte)
+    table = torch.arange(width, dtype=torch.int32, device=DEV).repeat(rows, 1)
+    q = tokens(torch.Generator().manual_seed(1), 8, group * heads, 64).to(DEV)
+    need = max(binding.mxfp4_kv_attention_workspace_bytes(cache, r, 8, group * heads) for r in (rows, 1))
+    ws = torch.zeros(need, dtype=torch.uint8, device=DEV)
+    flat = [0, 8] * (rows // 2) + [8]
+    for at in range(2, rows, 37):
+        lens = torch.full((rows,), 100, dtype=torch.int32, device=DEV)
+        lens[at & ~1] = long
+        binding.mxfp4_kv_attention(q, cache, table, lens, starts=torch.tensor(flat, dtype=torch.int32, device=DEV), workspace=ws)
+        assert not ws[: 4 * binding.KV_COUNTERS].any(), at
+    one = torch.tensor([long], dtype=torch.int32, device=DEV)
+    want = binding.mxfp4_kv_attention(q, cache, table[:1], one)
+    assert torch.equal(binding.mxfp4_kv_attention(q, cache, table[:1], one, workspace=ws), want)
