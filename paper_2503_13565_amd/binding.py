@@ -1063,6 +1063,12 @@ def mxfp4_kv_layer(cache: KvCache, layer: int) -> KvCache:
 
 
 def mxfp4_kv_all_layers(cache: KvCache) -> KvCache:
+    """The same memory with layers and heads in one dimension.  Some of the heads alone cannot be seen so (a copy would take what
+    extend, compact and copies store and lose it)."""
+    for x in cache:
+        if x.dim() != 5 or (x.shape[1] > 1 and x.shape[2] > 0 and x.stride(1) != x.shape[2] * x.stride(2)):
+            raise ValueError("a cache with layers is [pages, layers, heads, page, ...] with all heads of a layer in a row: got %r with strides %r" % (
+                tuple(x.shape), x.stride()))
     return KvCache(*(x.flatten(1, 2) for x in cache))
 
 
