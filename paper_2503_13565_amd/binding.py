@@ -1267,6 +1267,8 @@ def mxfp4_kv_extend(pool: KvPool, cache: KvCache, table: torch.Tensor, lens: tor
     if got is not None:
         return got
     dev = pool.refs.device
+    if cache.kq.device != dev:                                        # its pages are copied by a kernel of the pool's device
+        raise ValueError("the cache must be on the pool's device %s, it is on %s" % (dev, cache.kq.device))
     p, n = _kv_pool_desc(pool, cache, table, lens), _kv_two_lists(rows, add, "rows and add", dev)
     got = torch.empty((2 * n + 1,), dtype=torch.int32, device=dev)
     with _on(dev):

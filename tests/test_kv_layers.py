@@ -23,3 +23,10 @@ def test_all_layers_are_the_same_memory():
 def test_what_would_be_a_copy_is_refused(part):
     with pytest.raises(ValueError):
         binding.mxfp4_kv_all_layers(binding.KvCache(*(part(x) for x in make())))
+
+
+def test_a_cache_on_another_device_than_its_pool_is_refused():
+    pool, cache = binding.mxfp4_kv_pool(4, "cpu"), binding.mxfp4_kv_cache(4, 1, 16, 32, device="meta")
+    t, n = torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="the cache must be on the pool's device cpu"):
+        binding.mxfp4_kv_extend(pool, cache, t, n, n, n)
