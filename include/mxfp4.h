@@ -325,7 +325,8 @@ int mxfp4_kv_read(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, const
  *                 place of the causal rule.
  *   lse_f32       (NULL: none) [tokens][q_heads]: the natural logarithm of the sum of exp(scale q . k)
  * A token that sees nothing gives zeros and an lse of -infinity.  What a token does not see does not
- * touch its result, NaN blocks included; a NaN block that it sees gives NaN.
+ * touch its result, NaN blocks and infinities included (codes of 2 and more under scale byte 254 and of 4 and more under 253 are
+ * infinite in BF16; no cast gives them); a NaN block that it sees gives NaN, an infinity that it sees an infinity.
  *   workspace     mxfp4_kv_attention_workspace_bytes bytes, 16-byte aligned, the first MXFP4_KV_COUNTERS * 4 of them
  *                 ZERO before the first call; every call leaves them zero, for any contents of lens and starts.  Calls that
  *                 overlap in time must not share it.

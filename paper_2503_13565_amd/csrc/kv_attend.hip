@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
             __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x2, 4 / QT, 0);
         }
-        uint32_t nan_at = 0;                                           // bit (chunk, half, token): a NaN block, taken out of the values
+        bool odd = false;                                              // the tile has values that may be no numbers
         if (masked) {
             uint64_t word[QT];
 #pragma unroll
@@ -117,14 +117,15 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                         s[qt][h][i] = there && sight.sees(at_q[qt], word[qt], j) ? s[qt][h][i] : -INFINITY;
 #pragma unroll
                     for (int ch = 0; ch < kChunks; ++ch) {
-                        const bool bad = value_scale(t, h, i, ch) == 0xFFu;
-                        if (bad || !there) {
+                        if (!there)
                             clear_value(t, h, i, ch);
-                            nan_at |= (there && bad ? 1u : 0u) << (ch * 8 + h * 4 + i);
-                        }
+                        odd |= value_scale(t, h, i, ch) >= kOddScale;
                     }
                 }
             }
+            odd = __ballot(odd) != 0;
+            if (odd)
+                drop_odd_values(t);
         }
         bf16x8_t p[QT];
 #pragma unroll
@@ -141,26 +142,25 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                 for (int qt = 0; qt < QT; ++qt)
                     o[qt][ch * kEl + e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[e], p[qt], o[qt][ch * kEl + e], 0, 0, 0);
         }
-        if (masked && __ballot(nan_at != 0)) {
-            // NaN blocks in a tile that not every query sees whole: counted for each query that sees one, by the same product with
-            // ones in the places of the blocks and of what is seen.
+        if (odd) {
+            // They are loaded once more (no register holds them over the product), for the queries that see them.
+            load_tile(t, a.c, it.h, j0, t.page[0], t.page[1]);
+            bf16x8_t seen[QT];
 #pragma unroll
-            for (int ch = 0; ch < kChunks; ++ch) {
-                typedef __attribute__((ext_vector_type(8))) uint16_t ones;
-                ones x;
+            for (int qt = 0; qt < QT; ++qt) {
+                const uint64_t word = sight.word(a, it, at_q[qt]);
+                u32x4_t y = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    x[i] = (nan_at >> (ch * 8 + i)) & 1 ? 0x3F80 : 0;
-#pragma unroll
-                for (int qt = 0; qt < QT; ++qt) {
-                    ones y;
-                    const uint64_t word = sight.word(a, it, at_q[qt]);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        y[i] = sight.sees(at_q[qt], word, j0 + 16 * (i >> 2) + 4 * g + (i & 3)) ? 0x3F80 : 0;
-                    mark_nan<kEl>(__builtin_bit_cast(bf16x8_t, x), __builtin_bit_cast(bf16x8_t, y), &o[qt][ch * kEl]);
+                for (int i = 0; i < 8; ++i) {
+                    const int j = j0 + 16 * (i >> 2) + 4 * g + (i & 3);
+                    if (t.page[i >> 2] >= 0 && j < it.len && sight.sees(at_q[qt], word, j))
+                        y[i >> 1] |= i & 1 ? 0x3F800000u : 0x3F80u;
                 }
+                seen[qt] = __builtin_bit_cast(bf16x8_t, y);
             }
+#pragma unroll
+            for (int ch = 0; ch < kChunks; ++ch)
+                add_odd_values<QT, 2 * NB>(t, ch, seen, o);
         }
     };
 

@@ -424,17 +424,62 @@ __device__ __forceinline__ bf16x8_t softmax_step(const f32x4_t* s, float scale, 
     return p;
 }
 
-// NaN blocks among values that not every query sees: counted for each query that sees one, by the values' product with ones in
-// the places of the blocks (x) and of what is seen (y); the sums of the lane's elements that it hits become NaN.
-template <int kSums>
-__device__ __forceinline__ void mark_nan(bf16x8_t x, bf16x8_t y, f32x4_t* o)
+// Values that are no numbers in a tile that not every query sees whole: all of a block of scale byte 255 (NaN), and infinities, codes
+// of 2 and more under byte 254, of 4 and more under 253 (no cast gives them, a cache may be filled otherwise).  0 times them is NaN, so they
+// leave the tile, and each query that sees one gets it by products of ones in the places of what is odd and of what the queries
+// see: `all` counts what a query sees, `sum` the infinities with their signs, so that sum = all says +infinity, sum = -all -infinity, and
+// anything else NaN.
+constexpr uint32_t kOddScale = 253;
+__device__ __forceinline__ uint32_t infinite_codes(uint32_t w, uint32_t byte)            // a bit for each element
 {
-    const f32x4_t hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+    return (byte == 254 ? w >> 2 : byte == 253 ? (w >> 2) & (w >> 1) : 0u) & 0x11111111u;
+}
+template <int NB, bool kPad>
+__device__ __forceinline__ void drop_odd_values(KvTile<NB, kPad>& t)
+{
 #pragma unroll
-    for (int e = 0; e < kSums; ++e)
+    for (int k = 0; k < 8; ++k)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            o[e][i] = hit[i] > 0.f ? __uint_as_float(0x7FC00000u) : o[e][i];
+        for (int ch = 0; ch < KvTile<NB, kPad>::kChunks; ++ch) {
+            const uint32_t byte = value_scale(t, k >> 2, k & 3, ch);
+            t.v[k >> 2][k & 3][ch] &= ~(15 * infinite_codes(t.v[k >> 2][k & 3][ch], byte));
+            if (byte == 255)
+                clear_value(t, k >> 2, k & 3, ch);
+        }
+}
+template <int QT, int kSums, int NB, bool kPad>
+__device__ __forceinline__ void add_odd_values(const KvTile<NB, kPad>& t, int ch, const bf16x8_t* seen, f32x4_t (*o)[kSums])
+{
+    typedef KvTile<NB, kPad> T;
+    uint32_t odd[8];                                     // of each token: for each element a bit "odd", one "infinite", one "negative"
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const uint32_t w = t.v[k >> 2][k & 3][ch], byte = value_scale(t, k >> 2, k & 3, ch), inf = infinite_codes(w, byte);
+        odd[k] = byte == 255 ? 0x11111111u : 3 * inf | (w >> 3 & inf) << 2;
+    }
+#pragma unroll 1
+    for (int e = 0; e < T::kEl; ++e) {                   // (rare: the elements take turns in one copy of the code)
+        u32x4_t x, y;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            const uint32_t n0 = odd[2 * m] >> (4 * e), n1 = odd[2 * m + 1] >> (4 * e);
+            x[m] = (n0 & 1 ? 0x3F80u : 0u) | (n1 & 1 ? 0x3F800000u : 0u);
+            y[m] = (n0 & 2 ? 0x3F80u | (n0 & 4) << 13 : 0u) | (n1 & 2 ? 0x3F800000u | (n1 & 4) << 29 : 0u);
+        }
+#pragma unroll
+        for (int qt = 0; qt < QT; ++qt) {
+            const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+            const f32x4_t all = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, x), seen[qt], zero, 0, 0, 0);
+            const f32x4_t sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, y), seen[qt], zero, 0, 0, 0);
+#pragma unroll
+            for (int k = 0; k < T::kEl; ++k)
+                if (k == e)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (all[i] > 0.f)
+                            o[qt][ch * T::kEl + k][i] += __uint_as_float(sum[i] == all[i] ? 0x7F800000u : sum[i] == -all[i] ? 0xFF800000u : 0x7FC00000u);
+        }
+    }
 }
 
 // Stores and loads that all dies of the device see alike.
