@@ -118,6 +118,23 @@ __device__ __forceinline__ KvPlace kv_place(const KvBatch& b, int t)
     return p;
 }
 
+// Inclusive sums over the wave's lanes, in the vector unit (through the LDS crossbar a step waits for its answer).
+template <int kCtrl, int kRows>
+__device__ __forceinline__ int dpp_or_zero(int v)
+{
+    return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v += dpp_or_zero<0x111, 0xF>(v);         // row_shr 1, 2, 4, 8: sums within 16 lanes
+    v += dpp_or_zero<0x112, 0xF>(v);
+    v += dpp_or_zero<0x114, 0xF>(v);
+    v += dpp_or_zero<0x118, 0xF>(v);
+    v += dpp_or_zero<0x142, 0xA>(v);         // the last lane of rows 0 and 2 to rows 1 and 3
+    v += dpp_or_zero<0x143, 0xC>(v);         // lane 31 to the upper half
+    return v;
+}
+
 // Page of position `at` of a row, or -1 where there is none.
 __device__ __forceinline__ int kv_page(const int32_t* table, int64_t ldt, int width, int shift, int pages, int row, int at)
 {

@@ -48,33 +48,16 @@ __global__ __launch_bounds__(256) void kv_release_kernel(KvPool p, const int32_t
     }
 }
 
-// Inclusive sums over a wave's lanes, in the vector unit.
-template <int kCtrl, int kRows>
-__device__ __forceinline__ int shifted_or_zero(int v)
-{
-    return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xF, false);
-}
-__device__ __forceinline__ int scan_of_wave(int v)
-{
-    v += shifted_or_zero<0x111, 0xF>(v);
-    v += shifted_or_zero<0x112, 0xF>(v);
-    v += shifted_or_zero<0x114, 0xF>(v);
-    v += shifted_or_zero<0x118, 0xF>(v);
-    v += shifted_or_zero<0x142, 0xA>(v);
-    v += shifted_or_zero<0x143, 0xC>(v);
-    return v;
-}
-
-// The same for numbers below 2^31, whose sums stop there: rows may ask for 2^26 pages each, 2^38 together.
+// wave_scan for numbers below 2^31, whose sums stop there: rows may ask for 2^26 pages each, 2^38 together.
 __device__ __forceinline__ int add_up_to_cap(int a, int b) { return (int)min((uint32_t)a + (uint32_t)b, 0x7FFFFFFFu); }
-__device__ __forceinline__ int capped_scan_of_wave(int v)
+__device__ __forceinline__ int capped_wave_scan(int v)
 {
-    v = add_up_to_cap(v, shifted_or_zero<0x111, 0xF>(v));
-    v = add_up_to_cap(v, shifted_or_zero<0x112, 0xF>(v));
-    v = add_up_to_cap(v, shifted_or_zero<0x114, 0xF>(v));
-    v = add_up_to_cap(v, shifted_or_zero<0x118, 0xF>(v));
-    v = add_up_to_cap(v, shifted_or_zero<0x142, 0xA>(v));
-    v = add_up_to_cap(v, shifted_or_zero<0x143, 0xC>(v));
+    v = add_up_to_cap(v, dpp_or_zero<0x111, 0xF>(v));
+    v = add_up_to_cap(v, dpp_or_zero<0x112, 0xF>(v));
+    v = add_up_to_cap(v, dpp_or_zero<0x114, 0xF>(v));
+    v = add_up_to_cap(v, dpp_or_zero<0x118, 0xF>(v));
+    v = add_up_to_cap(v, dpp_or_zero<0x142, 0xA>(v));
+    v = add_up_to_cap(v, dpp_or_zero<0x143, 0xC>(v));
     return v;
 }
 
@@ -87,9 +70,9 @@ __device__ __forceinline__ Scan block_scan(int a, int b, int c, int (*sums)[16])
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Scan s;
-    s.a = capped_scan_of_wave(a);
-    s.b = scan_of_wave(b);
-    c = scan_of_wave(c);
+    s.a = capped_wave_scan(a);
+    s.b = wave_scan(b);
+    c = wave_scan(c);
     __syncthreads();                             // (the last scan's sums are read)
     if (lane == 63) {
         sums[0][wave] = s.a;
@@ -97,10 +80,10 @@ __device__ __forceinline__ Scan block_scan(int a, int b, int c, int (*sums)[16])
         sums[2][wave] = c;
     }
     __syncthreads();
-    const int upto_a = capped_scan_of_wave(lane < 16 ? sums[0][lane] : 0), upto_b = scan_of_wave(lane < 16 ? sums[1][lane] : 0);
+    const int upto_a = capped_wave_scan(lane < 16 ? sums[0][lane] : 0), upto_b = wave_scan(lane < 16 ? sums[1][lane] : 0);
     s.all_a = __builtin_amdgcn_readlane(upto_a, 15);
     s.all_b = __builtin_amdgcn_readlane(upto_b, 15);
-    s.all_c = __builtin_amdgcn_readlane(scan_of_wave(lane < 16 ? sums[2][lane] : 0), 15);
+    s.all_c = __builtin_amdgcn_readlane(wave_scan(lane < 16 ? sums[2][lane] : 0), 15);
     s.a = add_up_to_cap(s.a, wave ? __builtin_amdgcn_readlane(upto_a, max(wave - 1, 0)) : 0);
     s.b += wave ? __builtin_amdgcn_readlane(upto_b, max(wave - 1, 0)) : 0;
     return s;
