@@ -9,6 +9,9 @@
 namespace mxfp4 {
 
 constexpr int kKvMaxRows = 4096;             // sequences of one extend (its scans live in the LDS)
+// Workgroups of 256 threads of one launch: the device counts a grid's threads along x in 32 bits, and what is past them is left out without
+// an error.  Calls with more workgroups are several launches.
+constexpr int kKvMostBlocks = 1 << 23;
 
 // The cache: page p of array x at x + p * stride, [heads][page][dim / 2] or [heads][page][dim / 32] inside.
 struct KvView {
@@ -27,6 +30,7 @@ struct KvBatch {
     const int32_t* lens;
     const int32_t* starts;
     int rows, width, tokens, per_row;
+    int t0;                                  // the launch's first token
 };
 
 struct KvTensor {
@@ -51,6 +55,7 @@ struct KvAttend {
     int window;                              // 0: none
     float scale;                             // times log2(e)
     int target;                              // workgroups that the cutting of long rows aims for
+    int item0;                               // the launch's first share
     uint32_t* counters;
     float* part;
 };
@@ -64,9 +69,9 @@ struct KvPool {
     int pages, shift, width, rows;
 };
 
-hipError_t launch_kv_append(const KvView& c, const KvBatch& b, const KvTensor& k, const KvTensor& v, const KvTensor& q,
+hipError_t launch_kv_append(const KvView& c, KvBatch b, const KvTensor& k, const KvTensor& v, const KvTensor& q,
                             const KvTensor& q_out, int q_heads, const KvRope& rope, hipStream_t stream);
-hipError_t launch_kv_read(const KvView& c, const KvBatch& b, const KvTensor& k, const KvTensor& v, hipStream_t stream);
+hipError_t launch_kv_read(const KvView& c, KvBatch b, const KvTensor& k, const KvTensor& v, hipStream_t stream);
 hipError_t launch_kv_compact(const KvView& c, const int32_t* table, int64_t ldt, int width, const int32_t* base,
                              const int32_t* keep, int ldk, const int32_t* counts, int rows, hipStream_t stream);
 // `rows` (null: whole pages): only the slots in use before rows[i] grew by add[i] are copied (rounded up to 16).

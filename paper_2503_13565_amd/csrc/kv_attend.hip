@@ -29,7 +29,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
     KvItem it;
-    if (!kv_find<NW * 32>(a, blockIdx.x, kRows, QT == 1 ? 16 : 8, QT == 1 ? 3 : 4, &it))
+    if (!kv_find<NW * 32>(a, a.item0 + (int)blockIdx.x, kRows, QT == 1 ? 16 : 8, QT == 1 ? 3 : 4, &it))
         return;                                                        // (the whole workgroup)
     const int rows = it.n * a.group, row0 = it.tile * kRows;
     const int i0 = row0 / a.group, i1 = min((row0 + kRows - 1) / a.group, it.n - 1);
@@ -419,13 +419,17 @@ size_t kv_attend_part_bytes(int nb, int group, int64_t tokens, int64_t rows, con
 }
 
 template <int NB, bool kPad>
-static hipError_t launch_attend(const KvAttend& a, int qt, int64_t blocks, hipStream_t stream)
+static hipError_t launch_attend(KvAttend a, int qt, int64_t blocks, hipStream_t stream)
 {
     auto kernel = kv_attend_kernel<NB, 1, kPad>;
     if constexpr (NB <= 4)
         if (qt == 2)
             kernel = kv_attend_kernel<NB, 2, kPad>;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, stream, a);
+    // (Shares of one row may lie in two launches: nobody waits for a part, the last one joins.)
+    for (int64_t i = 0; i < blocks; i += kKvMostBlocks) {
+        a.item0 = (int)i;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)std::min<int64_t>(blocks - i, kKvMostBlocks)), dim3(256), 0, stream, a);
+    }
     return hipGetLastError();
 }
 

@@ -1,5 +1,7 @@
 // Into, out of and inside a paged MXFP4 cache for gfx950: the store of new tokens (rotary positions and the cast of
 // arXiv 2503.13565, section 3.4.3, in one launch), the values back out, tokens moved together, pages copied.
+#include <algorithm>
+
 #include "cast_block.h"
 #include "common.h"
 #include "kv.h"
@@ -72,7 +74,7 @@ __device__ __forceinline__ void kv_put(const u32x4_t x, const KvSlot& to, bool t
 __global__ __launch_bounds__(256) void kv_append_halves_kernel(KvView c, KvBatch b, KvTensor k, KvTensor v, KvTensor q, KvTensor qo,
                                                                int q_heads, KvRope rope)
 {
-    const int t = blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
+    const int t = b.t0 + (int)blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
     const int half = c.nb * 2;                                         // groups of eight in half a head; a multiple of four
     const int head_all = (int)((unsigned)g / (unsigned)half), e = (g - head_all * half) * 8, e2 = e + half * 8;
     const bool live = head_all < q_heads + 2 * c.heads;                // the same for a whole quad
@@ -106,7 +108,7 @@ __global__ __launch_bounds__(256) void kv_append_halves_kernel(KvView c, KvBatch
 __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvBatch b, KvTensor k, KvTensor v, KvTensor q, KvTensor qo,
                                                         int q_heads, KvRope rope)
 {
-    const int t = blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
+    const int t = b.t0 + (int)blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
     const int per_head = c.nb * 4;
     const int head_all = g / per_head, e = (g - head_all * per_head) * 8;
     const bool live = head_all < q_heads + 2 * c.heads;                // the same for a whole quad (per_head is a multiple of four)
@@ -140,7 +142,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvView c, KvBatch b, KvT
 // for one that is read; they are not read again soon and go past the L2's order of use.
 __global__ __launch_bounds__(256) void kv_read_kernel(KvView c, KvBatch b, KvTensor k, KvTensor v)
 {
-    const int t = blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
+    const int t = b.t0 + (int)blockIdx.x, g = blockIdx.y * 256 + threadIdx.x;
     const int per_head = c.nb * 4;                                     // groups of eight elements
     const int head_all = (int)((unsigned)g / (unsigned)per_head), e = (g - head_all * per_head) * 8;
     const KvPlace at = kv_place(b, t);                                 // (with all lanes of the wave)
@@ -235,20 +237,24 @@ __global__ __launch_bounds__(256) void kv_copy_kernel(KvView c, const int32_t* s
     }
 }
 
-hipError_t launch_kv_append(const KvView& c, const KvBatch& b, const KvTensor& k, const KvTensor& v, const KvTensor& q,
+hipError_t launch_kv_append(const KvView& c, KvBatch b, const KvTensor& k, const KvTensor& v, const KvTensor& q,
                             const KvTensor& qo, int q_heads, const KvRope& rope, hipStream_t stream)
 {
     const bool halves = c.nb % 2 == 0 && (rope.dim == 0 || rope.dim == c.nb * 32);
     const int64_t groups = (int64_t)(q_heads + 2 * c.heads) * c.nb * (halves ? 2 : 4);
-    hipLaunchKernelGGL(halves ? kv_append_halves_kernel : kv_append_kernel, dim3((unsigned)b.tokens, (unsigned)((groups + 255) / 256)), dim3(256), 0, stream, c, b, k, v,
-                       q, qo, q_heads, rope);
+    for (; b.t0 < b.tokens; b.t0 += kKvMostBlocks)
+        hipLaunchKernelGGL(halves ? kv_append_halves_kernel : kv_append_kernel,
+                           dim3((unsigned)std::min(b.tokens - b.t0, kKvMostBlocks), (unsigned)((groups + 255) / 256)), dim3(256), 0, stream, c, b, k,
+                           v, q, qo, q_heads, rope);
     return hipGetLastError();
 }
 
-hipError_t launch_kv_read(const KvView& c, const KvBatch& b, const KvTensor& k, const KvTensor& v, hipStream_t stream)
+hipError_t launch_kv_read(const KvView& c, KvBatch b, const KvTensor& k, const KvTensor& v, hipStream_t stream)
 {
     const int64_t groups = (int64_t)2 * c.heads * c.nb * 4;
-    hipLaunchKernelGGL(kv_read_kernel, dim3((unsigned)b.tokens, (unsigned)((groups + 255) / 256)), dim3(256), 0, stream, c, b, k, v);
+    for (; b.t0 < b.tokens; b.t0 += kKvMostBlocks)
+        hipLaunchKernelGGL(kv_read_kernel, dim3((unsigned)std::min(b.tokens - b.t0, kKvMostBlocks), (unsigned)((groups + 255) / 256)), dim3(256), 0,
+                           stream, c, b, k, v);
     return hipGetLastError();
 }
 
@@ -269,8 +275,9 @@ hipError_t launch_kv_copy(const KvView& c, const int32_t* src, const int32_t* ds
     int64_t blocks = (pieces + 255) / 256;
     const int64_t most = 1024 / count + 1;
     blocks = blocks < most ? blocks : most;
-    hipLaunchKernelGGL(kv_copy_kernel, dim3((unsigned)count, (unsigned)blocks), dim3(256), 0, stream, c, src, dst, pitch, rows, n_rows, lens,
-                       add);
+    for (int64_t i = 0; i < count; i += kKvMostBlocks)              // (`rows` come with at most kKvMaxRows pairs)
+        hipLaunchKernelGGL(kv_copy_kernel, dim3((unsigned)std::min<int64_t>(count - i, kKvMostBlocks), (unsigned)blocks), dim3(256), 0, stream, c,
+                           src + i * pitch, dst + i * pitch, pitch, rows, n_rows, lens, add);
     return hipGetLastError();
 }
 
