@@ -263,7 +263,8 @@ typedef struct mxfp4_kv_cache {
  * A batch: `rows` sequences, their tables, lengths and new tokens.  The new tokens of sequence b are rows
  * starts[b] .. starts[b + 1] - 1 of the packed tensors [tokens][...] (starts: rows + 1 ascending numbers,
  * starts[0] = 0) and stand at the last positions of the sequence, lens[b] - n .. lens[b] - 1.  starts = NULL:
- * the same number each, tokens / rows (tokens must be a multiple of rows).  table, lens and starts are
+ * the same number each, tokens / rows (tokens must be a multiple of rows).  Tokens that no row has (before starts[0], from
+ * starts[rows] on) are stored nowhere and read as zeros; attention writes no result for them.  table, lens and starts are
  * device pointers; width is the number of entries of a table row.
  */
 typedef struct mxfp4_kv_rows {
@@ -317,7 +318,7 @@ int mxfp4_kv_read(const mxfp4_kv_cache* cache, const mxfp4_kv_rows* batch, const
 /*
  * Attention of the batch's new tokens over the cache:  out[t][h] = sum_j softmax_j(scale q[t][h] . k[j]) v[j] over the
  * positions j that token t sees, k and v of head h / (q_heads / heads).  FP32 sums and softmax, attention
- * weights rounded to BF16 before they meet the values, BF16 result.
+ * weights rounded to BF16 before they meet the values (the result's error is 1.2 to 1.4 times that of its own rounding), BF16 result.
  *   causal != 0   token i of a sequence, at position p, sees j <= p
  *   window > 0    and only j > p - window (any causal)
  *   tree          (device, [tokens], NULL: none) bit m of a token's word: it sees new token m of its

@@ -1,11 +1,13 @@
-// Attention over a paged MXFP4 cache for gfx950, few queries per key/value head: drafting (one token), verifying (a draft or
-// a draft tree), short pieces of prompts.
+// Attention over a paged MXFP4 cache for gfx950: drafting (one token), verifying (a draft or a draft tree), pieces of prompts and
+// whole ones.
 //
 //   out[t][h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(scale q[t][h] . k_j - m)
 //
-// in one pass over the keys with the running maximum m.  Bound by HBM: 17/16 bytes per element of the head dimension and token
-// (codes and scales of key and value).  The queries of all heads that share a key/value head, and all new tokens, are the 16
-// columns of v_mfma_f32_16x16x32_bf16 (QT times 16), so a cached token is read and decoded once for all of them:
+// in one pass over the keys with the running maximum m.  With few queries bound by HBM: 17/16 bytes per element of the head dimension
+// and token (codes and scales of key and value); with many by the vector unit, whose converts and softmax steps and the matrix
+// instructions take turns (5001 tokens of a prompt: vector 64 % of a SIMD's cycles, matrix 28 %).  The queries of all heads that share a
+// key/value head, and all new tokens, are the 16 columns of v_mfma_f32_16x16x32_bf16 (QT times 16), so a cached token is read and decoded
+// once for all of them:
 //   scores   S^T[token][query]  = K . Q^T      keys are the left operand, decoded in registers (kv_tile.h)
 //   values   O^T[element][query] += V^T . P^T   the scores leave the first product in the layout in which the second one takes
 //                                               them as its right operand: no LDS and no crossing of lanes in the loop
@@ -20,7 +22,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
 {
     typedef KvTile<NB, kPad> T;
     constexpr int NW = 4, kRows = 16 * QT, kEl = T::kEl, kChunks = T::kChunks;
-    constexpr int kDepth = QT == 1 ? 3 : 2;                            // tiles in flight: what the registers hold (one more spills: prompt 372 us, not 311)
+    constexpr int kDepth = QT == 1 ? 3 : 2;                            // tiles in flight: what the registers hold (a third spills: prompt 331 us, not 303)
     constexpr int kSlot = QT * NB * 512 + 48 * QT;                     // floats of a partial result
     constexpr int kJoin = kKvJoin, kFinal = 8192;                         // parts added at a time; where the counters of the last sums begin
     __shared__ __align__(16) float comb[NW][kEl][4][64];
@@ -91,7 +93,8 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
                     s[qt][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[qt][j], j ? s[qt][h] : f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
             }
         // Converts between the products, four for each operand: the matrix pipe works beside them in one wave's stream better than blocks of
-        // either do in two waves' (5001 tokens of a prompt: 311 us, 316 in the compiler's order).
+        // either do in two waves' (9 new tokens each of 16 rows of 16000, dim 128: 168 us, 171 in the compiler's order; 5001 tokens of a prompt
+        // 303 and 304; dim 64 within 1 %).
         __builtin_amdgcn_sched_group_barrier(0x2, 6, 0);
 #pragma unroll
         for (int i = 0; i < 2 * NB * QT; ++i) {
@@ -278,7 +281,7 @@ __global__ __launch_bounds__(256, NB <= 4 ? 2 : 1) void kv_attend_kernel(KvAtten
     // Parts of one row of keys: of every kJoin parts the workgroup that comes last adds them, of these the one that comes last
     // again, in the order of the parts whoever it is.  Nobody waits.  The parts go past the L2 (each die has its own) with coherent stores,
     // which have arrived when the wave's counter of stores is at zero, so that the count needs no write-back of a whole L2 in front of
-    // it: with __threadfence() in that place one row of 131071 tokens took 136 us, not 37.
+    // it: with __threadfence() in that place one row of 131071 tokens took 136 us, not 38.
     // Lanes without a query store and load as well, so that lines are whole and nothing branches (one token, 32 heads of their own, 2000
     // tokens: 10.4 us, 12.4 with those lanes left out).
     const float* parts = a.part + (int64_t)it.slot0 * kSlot;
@@ -392,8 +395,11 @@ static int most_query_tiles(int nb, int64_t queries) { return queries <= 16 || n
 
 // Two tiles decode a token once for both, one tile loads, combines and joins less in front of the first result: one where the
 // workgroups with one tile run at once and all of them read less than 4096 tokens for each compute unit, as far as the table can
-// tell the lengths (us with one and with two: 4 new tokens, 64 heads on 8, over 1000: 9.6 and 13.2, 4 rows over 16000: 30 and 34, over
-// 32000: 52 and 50, 16 rows over 16000: 95 and 80; prompts of 32 heads of their own, 100 tokens: 6.2 and 8.2, 1000: 39 and 31, 5001: 456 and 311).
+// tell the lengths: a table with room for more tokens than there are takes the rule past its border (us with one and with two: 4 new
+// tokens, 64 heads on 8, over 1000: 9.6 and 13.1, 4 rows over 16000: 30.3 and 33.4, 16 rows over 4000: 30.1 and 28.0, over 16000: 94 and 76; prompts of
+// 3000: 366 and 246, 5001: 454 and 303; dim 64, 9 tokens over 1000: 8.2 and 11.1, 16 rows of them over 16000: 49 and 42; dim 32 likewise 8.0 and 10.4,
+// 68 and 72).  Heads of 96 elements run two tiles with 11 registers in scratch memory, and gain by it all the same: 16 rows over 16000 92 and
+// 70, prompts of 3000 132 and 93.
 static int query_tiles(const KvAttend& a, const DeviceInfo& dev)
 {
     const int64_t queries = ((int64_t)a.b.tokens * a.group + a.b.rows - 1) / a.b.rows;

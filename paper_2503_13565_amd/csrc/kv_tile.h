@@ -72,18 +72,21 @@ __device__ __forceinline__ KvRow kv_row(const KvAttend& a, int b)
 // 2 target + (heads x tiles) workgroups.  Each finds its own share from the lengths, so that one launch fits any lengths, also those that
 // change between replays of a graph, and sequences of different lengths load the device evenly.  Only rows of two parts or more need
 // partial results: at most 4 target of them (U is summed in FP32, which all workgroups do alike; a few more for its rounding).
-// What the parts aim for (dim 128, us):
+// What the parts aim for (us; 64 query heads on 8 of dim 128 where nothing else is said, 16 on 2 of dim 256 with four times the rows; both sides
+// of every rule at six head sizes are in profiles/paged_cache_cutting.txt):
 //   as they are  rows whose longest ends no later than parts would, the joining (`joint` units' time) with them; and starts that descend
 //                somewhere: the rows then have more shares together than the launch has workgroups, and a row's parts would wait
-//                for some that never come, with their counter above zero
-//   one round    with few rows of one length, the shortest parts that `target` workgroups hold at once (16 rows of 32000 tokens, 64 query heads on 8:
-//                113; twice as many parts 118)
+//                for some that never come, with their counter above zero (56 rows of 4000 tokens: 54, 65 in parts; 60 of 8000: 102 and 113; dim
+//                256: 140 and 166.  Without the joining's units the rule misses all of these; with twice as many a row of 1000 takes 10.7, not 9.2)
+//   one round    with few rows of one length, the shortest parts that `target` workgroups hold at once (20 rows of 9000 tokens: 48, and 56 with a
+//                workgroup's share each; 24 of 16000: 95 and 109; dim 256, 40 of 20000: 139 and 153; 16 of 32000: 108 and 110)
 //   several      with many rows of different lengths, parts of half a workgroup's share, since parts of one length do not come out
-//                (64 rows of 500 to 16384 tokens: 85, not 87.5)
-//   short parts  (up to `brief` units) half of `target`, because joining costs more than it saves (4 rows of 16000 tokens: 22.9,
-//                not 24.3)
-//   a row alone  no more than the kKvJoin parts that are joined at a time, unless that leaves a part over four units
-//                (one row of 2000 tokens: 9.6, and 11.3 with parts of one unit); whole up to six units (32 heads, 500 tokens: 8.2, not 9.6)
+//                (64 rows of 500 to 16384 tokens: 82, not 86; dim 192: 116, not 123; no more than 1 % at dims 32, 64 and 256)
+//   short parts  (up to `brief` units) half of `target`, because joining costs more than it saves (4 rows of 16000 tokens: 22.7, not
+//                24.4; 4 heads of dim 192: 30, not 43; `brief` of 32: one row of 131071 41, not 37)
+//   a row alone  no more than the kKvJoin parts that are joined at a time, unless that leaves a part over four units (one row of 4000 tokens
+//                11.0, 12.1 with two units, of 16000 15.0, 17.7 with eight); whole up to six units (500 tokens 8.3, 9.4 in parts; 1000 9.2,
+//                11.0 whole)
 constexpr int kKvJoin = 8;
 template <int kUnit>
 __device__ __forceinline__ bool kv_find(const KvAttend& a, int item, int tile_rows, int brief, int joint, KvItem* out)
@@ -396,7 +399,10 @@ __device__ __forceinline__ bf16x8_t softmax_step(const f32x4_t* s, float scale, 
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         w[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale, off));
-    // rounded to BF16 (the type of the values' product; half a step, 2^-8 of a weight at most, and the weights' errors average out)
+    // rounded to BF16 (the type of the values' product; half a step, 2^-8 of a weight at most, and the weights' errors average out: the result is
+    // off by 2.0e-3 to 2.3e-3 of its norm, its own rounding alone by 1.65e-3).  What the rounding leaves of a weight as a second BF16 operand
+    // takes that back to 1.65e-3 and costs every row a second product: one token over 131071 39.7 us, not 38.4, 64 rows of 500 to 16384 88.5,
+    // not 85.4, 16 rows of 8000 38.4, not 33.9, pieces and prompts, which the vector unit bounds, 79.5, not 69 and 357, not 304.
     const bf16x8_t p = __builtin_bit_cast(bf16x8_t, (u32x4_t{f32_to_bf16_rne2(w[0], w[1]), f32_to_bf16_rne2(w[2], w[3]),
                                                              f32_to_bf16_rne2(w[4], w[5]), f32_to_bf16_rne2(w[6], w[7])}));
     if (wanted)
