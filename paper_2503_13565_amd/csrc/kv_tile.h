@@ -378,13 +378,20 @@ __device__ __forceinline__ int part_begin(int n, int s, int S)
 // as they are, for the logarithm, in which a single weight's rounding would show.  A NaN score makes `top` NaN (the maximum here is
 // the one that carries it on), which moves nothing, and a NaN weight, which makes the query's sums NaN.
 template <int kSums>
-__device__ __forceinline__ bf16x8_t softmax_step(const f32x4_t* s, float scale, bool wanted, float* m, f32x4_t* l, float* exact, f32x4_t* o)
+__device__ __forceinline__ bf16x8_t softmax_step(f32x4_t* s, float scale, bool wanted, float* m, f32x4_t* l, float* exact, f32x4_t* o)
 {
     float top = max_of_three(max_of_three(max_of_three(s[0][0], s[0][1], s[0][2]), s[0][3], s[1][0]), s[1][1], s[1][2]);
     top = max_of_rows(max_of_three(top, s[1][3], s[1][3]));
     // The sums move to a new maximum only when it is 2^8 above the old one: the weights then stay below 2^8, which FP32 sums and
-    // BF16 weights hold as well as weights up to 1.
-    if (__ballot((top - *m) * scale > 8.f || (*m == -INFINITY && top > -INFINITY))) {
+    // BF16 weights hold as well as weights up to 1.  (The first maximum is infinitely far above none.)
+    // A weight's exponent is (s - m) scale, with the difference first: it is exact next to the maximum.  s scale - m scale is one operation
+    // less, and the rounding of its second product stays in it: 2^-15 at most while that product is below 2^10, but a weight of 2^128 where
+    // it is 2^31.  Up to dim 128 (vector-bound with many queries: 303 us for 5001 tokens of a prompt, 310 with eight more operations) it is
+    // taken below 2^10, and past that the maximum leaves the scores in the rescaling's branch, so that the usual tile has no more blocks
+    // than before; the larger heads, where that costs 1 to 7 % and the operations nothing, take the difference always.
+    constexpr bool kFused = kSums <= 8;
+    float off = kFused && *m != -INFINITY ? -*m * scale : 0.f;
+    if (__ballot((top - *m) * scale > 8.f || fabsf(off) > 1024.f)) {
         const float now = top > *m ? top : *m;
         const float f = now == -INFINITY ? 1.f : exp2f((*m - now) * scale);
         *m = now;
@@ -393,12 +400,20 @@ __device__ __forceinline__ bf16x8_t softmax_step(const f32x4_t* s, float scale, 
 #pragma unroll
         for (int e = 0; e < kSums; ++e)
             o[e] *= f;
+        if constexpr (kFused) {
+            off = now == -INFINITY ? 0.f : -now * scale;
+            const float first = fabsf(off) > 1024.f ? now : 0.f;
+            off = fabsf(off) > 1024.f ? 0.f : off;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                s[i >> 2][i & 3] -= first;
+        }
     }
-    const float off = *m == -INFINITY ? 0.f : -*m * scale;
+    const float base = *m == -INFINITY ? 0.f : *m;
     float w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        w[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], scale, off));
+        w[i] = __builtin_amdgcn_exp2f(kFused ? fmaf(s[i >> 2][i & 3], scale, off) : (s[i >> 2][i & 3] - base) * scale);
     // rounded to BF16 (the type of the values' product; half a step, 2^-8 of a weight at most, and the weights' errors average out: the result is
     // off by 2.0e-3 to 2.3e-3 of its norm, its own rounding alone by 1.65e-3).  What the rounding leaves of a weight as a second BF16 operand
     // takes that back to 1.65e-3 and costs every row a second product: one token over 131071 39.7 us, not 38.4, 64 rows of 500 to 16384 88.5,
