@@ -94,7 +94,7 @@ class Decoder:
 
 
 def norm(x):
-    return (x.float() * torch.rsqrt(x.float().square().mean(-1, keepdim=True) + 1e-6)).to(torch.bfloat16)
+    return b.mxfp4_rms_norm(x).y
 
 
 def generate(prompt, tokens, drafts, seed=0):

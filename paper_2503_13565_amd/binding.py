@@ -37,6 +37,7 @@ EXPORTS = [
     "mxfp4_woq_gemm_t_workspace_bytes", "mxfp4_woq_gemm_t",
     "mxfp4_kv_append", "mxfp4_kv_read", "mxfp4_kv_attention_workspace_bytes", "mxfp4_kv_attention",
     "mxfp4_kv_fork", "mxfp4_kv_extend", "mxfp4_kv_release", "mxfp4_kv_compact", "mxfp4_kv_copy_pages",
+    "mxfp4_rms_norm", "mxfp4_w4a8_gemm", "mxfp4_lora_workspace_bytes", "mxfp4_lora",
     "mxfp4_tile_repack_q_bytes", "mxfp4_tile_repack_s_bytes", "mxfp4_tile_repack", "mxfp4_woq_gemm_tiled",
     "mxfp4_woq_gemm_tiled_ws",
     "mxfp4_woq_gemm_tiled_argmax", "mxfp4_woq_gemm_tiled_verify", "mxfp4_woq_gemm_tiled_fused",
@@ -76,6 +77,19 @@ _kv = None
 def _kv_host():
     load()
     return _kv
+
+
+class _Layer:
+    """The extension's calls of what surrounds a layer's products, in the same way."""
+    rms_norm = w4a8 = lora = staticmethod(lambda *args: None)
+
+
+_layer = None
+
+
+def _layer_host():
+    load()
+    return _layer
 
 
 class GemmDesc(ctypes.Structure):
@@ -138,7 +152,7 @@ class Mxfp4Error(RuntimeError):
 
 def load() -> ctypes.CDLL:
     """Load the HIP library (torch first, so that both share one HIP runtime)."""
-    global _lib, _product, _verify, _cast, _kv
+    global _lib, _product, _verify, _cast, _kv, _layer
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -251,6 +265,14 @@ def load() -> ctypes.CDLL:
     lib.mxfp4_kv_copy_pages.argtypes = [ref(KvCacheDesc), vp, vp, i64, vp]
     for name in ("append", "read", "attention", "fork", "extend", "release", "compact", "copy_pages"):
         getattr(lib, "mxfp4_kv_" + name).restype = i32
+    lib.mxfp4_rms_norm.argtypes = [vp, i64, i64, i64, vp, i64, vp, ctypes.c_float, vp, i64, vp, i64, vp, vp, vp]
+    lib.mxfp4_rms_norm.restype = i32
+    lib.mxfp4_w4a8_gemm.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, vp, i64, vp, i64, vp]
+    lib.mxfp4_w4a8_gemm.restype = i32
+    lib.mxfp4_lora_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.mxfp4_lora_workspace_bytes.restype = sz
+    lib.mxfp4_lora.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, i64, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    lib.mxfp4_lora.restype = i32
     lib.mxfp4_diag_stream_read.argtypes = [vp, sz, vp, vp]
     lib.mxfp4_diag_stream_copy.argtypes = [vp, vp, sz, vp]
     for name in ("mxfp4_direct_cast", "mxfp4_direct_cast_bits", "mxfp4_dequant", "mxfp4_dequant_hwcvt", "mxfp4_woq_gemm",
@@ -259,7 +281,7 @@ def load() -> ctypes.CDLL:
         getattr(lib, name).restype = i32
     lib.mxfp4_last_error.restype = ctypes.c_char_p
     lib.mxfp4_version.restype = ctypes.c_char_p
-    _product, _verify, _cast, _kv = _host_calls()
+    _product, _verify, _cast, _kv, _layer = _host_calls()
     _lib = lib
     return lib
 
@@ -274,12 +296,15 @@ def _host_calls():
     except ImportError as e:
         warnings.warn("the extension module _host cannot be used (%s): calls go through ctypes, which takes more host time; "
                       "build it with `python -m paper_2503_13565_amd.build`" % e, RuntimeWarning, stacklevel=3)
-        return (*(lambda *args: None,) * 3, _Kv)
+        return (*(lambda *args: None,) * 3, _Kv, _Layer)
     _host.on_failure(_check)
 
     class kv(_Kv):
         append, read, attention, pages, compact = _host.kv_append, _host.kv_read, _host.kv_attention, _host.kv_pages, _host.kv_compact
-    return _host.product, _host.verify, _host.cast, kv
+
+    class layer(_Layer):
+        rms_norm, w4a8, lora = _host.rms_norm, _host.w4a8, _host.lora
+    return _host.product, _host.verify, _host.cast, kv, layer
 
 
 def _check(rc: int) -> None:
@@ -1304,3 +1329,133 @@ def mxfp4_kv_copy_pages(cache: KvCache, src: torch.Tensor, dst: torch.Tensor) ->
     c, n = _kv_cache_desc(cache), _kv_two_lists(src, dst, "src and dst", cache.kq.device)
     with _on(cache.kq.device):
         _check(load().mxfp4_kv_copy_pages(c, _ptr(src), _ptr(dst), n, _stream()))
+
+
+# ---- what surrounds the products of a layer: norm, products of 8-bit rows, adapters of many requests ----------------------------------
+
+
+class Normed(NamedTuple):
+    """What a norm leaves: ``y`` BF16, ``total`` (the sum with the residual) BF16, ``q8`` and ``s`` (``y`` in 8 bits); None for what
+    was not asked for."""
+    y: Optional[torch.Tensor]
+    total: Optional[torch.Tensor]
+    q8: Optional[torch.Tensor]
+    s: Optional[torch.Tensor]
+
+
+_NORM_OUT = {"bf16": (True, False), "e4m3": (False, True), "both": (True, True)}
+
+
+def _row_stride(t: Optional[torch.Tensor], what: str, device, *shape) -> int:
+    """Checks a BF16 tensor of rows; its row stride (0: none given)."""
+    if t is None:
+        return 0
+    if t.dtype != torch.bfloat16 or t.dim() != 2 or t.device != device or tuple(t.shape) != shape or (shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be a BF16 tensor %r with a contiguous last dimension, on the device of the rows" % (what, shape))
+    return t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _whole(t: Optional[torch.Tensor], what: str, dtype, device, *shape) -> None:
+    if t is not None and (t.dtype != dtype or t.device != device or tuple(t.shape) != shape or not t.is_contiguous()):
+        raise ValueError("%s must be a contiguous %s tensor %r on the device of the rows" % (what, dtype, shape))
+
+
+def mxfp4_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                   out: str = "bf16", y: Optional[torch.Tensor] = None, total: Optional[torch.Tensor] = None) -> Normed:
+    """Root-mean-square norm of BF16 rows ``x [M, K]``, of ``x + residual`` where a residual is given (that sum is ``total``).  ``out``: the
+    normed rows in "bf16", in 8 bits ("e4m3": codes and scale bytes for :func:`mxfp4_w4a8_gemm`), or "both".  ``y`` and ``total`` may be
+    given; each may be ``x`` or ``residual`` itself."""
+    if out not in _NORM_OUT:
+        raise ValueError("out must be one of %s" % ", ".join(_NORM_OUT))
+    bf16, e4m3 = _NORM_OUT[out]
+    if y is None and total is None:
+        got = _layer_host().rms_norm(x, weight, residual, eps, bf16, e4m3)
+        if got is not None:
+            return Normed._make(got)
+    _dev(x)
+    if x.dtype != torch.bfloat16 or x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1):
+        raise ValueError("x must be a 2-D BF16 tensor with a contiguous last dimension")
+    if y is not None and not bf16:
+        raise ValueError("y is given, but out is %r" % out)
+    if total is not None and residual is None:
+        raise ValueError("total is given without a residual")
+    m, k = x.shape
+    ldx, ldr = _row_stride(x, "x", x.device, m, k), _row_stride(residual, "residual", x.device, m, k)
+    _whole(weight, "weight", torch.bfloat16, x.device, k)
+    if bf16 and y is None:
+        y = torch.empty((m, k), dtype=torch.bfloat16, device=x.device)
+    if residual is not None and total is None:
+        total = torch.empty((m, k), dtype=torch.bfloat16, device=x.device)
+    q8 = torch.empty((m, k), dtype=torch.uint8, device=x.device) if e4m3 else None
+    s = torch.empty((m, k // 32), dtype=torch.uint8, device=x.device) if e4m3 else None
+    ldy, lds = _row_stride(y, "y", x.device, m, k), _row_stride(total, "total", x.device, m, k)
+    if y is not None and total is not None and y.data_ptr() == total.data_ptr() and m:
+        raise ValueError("y and total must not be the same tensor")
+    with _on(x.device):
+        _check(load().mxfp4_rms_norm(_ptr(x), m, k, ldx, _ptr(residual), ldr, _ptr(weight), float(eps), _ptr(total), lds, _ptr(y), ldy,
+                                     _ptr(q8), _ptr(s), _stream()))
+    return Normed(y, total, q8, s)
+
+
+def mxfp4_w4a8_gemm(x8: torch.Tensor, xs: torch.Tensor, q: torch.Tensor, s: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                    act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The product of 8-bit rows (``x8 [M, K]``, ``xs [M, K/32]`` from :func:`mxfp4_rms_norm` or :func:`mxfp4_e4m3_direct_cast`) with MXFP4
+    weights, with bias, gate and residual add behind it as in :func:`mxfp4_woq_gemm_fused`; ``residual`` may be ``y`` itself."""
+    if y is None:
+        got = _layer_host().w4a8(x8, xs, q, s, bias, act, residual)
+        if got is not None:
+            return got
+    _dev(x8)
+    if x8.dim() != 2 or q.dim() != 2:
+        raise ValueError("x8 and q must be 2-D")
+    (m, k), n, dev = x8.shape, q.shape[0], x8.device
+    for t, what, shape in ((x8, "x8", (m, k)), (xs, "xs", (m, k // 32)), (q, "q", (n, k // 2)), (s, "s", (n, k // 32))):
+        _whole(t, what, torch.uint8, dev, *shape)
+    c = n // 2 if act == ACT_SWIGLU else n
+    _whole(bias, "bias", torch.bfloat16, dev, n)
+    ldr = _row_stride(residual, "residual", dev, m, c)
+    if y is None:
+        y = torch.empty((m, c), dtype=torch.bfloat16, device=dev)
+    ldy = _row_stride(y, "y", dev, m, c)
+    if residual is not None and residual.data_ptr() == y.data_ptr() and ldr != ldy:
+        raise ValueError("residual is y with another row stride")
+    with _on(dev):
+        _check(load().mxfp4_w4a8_gemm(_ptr(x8), _ptr(xs), m, _ptr(q), _ptr(s), n, k, _ptr(bias), act, _ptr(residual), ldr, _ptr(y), ldy,
+                                      _stream()))
+    return y
+
+
+def mxfp4_lora_workspace_bytes(m: int, k: int, rank: int) -> int:
+    return int(load().mxfp4_lora_workspace_bytes(m, k, rank))
+
+
+def mxfp4_lora(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, ids: torch.Tensor, base: Optional[torch.Tensor] = None,
+               scales: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None
+               ) -> torch.Tensor:
+    """Adapters of many requests beside a shared projection: ``y[m] = base[m] + scales[i] * b[i] @ (a[i] @ x[m])`` with ``i = ids[m]``;
+    rows with an id outside ``[0, adapters)`` get ``base[m]``.  ``a [adapters, R, K]``, ``b [adapters, N, R]`` BF16, ``ids`` int32 ``[M]``;
+    ``y`` may be ``base`` itself."""
+    if y is None and workspace is None:
+        got = _layer_host().lora(x, a, b, ids, base, scales)
+        if got is not None:
+            return got
+    _dev(x)
+    if x.dtype != torch.bfloat16 or x.dim() != 2 or a.dim() != 3 or b.dim() != 3:
+        raise ValueError("x must be a 2-D BF16 tensor, a and b 3-D ones")
+    (m, k), (many, rank, _), n, dev = x.shape, a.shape, b.shape[1], x.device
+    ldx, ldb = _row_stride(x, "x", dev, m, k), _row_stride(base, "base", dev, m, n)
+    _whole(a, "a", torch.bfloat16, dev, many, rank, k)
+    _whole(b, "b", torch.bfloat16, dev, many, n, rank)
+    _whole(ids, "ids", torch.int32, dev, m)
+    _whole(scales, "scales", torch.float32, dev, many)
+    if y is None:
+        y = torch.empty((m, n), dtype=torch.bfloat16, device=dev)
+    ldy = _row_stride(y, "y", dev, m, n)
+    if workspace is None:
+        workspace = torch.empty((mxfp4_lora_workspace_bytes(m, k, rank),), dtype=torch.uint8, device=dev)
+    elif workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the device of x")
+    with _on(dev):
+        _check(load().mxfp4_lora(_ptr(x), m, ldx, _ptr(a), _ptr(b), many, rank, n, k, _ptr(ids), _ptr(scales), _ptr(base), ldb, _ptr(y), ldy,
+                                 _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+    return y

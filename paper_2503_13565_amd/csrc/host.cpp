@@ -253,6 +253,7 @@ PyMODINIT_FUNC PyInit__host()
 {
     PyObject* module = PyModule_Create(&kModule);
     if (module && (PyModule_AddFunctions(module, mxfp4_host::kv_methods) < 0 ||
+                   PyModule_AddFunctions(module, mxfp4_host::layer_methods) < 0 ||
                    PyModule_AddStringConstant(module, "torch_version", MXFP4_TORCH_VERSION) < 0)) {
         Py_DECREF(module);
         return nullptr;

@@ -1,4 +1,4 @@
-// What the calls of the extension module share (host.cpp, host_kv.cpp): how a Python object becomes memory and sizes, how new tensors
+// What the calls of the extension module share (host.cpp, host_kv.cpp, host_layer.cpp): how a Python object becomes memory and sizes, how new tensors
 // are made, how a status becomes a result or an error.
 #pragma once
 
@@ -89,7 +89,8 @@ inline PyObject* wrap_list(const at::Tensor* t, int count)
 inline PyObject* wrap_three(const at::Tensor* t) { return wrap_list(t, 3); }
 inline PyObject* wrap_two(const at::Tensor* t) { return wrap_list(t, 2); }
 
-// The module's functions that live in host_kv.cpp.
+// The module's functions that live in host_kv.cpp and host_layer.cpp.
 extern PyMethodDef kv_methods[];
+extern PyMethodDef layer_methods[];
 
 }  // namespace mxfp4_host

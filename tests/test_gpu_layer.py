@@ -1,0 +1,334 @@
+"""What surrounds a layer's products on the GPU against the definitions in 64 bits (layer_plain.py)."""
+import pytest
+import torch
+
+import layer_plain as plain
+from paper_2503_13565_amd import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+INF, NAN = float("inf"), float("nan")
+
+
+def _gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def _bf16(shape, seed, scale=1.0, large=20.0):
+    x = torch.randn(shape, generator=_gen(seed)) * scale
+    if x.shape[-1] > 8:
+        x[..., 3] *= large
+    return x.to(torch.bfloat16).to(DEV)
+
+
+def _wide(t, extra):
+    """The same rows with `extra` more columns of NaN behind each."""
+    got = torch.full((t.shape[0], t.shape[1] + extra), NAN, dtype=t.dtype, device=t.device)
+    got[:, : t.shape[1]] = t
+    return got[:, : t.shape[1]]
+
+
+# ---- the norm ---------------------------------------------------------------------------------------------------------
+
+def _check_norm(x, w, r, eps, got):
+    y, y_off, h, h_off = plain.norm(x, r, w, eps)
+    if got.y is not None:
+        plain.near(got.y, y, y_off, "y")
+    assert (got.total is None) == (r is None)
+    if r is not None:
+        plain.near(got.total, h, h_off, "sum")
+
+
+@pytest.mark.parametrize("m,k", [(1, 8), (3, 24), (5, 32), (37, 128), (1, 136), (18, 512), (7, 520), (5, 1024), (4, 2048), (3, 2056), (1, 4096), (9, 4096),
+                                 (259, 4096), (2, 5120), (3, 8192), (2, 8200), (2, 11008), (1, 16384), (2, 16392), (1, 65536), (700, 256), (300, 1376)])
+@pytest.mark.parametrize("residual,weight", [(False, True), (True, True), (True, False)])
+def test_norm(m, k, residual, weight):
+    x = _bf16((m, k), m + k)
+    r = _bf16((m, k), m + k + 1, 0.3) if residual else None
+    w = _bf16((k,), m + k + 2) if weight else None
+    got = binding.mxfp4_rms_norm(x, w, residual=r, eps=1e-5, out="bf16")
+    _check_norm(x, w, r, 1e-5, got)
+    if k % 32:
+        with pytest.raises(binding.Mxfp4Error, match="32"):
+            binding.mxfp4_rms_norm(x, w, residual=r, eps=1e-5, out="e4m3")
+        return
+    for out in ("both", "e4m3"):
+        eight = binding.mxfp4_rms_norm(x, w, residual=r, eps=1e-5, out=out)
+        code, scale = binding.mxfp4_e4m3_direct_cast(got.y)
+        assert torch.equal(eight.q8, code) and torch.equal(eight.s, scale), out
+        assert out == "e4m3" or torch.equal(eight.y, got.y)
+        assert r is None or torch.equal(eight.total, got.total)
+
+
+@pytest.mark.parametrize("m,k", [(3, 64), (6, 4096), (2, 12288)])
+def test_norm_strides_and_places(m, k):
+    x, r, w = _bf16((m, k), 1), _bf16((m, k), 2), _bf16((k,), 3)
+    want = binding.mxfp4_rms_norm(x, w, residual=r, eps=1e-5)
+    xs, rs = _wide(x, 8), _wide(r, 24)
+    got = binding.mxfp4_rms_norm(xs, w, residual=rs, eps=1e-5)
+    assert torch.equal(got.y, want.y) and torch.equal(got.total, want.total)
+    y, total = _wide(torch.zeros_like(x), 16), _wide(torch.zeros_like(x), 40)
+    got = binding.mxfp4_rms_norm(xs, w, residual=rs, eps=1e-5, y=y, total=total)
+    assert got.y is y and got.total is total and torch.equal(y, want.y) and torch.equal(total, want.total)
+    assert bool(torch.isnan(y._base[:, k:]).all()) and bool(torch.isnan(total._base[:, k:]).all())
+    for a, b in ((0, 1), (1, 0)):                               # in the places of the inputs
+        both = [x.clone(), r.clone()]
+        binding.mxfp4_rms_norm(both[0], w, residual=both[1], eps=1e-5, y=both[a], total=both[b])
+        assert torch.equal(both[a], want.y) and torch.equal(both[b], want.total)
+    with pytest.raises(ValueError, match="same"):
+        binding.mxfp4_rms_norm(x, w, residual=r, y=y, total=y)
+    with pytest.raises(ValueError, match="without a residual"):
+        binding.mxfp4_rms_norm(x, w, total=total)
+    with pytest.raises(ValueError, match="residual"):
+        binding.mxfp4_rms_norm(x, w, residual=r[:, : k - 8])
+    with pytest.raises(ValueError, match="weight"):
+        binding.mxfp4_rms_norm(x, w.float())
+
+
+@pytest.mark.parametrize("k", [64, 512, 4096, 20480])
+def test_norm_of_any_finite_row(k):
+    """Squares beyond FP32 on both sides, a sum beyond it, zeros, rows whose elements lie far apart."""
+    x, r = _bf16((8, k), 5).cpu(), torch.zeros((8, k), dtype=torch.bfloat16)
+    x[0] *= 2.0 ** 100
+    x[1] *= 2.0 ** -80
+    x[2] = torch.where(torch.arange(k) % 2 == 0, 3.0e38, -1.0e38)
+    r[2] = torch.where(torch.arange(k) % 2 == 0, 3.0e38, 2.0e38)
+    x[3] = 0
+    x[4] *= 2.0 ** -120
+    x[5, 1:] = 0
+    x[5, 0] = 1.5 * 2.0 ** 127
+    x[6, ::3] *= 2.0 ** 90
+    x, r = x.to(DEV), r.to(DEV)
+    for eps in (1e-5, 1e-30):
+        got = binding.mxfp4_rms_norm(x, None, residual=r, eps=eps)
+        y, y_off, h, h_off = plain.norm(x, r, None, eps)
+        h = torch.where(h.abs() > 3.39e38, torch.sign(h) * INF, h)      # (what BF16 cannot hold)
+        plain.near(got.y, y, y_off, "y")
+        plain.near(got.total, h, torch.where(h.isinf(), 0.0, h_off), "sum")
+
+
+def test_norm_of_rows_that_are_not_finite():
+    x = _bf16((4, 4096), 6).cpu()
+    x[0, 7], x[1, 9], x[2, 11] = NAN, INF, -INF
+    got = binding.mxfp4_rms_norm(x.to(DEV), None, out="both")
+    y, off, _, _ = plain.norm(x, None, None, 1e-6)
+    plain.near(got.y, y, off)
+    assert bool(got.y[0].isnan().all()) and int(got.y[1].isnan().sum()) == 1 and not bool(got.y[3].isnan().any())
+    assert bool((got.s[0] == 255).all()) and int((got.s[1] == 255).sum()) == 1 and int((got.s[3] == 255).sum()) == 0
+
+
+# ---- the product ------------------------------------------------------------------------------------------------------
+
+def _weights(n, k, seed):
+    return binding.mxfp4_direct_cast(_bf16((n, k), seed, 0.05, 4.0))
+
+
+def _eight(m, k, seed):
+    return binding.mxfp4_e4m3_direct_cast(_bf16((m, k), seed))
+
+
+@pytest.mark.parametrize("m,n,k", [
+    (1, 1, 32), (1, 5, 64), (2, 16, 96), (1, 33, 128), (3, 130, 160), (1, 256, 512), (5, 100, 544), (16, 64, 1024), (17, 48, 1376), (9, 512, 2048), (1, 4096, 4096),
+    (31, 97, 640), (33, 200, 384), (64, 64, 256), (65, 300, 4096), (96, 66, 1056), (128, 128, 512), (129, 257, 768), (200, 1000, 224), (255, 512, 2752),
+    (256, 256, 1152), (257, 514, 896), (300, 768, 4128), (511, 270, 1408), (520, 4096, 512), (700, 1030, 1280)])
+@pytest.mark.parametrize("more", ["", "bias residual", "gate", "bias gate residual"])
+def test_product(m, n, k, more):
+    if "gate" in more:
+        n += n % 2
+    x8, xs = _eight(m, k, m + n + k)
+    q, s = _weights(n, k, m + n + k + 1)
+    c = n // 2 if "gate" in more else n
+    bias = _bf16((n,), 3) if "bias" in more else None
+    residual = _bf16((m, c), 4) if "residual" in more else None
+    act = binding.ACT_SWIGLU if "gate" in more else binding.ACT_NONE
+    y = binding.mxfp4_w4a8_gemm(x8, xs, q, s, bias=bias, act=act, residual=residual)
+    want, off = plain.product(x8, xs, q, s, bias, "gate" in more, residual)
+    plain.near(y, want, off)
+    again = binding.mxfp4_w4a8_gemm(x8, xs, q, s, bias=bias, act=act, residual=residual)
+    assert torch.equal(y, again)
+
+
+@pytest.mark.parametrize("m,n,k", [(3, 40, 128), (40, 90, 1024), (300, 514, 640)])
+def test_product_strides_and_places(m, n, k):
+    x8, xs = _eight(m, k, 1)
+    q, s = _weights(n, k, 2)
+    r = _bf16((m, n), 3)
+    want = binding.mxfp4_w4a8_gemm(x8, xs, q, s, residual=r)
+    for extra in (8, 3):                                        # (3: rows at odd addresses)
+        y, wide = _wide(torch.zeros_like(r), extra), _wide(r, extra + 2)
+        assert torch.equal(binding.mxfp4_w4a8_gemm(x8, xs, q, s, residual=wide, y=y), want)
+        assert bool(torch.isnan(y._base[:, n:]).all())
+    y = r.clone()
+    binding.mxfp4_w4a8_gemm(x8, xs, q, s, residual=y, y=y)
+    assert torch.equal(y, want)
+    with pytest.raises(ValueError, match="xs"):
+        binding.mxfp4_w4a8_gemm(x8, xs[:, :-1], q, s)
+    with pytest.raises(ValueError, match="q must"):
+        binding.mxfp4_w4a8_gemm(x8, xs, q[:, :-1], s)
+    with pytest.raises(binding.Mxfp4Error, match="act"):
+        binding.mxfp4_w4a8_gemm(x8, xs, q, s, act=5)
+
+
+@pytest.mark.parametrize("m,n,k", [(2, 48, 160), (20, 70, 512), (150, 300, 1024), (300, 320, 512)])
+def test_product_of_every_code_and_scale(m, n, k):
+    """All codes, NaN ones among them, and scale bytes from end to end: what meets a NaN is NaN, nothing else is."""
+    gen = _gen(7)
+    x8 = torch.randint(0, 256, (m, k), generator=gen, dtype=torch.uint8)
+    x8[(x8 & 127) == 127] = 3
+    xs = torch.randint(100, 150, (m, k // 32), generator=gen, dtype=torch.uint8)
+    q = torch.randint(0, 256, (n, k // 2), generator=gen, dtype=torch.uint8)
+    s = torch.randint(100, 150, (n, k // 32), generator=gen, dtype=torch.uint8)
+    x8[m // 2, 5], xs[0, 1], s[n // 3, k // 32 - 1] = 127, 255, 255
+    xs[m - 1], s[n - 1] = 20, 195                               # (products of 2^118 at most: no sum leaves FP32)
+    xs[1 % m, 0], s[0] = 160, 40
+    y = binding.mxfp4_w4a8_gemm(x8.to(DEV), xs.to(DEV), q.to(DEV), s.to(DEV))
+    plain.near(y, *plain.product(x8, xs, q, s))
+
+
+@pytest.mark.parametrize("k", [96, 128, 640])
+def test_product_of_the_outermost_scales(k):
+    scales = [0, 1, 64, 127, 190, 253, 254]
+    m = n = len(scales)
+    x8, q = torch.zeros((m, k), dtype=torch.uint8), torch.zeros((n, k // 2), dtype=torch.uint8)
+    x8[:, k - 32], q[:, k // 2 - 16] = 0x38, 0x2                # 1 and 1
+    xs = torch.tensor(scales, dtype=torch.uint8)[:, None].repeat(1, k // 32)
+    y = binding.mxfp4_w4a8_gemm(x8.to(DEV), xs.to(DEV), q.to(DEV), xs.to(DEV)).double().cpu()
+    at = torch.tensor(scales, dtype=torch.float64) - 127
+    want = torch.pow(2.0, at[:, None] + at[None])
+    want[want >= 2.0 ** 128] = INF
+    plain.near(y, want, torch.where(want.isinf(), 0.0, want * plain.ROUND + plain.TINY))
+
+
+def test_product_counts_positions_exactly():
+    """One element of a row against one of a weight row: every pair of the same position, and no other, gives its product."""
+    k = 288
+    x8, xs = torch.zeros((k, k), dtype=torch.uint8), torch.full((k, k // 32), 127, dtype=torch.uint8)
+    x8[torch.arange(k), torch.arange(k)] = 0x38                 # 1
+    q, s = torch.zeros((k, k // 2), dtype=torch.uint8), torch.full((k, k // 32), 127, dtype=torch.uint8)
+    for i in range(k):
+        q[i, i // 2] = 0x4 << (4 * (i % 2))                     # 2
+    for rows in (5, 40, k):
+        y = binding.mxfp4_w4a8_gemm(x8[:rows].to(DEV), xs[:rows].to(DEV), q.to(DEV), s.to(DEV))
+        assert torch.equal(y.float().cpu(), 2 * torch.eye(k)[:rows])
+
+
+# ---- adapters ---------------------------------------------------------------------------------------------------------
+
+def _stack(many, rank, n, k, seed):
+    return _bf16((many, rank, k), seed, k ** -0.5, 1.0), _bf16((many, n, rank), seed + 1, 1.0, 1.0), torch.rand(many, generator=_gen(seed + 2)).to(DEV)
+
+
+def _ids(m, many, how, seed):
+    if how == "mixed":
+        return torch.randint(-2, many + 2, (m,), generator=_gen(seed), dtype=torch.int32).to(DEV)
+    if how == "runs":
+        return (torch.arange(m, dtype=torch.int32) * (many + 1) // m - 1).to(DEV)
+    return torch.full((m,), {"one": many - 1, "none": -1}[how], dtype=torch.int32, device=DEV)
+
+
+@pytest.mark.parametrize("m,n,k,rank,many", [
+    (1, 8, 8, 8, 1), (1, 4096, 4096, 16, 3), (2, 24, 40, 8, 5), (15, 264, 128, 24, 40), (16, 512, 1000, 32, 7), (17, 72, 4096, 64, 2), (33, 1032, 520, 128, 9),
+    (100, 96, 2056, 16, 64), (130, 2048, 256, 40, 12), (511, 128, 264, 8, 30), (512, 264, 128, 16, 5), (513, 88, 1032, 32, 90), (700, 640, 512, 64, 6), (1025, 72, 264, 120, 3)])
+@pytest.mark.parametrize("how", ["mixed", "runs", "one", "none"])
+def test_adapters(m, n, k, rank, many, how):
+    x, base = _bf16((m, k), 1), _bf16((m, n), 2)
+    a, b, scales = _stack(many, rank, n, k, m)
+    ids = _ids(m, many, how, m + n)
+    y = binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales)
+    plain.near(y, *plain.adapters(x, a, b, ids, base, scales))
+    own = base.clone()
+    assert binding.mxfp4_lora(x, a, b, ids, base=own, scales=scales, y=own) is own and torch.equal(own, y)
+    if how == "mixed":
+        plain.near(binding.mxfp4_lora(x, a, b, ids), *plain.adapters(x, a, b, ids))
+
+
+@pytest.mark.parametrize("m", [20, 600])
+def test_adapters_of_others_do_not_reach_a_row(m):
+    n, k, rank, many = 200, 320, 24, 6
+    x, base = _bf16((m, k), 3), _bf16((m, n), 4)
+    a, b, scales = _stack(many, rank, n, k, 5)
+    ids = _ids(m, many - 2, "mixed", 6)                         # (the last two are asked for now and then)
+    want = binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales)
+    a[1, 3, 5], b[2, 7, 2], b[3] = NAN, INF, NAN
+    x[4] = NAN
+    got = binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales)
+    clean = ~torch.isin(ids, torch.tensor([1, 2, 3], dtype=torch.int32, device=DEV))
+    clean[4] = bool(ids[4] < 0) or bool(ids[4] >= many)
+    assert torch.equal(got[clean], want[clean]) and bool(got[~clean].isnan().any())
+    plain.near(got[ids == 1], torch.full((int((ids == 1).sum()), n), NAN, dtype=torch.float64), torch.zeros(1))
+
+
+def test_adapters_strides():
+    m, n, k = 70, 136, 264
+    x, base = _bf16((m, k), 3), _bf16((m, n), 4)
+    a, b, scales = _stack(4, 16, n, k, 5)
+    ids = _ids(m, 4, "mixed", 6)
+    want = binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales)
+    y = _wide(torch.zeros_like(base), 8)
+    ws = torch.full((binding.mxfp4_lora_workspace_bytes(m, k, 16),), 255, dtype=torch.uint8, device=DEV)
+    binding.mxfp4_lora(_wide(x, 8), a, b, ids, base=_wide(base, 16), scales=scales, y=y, workspace=ws)
+    assert torch.equal(y, want) and bool(torch.isnan(y._base[:, n:]).all())
+    wide = _wide(base, 24)                                      # the columns of one projection of a fused output, in place
+    binding.mxfp4_lora(x, a, b, ids, base=wide, scales=scales, y=wide)
+    assert torch.equal(wide, want) and bool(torch.isnan(wide._base[:, n:]).all())
+    with pytest.raises(ValueError, match="ids"):
+        binding.mxfp4_lora(x, a, b, ids.long(), base=base)
+    with pytest.raises(ValueError, match="b must"):
+        binding.mxfp4_lora(x, a, b[:2], ids, base=base)
+    with pytest.raises(binding.Mxfp4Error, match="workspace"):
+        binding.mxfp4_lora(x, a, b, ids, base=base, workspace=ws[:64])
+
+
+# ---- together ---------------------------------------------------------------------------------------------------------
+
+def _layer(x, r, w, q, s, a, b, ids, scales):
+    n = binding.mxfp4_rms_norm(x, w, residual=r, out="both")
+    y = binding.mxfp4_w4a8_gemm(n.q8, n.s, q, s)
+    return n, binding.mxfp4_lora(n.y, a, b, ids, base=y, scales=scales, y=y)
+
+
+@pytest.mark.parametrize("m", [1, 5, 70, 600])
+def test_a_projection_of_a_layer(m):
+    k, n, many = 1024, 1536, 5
+    x, r, w = _bf16((m, k), 1), _bf16((m, k), 2, 0.2), _bf16((k,), 3)
+    q, s = _weights(n, k, 4)
+    a, b, scales = _stack(many, 16, n, k, 5)
+    ids = _ids(m, many, "mixed", 6)
+    got, y = _layer(x, r, w, q, s, a, b, ids, scales)
+    _check_norm(x, w, r, 1e-6, got)
+    base = binding.mxfp4_w4a8_gemm(got.q8, got.s, q, s)
+    plain.near(base, *plain.product(got.q8, got.s, q, s))
+    plain.near(y, *plain.adapters(got.y, a, b, ids, base, scales))
+
+
+@pytest.mark.parametrize("m", [1, 40, 530])
+def test_streams_and_graphs(m):
+    """On another stream than the current one of the tensors' making, and as a captured graph that is replayed with new inputs between
+    eager calls of the same."""
+    k, n, many = 512, 768, 4
+    q, s = _weights(n, k, 1)
+    a, b, scales = _stack(many, 32, n, k, 2)
+    w = _bf16((k,), 3)
+    inputs = [(_bf16((m, k), 10 + i), _bf16((m, k), 20 + i), _ids(m, many, "mixed", 30 + i)) for i in range(4)]
+    want = [_layer(x, r, w, q, s, a, b, ids, scales)[1] for x, r, ids in inputs]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = [_layer(x, r, w, q, s, a, b, ids, scales)[1] for x, r, ids in inputs]
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(g, v) for g, v in zip(got, want))
+    x, r, ids = (t.clone() for t in inputs[0])
+    graphs = []
+    for _ in range(2):                                          # two graphs that are replayed in turn
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = _layer(x, r, w, q, s, a, b, ids, scales)[1]
+        graphs.append((g, out))
+    for i in (0, 1, 2, 3, 1, 0):
+        for dst, src in zip((x, r, ids), inputs[i]):
+            dst.copy_(src)
+        g, out = graphs[i % 2]
+        g.replay()
+        eager = _layer(x, r, w, q, s, a, b, ids, scales)[1]
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[i]) and torch.equal(eager, want[i])
