@@ -7,66 +7,12 @@
 //   activations (B)  16 bytes from 16 g on and 16 bytes from 64 + 16 g on,
 //   scales           the byte of block g, of either operand.
 // The sums: row i of x, weight rows 4 g .. 4 g + 3.
-#include "common.h"
-#include "layer.h"
-#include "../../include/mxfp4.h"
+#include "gemm_a8.h"
 
 namespace mxfp4 {
 namespace a8 {
 
-typedef __attribute__((ext_vector_type(8))) int i32x8_t;
-
-constexpr int kOob = 0x7FFFFFF0;        // lane offset beyond any descriptor: the load returns zero
-
-// 0 where at <= last, else an offset beyond any descriptor (arithmetic, as a branch around a load makes the compiler wait for it).
-__device__ __forceinline__ int past(int last, int at) { return ((last - at) >> 31) & kOob; }
-
-__device__ __forceinline__ f32x4_t mfma(u32x4_t w, const u32x4_t* x, f32x4_t sum, uint32_t ws, uint32_t xs)
-{
-    const i32x8_t a = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
-    const i32x8_t b = {(int)x[0][0], (int)x[0][1], (int)x[0][2], (int)x[0][3], (int)x[1][0], (int)x[1][1], (int)x[1][2], (int)x[1][3]};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, sum, 4, 0, 0, (int)ws, 0, (int)xs);
-}
-
-// Four finished sums of row m, weight rows n .. n + 3 (n a multiple of 4), on their way out.
-struct Out {
-    const uint16_t* bias;
-    const uint16_t* residual;
-    uint16_t* y;
-    int64_t ldy, ldr;
-    int m, n, act;
-};
-
-__device__ __forceinline__ void finish(const Out& o, int m, int n, f32x4_t z)
-{
-    if (m >= o.m || n >= o.n)
-        return;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (o.bias && n + i < o.n)
-            z[i] += bf16_bits_to_f32(o.bias[n + i]);
-    if (o.act == MXFP4_ACT_SWIGLU) {
-#pragma unroll
-        for (int i = 0; i < 4; i += 2) {
-            if (n + i >= o.n)
-                break;
-            const int c = (n + i) >> 1;
-            float t = silu_gate(z[i], z[i + 1]);
-            if (o.residual)
-                t += bf16_bits_to_f32(o.residual[m * o.ldr + c]);
-            o.y[m * o.ldy + c] = f32_to_bf16_rne(t);
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (n + i >= o.n)
-            break;
-        if (o.residual)
-            z[i] += bf16_bits_to_f32(o.residual[m * o.ldr + n + i]);
-        o.y[m * o.ldy + n + i] = f32_to_bf16_rne(z[i]);
-    }
-}
+namespace {
 
 // A workgroup computes 16 MF rows of x times 16 NF weight rows; its eight waves share the steps of K, and both operands go straight to
 // the registers.  The waves' sums meet in the LDS and are added in wave order.
@@ -164,11 +110,19 @@ hipError_t launch(const A8Args& a, hipStream_t stream)
     return hipSuccess;
 }
 
+}  // namespace
+
 }  // namespace a8
 
 hipError_t launch_w4a8(const A8Args& a, const DeviceInfo&, hipStream_t stream)
 {
     const bool ragged = a.k % 128 != 0;
+    if (const char* e = knob("MXFP4_A8_SHAPE")) {
+        if (atoi(e) >= 0)
+            return a8::launch_block(a, atoi(e), stream);
+    } else if (a.m > 64) {
+        return a8::launch_block(a, a.m > 512 ? 0 : a.m > 128 ? 1 : a.m > 64 ? 2 : 3, stream);
+    }
     if (a.m <= 16)
         return ragged ? a8::launch<1, 1, true>(a, stream) : a8::launch<1, 1, false>(a, stream);
     if (a.m <= 32)
