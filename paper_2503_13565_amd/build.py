@@ -20,7 +20,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libmxfp4_hip.so")
 HOST = os.path.join(HERE, "_host.so")
-SOURCES = ["api.hip", "cast.hip", "gemv.hip", "gemv_reg.hip", "gemv_short.hip", "chain.hip", "mfma.hip", "mfma_tile.hip", "bf16.hip", "e4m3.hip", "e2m3.hip", "mxfmt.hip", "gemm_t.hip", "gemv_tile.hip", "gemm_wide.hip", "gemm_wide_fmt.hip", "gemm_wide_bf16.hip", "kv_api.hip", "kv_store.hip", "kv_pages.hip", "kv_attend.hip", "layer_api.hip", "norm.hip", "gemm_a8.hip", "gemm_a8_block.hip", "lora.hip"]
+SOURCES = ["api.hip", "cast.hip", "gemv.hip", "gemv_reg.hip", "gemv_short.hip", "chain.hip", "mfma.hip", "mfma_tile.hip", "bf16.hip", "e4m3.hip", "e2m3.hip", "mxfmt.hip", "gemm_t.hip", "gemv_tile.hip", "gemm_wide.hip", "gemm_wide_fmt.hip", "gemm_wide_bf16.hip", "kv_api.hip", "kv_store.hip", "kv_pages.hip", "kv_attend.hip", "layer_api.hip", "norm.hip", "gemm_a8.hip", "gemm_a8_mid.hip", "gemm_a8_block.hip", "lora.hip"]
 HOST_SOURCES = ["host.cpp", "host_kv.cpp", "host_layer.cpp"]
 # packed FP32 instructions are disabled on purpose: see the build notes of this project
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

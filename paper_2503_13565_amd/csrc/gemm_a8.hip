@@ -1,12 +1,22 @@
 // The product of 8-bit rows with MXFP4 weights, y = x8 * dequant(W)^T, on the scaled matrix instructions: E4M3 codes against E2M1 codes,
 // each block of 32 with its scale byte, exactly as both lie in memory (arXiv 2503.13565, section 3.4.3, Eq. 2 with 8-bit rows in place
-// of BF16).  Nothing is decoded, and an instruction does four times the work of a BF16 one in twice its time.
+// of BF16).  Nothing is decoded, and an instruction does four times the work of a BF16 one in twice its time.  This file has the kernel of
+// few rows, where the weights' way from memory is what there is to do; gemm_a8_block.hip has many.
 //
 // v_mfma_scale_f32_16x16x128_f8f6f4, one step of 128 along K: lane i + 16 g holds, of row i,
 //   weights (A)      16 bytes: block g of the step,
 //   activations (B)  16 bytes from 16 g on and 16 bytes from 64 + 16 g on,
 //   scales           the byte of block g, of either operand.
-// The sums: row i of x, weight rows 4 g .. 4 g + 3.
+// The sums: row i of x, weight rows 4 g .. 4 g + 3.  (How the instruction adds: include/mxfp4.h, mxfp4_w4a8_gemm.)
+//
+// A workgroup has 16 NF weight rows and all rows of x (up to 16 WM MF of them), and its eight waves are WM x WK: WK share the steps of K.  K goes
+// by in phases of WK steps.  Both operands of a phase lie in the LDS as rows, brought there by loads that write it directly, whole lines of memory an
+// instruction (loads in the layout of the matrix instruction touch a line per lane: 77 rows x 4096 x 11008 33 us), D - 1 phases ahead.  The
+// partial sums of the WK waves meet in the LDS at the end and are added in wave order.
+//   - Chunk c (16 bytes) of row r lies at c ^ (r % 16): the sixteen lanes that a turn of the LDS serves find sixteen different places.
+//   - XR rows of x are held; with fewer than 16, the instruction's other columns read them again, and are not stored.
+//   - The scale bytes of the workgroup's rows are one piece of memory, which is copied at the start; a lane reads its byte.
+//   - What lies past K loads as zeros, under the row's last scale (which is NaN only where the row is).
 #include "gemm_a8.h"
 
 namespace mxfp4 {
@@ -14,95 +24,141 @@ namespace a8 {
 
 namespace {
 
-// A workgroup computes 16 MF rows of x times 16 NF weight rows; its eight waves share the steps of K, and both operands go straight to
-// the registers.  The waves' sums meet in the LDS and are added in wave order.
-template <int MF, int NF, bool kRagged>
-__global__ __launch_bounds__(512) void w4a8_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ xs,
-                                                   const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, int k, int tiles_m, Out out)
+constexpr int rows_buffer(int wk, int xr, int bn) { return wk * (xr * 128 + bn * 64); }
+constexpr int rows_scales(int rows, int nblk) { return (rows * nblk + 1023) / 1024 * 1024; }
+// D buffers (afterwards: the waves' sums), a KiB that surplus loads write, the scales
+constexpr int rows_fixed(int wk, int mf, int nf, int xr, int bn, int d)
 {
-    constexpr int BM = MF * 16, BN = NF * 16, D = 2;
-    __shared__ f32x4_t red[8][MF * NF][64];
+    const int buffers = d * rows_buffer(wk, xr, bn), sums = 8 * mf * nf * 1024;
+    return (buffers > sums ? buffers : sums) + 1024;
+}
+template <int WM, int WN, int WK, int MF, int NF, int XR, int D>
+__global__ __launch_bounds__(512) void w4a8_rows_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ xs,
+                                                        const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, int k, int tiles_m, Out out)
+{
+    static_assert(WM * WN * WK == 8 && (XR == WM * MF * 16 || (WM * MF == 1 && XR < 16)), "eight waves; the rows of x");
+    constexpr int BM = WM * MF * 16, BN = WN * NF * 16;
+    constexpr int kX = XR * WK / 8, kW = BN * WK / 16, kUnits = kX + kW, C = (kUnits + 7) / 8;     // KiB of a phase, loads of a wave
+    static_assert(kX * 8 == XR * WK && kW * 16 == BN * WK, "whole KiB");
+    constexpr int kBuf = rows_buffer(WK, XR, BN), kFixed = rows_fixed(WK, MF, NF, XR, BN, D);
+    extern __shared__ __align__(16) uint8_t smem[];
     const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / (WN * WK), wn = wave / WK % WN, wk = wave % WK;
     const int m0 = (int)(blockIdx.x % tiles_m) * BM, n0 = (int)(blockIdx.x / tiles_m) * BN;
     const int rows = min(BM, out.m - m0), cols = min(BN, out.n - n0);
-    const int nblk = k >> 5, steps = (k + 127) >> 7;
-    auto view = [](const uint8_t* p, int bytes) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, bytes, 0x00020000); };
-    const __amdgpu_buffer_rsrc_t rx = view(x + (int64_t)m0 * k, rows * k), rxs = view(xs + (int64_t)m0 * nblk, rows * nblk);
-    const __amdgpu_buffer_rsrc_t rq = view(q + (int64_t)n0 * (k >> 1), cols * (k >> 1)), rs = view(s + (int64_t)n0 * nblk, cols * nblk);
+    const int nblk = k >> 5, steps = (k + 127) >> 7, phases = (steps + WK - 1) / WK;
+    const u32x4_t rx = words(x + (int64_t)m0 * k, rows * k), rq = words(q + (int64_t)n0 * (k >> 1), cols * (k >> 1));
+    const uint32_t lds_at = lds_address(smem);
 
-    struct Slot {
-        u32x4_t w[NF], x[MF][2];
-        uint32_t ws[NF], xs[MF];
+    // Load c of wave w fills KiB 8 c + w of a phase: x first, the weights behind it.
+    int off[C], chunk[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int u = c * 8 + wave;
+        const bool of_x = u < kX;
+        const int at = (of_x ? u : u - kX) * 64 + lane;
+        const int row = of_x ? at / (WK * 8) : at / (WK * 4);
+        chunk[c] = of_x ? at % (WK * 8) ^ turn(row, WK * 8) : at % (WK * 4) ^ turn(row, WK * 4);
+        off[c] = u >= kUnits ? kOob : of_x ? (row * k + chunk[c] * 16) | past(rows - 1, row) : (row * (k >> 1) + chunk[c] * 16) | past(cols - 1, row);
+    }
+    auto issue = [&](int p, int b) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int u = c * 8 + wave;
+            if (u < kX)
+                direct(lds_at + b * kBuf + u * 1024, off[c] | past((k >> 4) - 1, p * (WK * 8) + chunk[c]), rx, p < phases ? p * (WK * 128) : 0);
+            else
+                direct(lds_at + (u < kUnits ? b * kBuf + u * 1024 : kFixed - 1024), off[c] | past(nblk - 1, p * (WK * 4) + chunk[c]), rq,
+                       p < phases ? p * (WK * 64) : 0);
+        }
     };
-    Slot slot[D];
-    // What lies past K, or past the last row, loads as zeros under the scale 2^-127.
-    auto issue = [&](Slot& v, int T) {
-        const int p_w = past(nblk - 1, 4 * T + lg), p_lo = past((k >> 4) - 1, 8 * T + lg), p_hi = past((k >> 4) - 1, 8 * T + 4 + lg);
-        const int p_s = kRagged ? p_w : past(steps - 1, T);
-        auto scale = [&](const __amdgpu_buffer_rsrc_t r, int off) {
-            return kRagged ? (uint32_t)__builtin_amdgcn_raw_buffer_load_b8(r, (off + 4 * T + lg) | p_s, 0, 0)
-                           : (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (off + 4 * T) | p_s, 0, 0);
-        };
+
+    const int ws_bytes = rows_scales(BN, nblk), xs_bytes = rows_scales(XR, nblk);
+    {
+        // (a load is in range by whole dwords: the last one, which holds the last byte, counts)
+        const u32x4_t rs = words(s + (int64_t)n0 * nblk, (cols * nblk + 3) & ~3), rxs = words(xs + (int64_t)m0 * nblk, (rows * nblk + 3) & ~3);
+        for (int u = wave; u * 1024 < ws_bytes; u += 8)
+            direct(lds_at + kFixed + u * 1024, u * 1024 + lane * 16, rs, 0);
+        for (int u = wave; u * 1024 < xs_bytes; u += 8)
+            direct(lds_at + kFixed + ws_bytes + u * 1024, u * 1024 + lane * 16, rxs, 0);
+    }
+#pragma unroll
+    for (int d = 0; d < D - 1; ++d)
+        issue(d, d);
+
+    const int xrow = XR < 16 ? min(li, XR - 1) : wm * MF * 16 + li, wrow = wn * NF * 16 + li;
+    const int x_lo = xrow * (WK * 128) + ((8 * wk + lg) ^ turn(xrow, WK * 8)) * 16;
+    const int x_hi = xrow * (WK * 128) + ((8 * wk + 4 + lg) ^ turn(xrow, WK * 8)) * 16;
+    const int w_at = kX * 1024 + wrow * (WK * 64) + ((4 * wk + lg) ^ turn(wrow, WK * 4)) * 16;
+    const uint8_t *sw = smem + kFixed + wrow * nblk, *sx = smem + kFixed + ws_bytes + xrow * nblk;
+    f32x4_t acc[MF][NF] = {};
+    int b = 0;
+    for (int p = 0; p < phases; ++p) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 2) * C) : "memory");      // (D - 2 phases are younger than this one)
+        lds_barrier();
+        issue(p + D - 1, b == 0 ? D - 1 : b - 1);               // into the buffer that the phase before this one read
+        const uint8_t* buf = smem + b * kBuf;
+        const int block = min(4 * (p * WK + wk) + lg, nblk - 1);
+        u32x4_t w[NF], v[MF][2];
+        uint32_t ws[NF], vs[MF];
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
-            const int row = f * 16 + li, gone = past(cols - 1, row);
-            v.w[f] = __builtin_amdgcn_raw_buffer_load_b128(rq, (row * (k >> 1) + T * 64 + lg * 16) | p_w | gone, 0, 0);
-            v.ws[f] = scale(rs, (row * nblk) | gone);
+            w[f] = *reinterpret_cast<const u32x4_t*>(buf + w_at + f * (16 * WK * 64));
+            ws[f] = sw[f * 16 * nblk + block];
         }
 #pragma unroll
         for (int f = 0; f < MF; ++f) {
-            const int row = f * 16 + li, gone = past(rows - 1, row);
-            v.x[f][0] = __builtin_amdgcn_raw_buffer_load_b128(rx, (row * k + T * 128 + lg * 16) | p_lo | gone, 0, 0);
-            v.x[f][1] = __builtin_amdgcn_raw_buffer_load_b128(rx, (row * k + T * 128 + 64 + lg * 16) | p_hi | gone, 0, 0);
-            v.xs[f] = scale(rxs, (row * nblk) | gone);
+            v[f][0] = *reinterpret_cast<const u32x4_t*>(buf + x_lo + f * (16 * WK * 128));
+            v[f][1] = *reinterpret_cast<const u32x4_t*>(buf + x_hi + f * (16 * WK * 128));
+            vs[f] = sx[f * 16 * nblk + block];
         }
-    };
-    f32x4_t acc[MF][NF] = {};
-    auto multiply = [&](const Slot& v) {
 #pragma unroll
-        for (int a = 0; a < MF; ++a)
+        for (int i = 0; i < MF; ++i)
 #pragma unroll
-            for (int b = 0; b < NF; ++b)
-                acc[a][b] = mfma(v.w[b], v.x[a], acc[a][b], kRagged ? v.ws[b] : v.ws[b] >> (8 * lg), kRagged ? v.xs[a] : v.xs[a] >> (8 * lg));
-    };
-    int T = wave;
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-        issue(slot[d], T + 8 * d);
-    for (; T < steps; T += 8 * D) {
-#pragma unroll
-        for (int d = 0; d < D; ++d) {
-            multiply(slot[d]);
-            issue(slot[d], T + 8 * (d + D));
-        }
+            for (int f = 0; f < NF; ++f)
+                acc[i][f] = mfma(w[f], v[i], acc[i][f], ws[f], vs[i]);
+        b = b == D - 1 ? 0 : b + 1;
     }
-#pragma unroll
-    for (int a = 0; a < MF; ++a)
-#pragma unroll
-        for (int b = 0; b < NF; ++b)
-            red[wave][a * NF + b][lane] = acc[a][b];
+
+    drain_vmem();                                               // (the loads behind the last phase write the LDS)
     __syncthreads();
-    for (int i = threadIdx.x; i < MF * NF * 64; i += 512) {
-        const int f = i >> 6, l = i & 63;
-        f32x4_t z = red[0][f][l];
+    f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);
 #pragma unroll
-        for (int w = 1; w < 8; ++w)
-            z += red[w][f][l];
-        finish(out, m0 + f / NF * 16 + (l & 15), n0 + f % NF * 16 + 4 * (l >> 4), z);
+    for (int i = 0; i < MF; ++i)
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+            red[((wk * WM + wm) * MF + i) * (WN * NF * 64) + (wn * NF + f) * 64 + lane] = acc[i][f];
+    __syncthreads();
+    constexpr int kSums = WM * MF * WN * NF * 64;
+    for (int i = threadIdx.x; i < kSums; i += 512) {
+        const int f = i >> 6, l = i & 63;
+        f32x4_t z = red[i];
+#pragma unroll
+        for (int w = 1; w < WK; ++w)
+            z += red[w * kSums + i];
+        if (XR == BM || (l & 15) < XR)
+            finish(out, m0 + f / (WN * NF) * 16 + (l & 15), n0 + f % (WN * NF) * 16 + 4 * (l >> 4), z);
     }
 }
 
 // A grid holds less than 2^32 threads, so very many rows are several launches.
-template <int MF, int NF, bool kRagged>
+template <int WM, int WN, int WK, int MF, int NF, int XR, int D>
 hipError_t launch(const A8Args& a, hipStream_t stream)
 {
-    const int64_t tiles_n = (a.n + NF * 16 - 1) / (NF * 16), most = max(((int64_t)1 << 22) / tiles_n, (int64_t)1) * (MF * 16);
+    constexpr int BM = WM * MF * 16, BN = WN * NF * 16;
+    const int nblk = a.k >> 5, lds = rows_fixed(WK, MF, NF, XR, BN, D) + rows_scales(BN, nblk) + rows_scales(XR, nblk);
+    if (lds > 160 * 1024)                                       // (a K so long that the rows' scales leave no room)
+        return launch_mid(a, 3, 1, stream);
+    static LdsLimit limit;
+    const hipError_t raised = limit.raise(reinterpret_cast<const void*>(w4a8_rows_kernel<WM, WN, WK, MF, NF, XR, D>), 160 * 1024);
+    if (raised != hipSuccess)
+        return raised;
+    const int64_t tiles_n = (a.n + BN - 1) / BN, most = max(((int64_t)1 << 22) / tiles_n, (int64_t)1) * BM;
     for (int64_t at = 0; at < a.m; at += most) {
-        const int m = (int)min(most, a.m - at), tiles_m = (m + MF * 16 - 1) / (MF * 16);
-        const Out out = {a.epi.bias, a.epi.residual ? a.epi.residual + at * a.ldr : nullptr, a.y + at * a.ldy, a.ldy, a.ldr, m, a.n, a.epi.act};
-        w4a8_kernel<MF, NF, kRagged><<<dim3((unsigned)(tiles_m * tiles_n)), 512, 0, stream>>>(
-            a.x + at * a.k, a.xs + at * (a.k >> 5), a.q, a.s, a.k, tiles_m, out);
+        const int m = (int)min(most, a.m - at), tiles_m = (m + BM - 1) / BM;
+        w4a8_rows_kernel<WM, WN, WK, MF, NF, XR, D><<<dim3((unsigned)(tiles_m * tiles_n)), 512, lds, stream>>>(
+            a.x + at * a.k, a.xs + at * (a.k >> 5), a.q, a.s, a.k, tiles_m, out_of(a, at, m));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
@@ -114,20 +170,62 @@ hipError_t launch(const A8Args& a, hipStream_t stream)
 
 }  // namespace a8
 
-hipError_t launch_w4a8(const A8Args& a, const DeviceInfo&, hipStream_t stream)
+namespace {
+
+struct Plan {
+    int shape, splits;
+};
+
+Plan plan(int64_t m, int64_t n, int64_t k, const DeviceInfo& dev)
 {
-    const bool ragged = a.k % 128 != 0;
-    if (const char* e = knob("MXFP4_A8_SHAPE")) {
-        if (atoi(e) >= 0)
-            return a8::launch_block(a, atoi(e), stream);
-    } else if (a.m > 64) {
-        return a8::launch_block(a, a.m > 512 ? 0 : a.m > 128 ? 1 : a.m > 64 ? 2 : 3, stream);
+    Plan p = {m <= 1 ? 10 : m <= 4 ? 11 : m <= 16 ? 30 : m > 512 ? 0 : m > 64 ? 2 : 1, 1};
+    if (const char* e = knob("MXFP4_A8_SHAPE"))
+        p.shape = atoi(e);
+    if (const char* e = knob("MXFP4_A8_SPLITS"))
+        p.splits = atoi(e);
+    return p;
+}
+
+}  // namespace
+
+size_t a8_part_bytes(int64_t m, int64_t n, int64_t k, const DeviceInfo& dev)
+{
+    const Plan p = plan(m, n, k, dev);
+    return p.splits > 1 ? (size_t)p.splits * m * ((n + 255) / 256 * 256) * sizeof(float) : 0;
+}
+
+hipError_t launch_w4a8(const A8Args& a, const DeviceInfo& dev, hipStream_t stream)
+{
+    using namespace a8;
+    const Plan p = plan(a.m, a.n, a.k, dev);
+    const int shape = p.shape, splits = p.splits > 1 && a.part ? p.splits : 1;
+    switch (shape) {
+    case 0:
+        return launch_block(a, stream);
+    case 10:
+        return launch<1, 1, 8, 1, 1, 1, 3>(a, stream);
+    case 11:
+        return launch<1, 1, 8, 1, 1, 4, 3>(a, stream);
+    case 12:
+        return launch<1, 1, 8, 1, 1, 16, 3>(a, stream);
+    case 23:
+        return launch<1, 2, 4, 1, 1, 2, 3>(a, stream);
+    case 30:
+        return launch<1, 2, 4, 1, 1, 16, 2>(a, stream);
+    case 31:
+        return launch<1, 2, 4, 1, 1, 16, 3>(a, stream);
+    case 37:
+        return launch<1, 1, 8, 1, 2, 16, 2>(a, stream);
+    case 38:
+        return launch<1, 1, 8, 1, 1, 16, 2>(a, stream);
+    case 40:
+        return launch<2, 1, 4, 1, 1, 32, 3>(a, stream);
+    case 43:
+        return launch<1, 2, 4, 2, 1, 32, 3>(a, stream);
+    case 47:
+        return launch<1, 2, 4, 2, 2, 32, 3>(a, stream);
     }
-    if (a.m <= 16)
-        return ragged ? a8::launch<1, 1, true>(a, stream) : a8::launch<1, 1, false>(a, stream);
-    if (a.m <= 32)
-        return ragged ? a8::launch<2, 1, true>(a, stream) : a8::launch<2, 1, false>(a, stream);
-    return ragged ? a8::launch<4, 2, true>(a, stream) : a8::launch<4, 2, false>(a, stream);
+    return launch_mid(a, shape, splits, stream);
 }
 
 }  // namespace mxfp4

@@ -13,8 +13,7 @@
 //   - Scale bytes come through registers four steps at a time (16 bytes a row, at any address, as K / 32 may be any number) and are laid out
 //     by position: [step][block][wave row][i][tile], so that one read gives a lane the bytes of all its tiles, which the
 //     instruction takes by number.  Blocks past K get zero bytes, as their codes load as zeros.
-#include <utility>
-
+#include "block_out.h"
 #include "gemm_a8.h"
 
 namespace mxfp4 {
@@ -22,47 +21,8 @@ namespace a8 {
 
 namespace {
 
-typedef __attribute__((ext_vector_type(16))) float f32x16_t;
-
-template <class F, int... I>
-__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>)
-{
-    (f(std::integral_constant<int, I>{}), ...);
-}
-template <int N, class F>
-__device__ __forceinline__ void each(F f)
-{
-    each_of(f, std::make_integer_sequence<int, N>{});
-}
-
 constexpr int lds_buffer(int bm, int bn) { return bm * 128 + bn * 64; }
-constexpr int lds_bytes(int bm, int bn) { return 3 * lds_buffer(bm, bn) + 2 * 16 * (bm + bn); }
-
-// Up to eight finished outputs of row m from column c on (a multiple of 8 of o's columns), before the residual.  wide: rows' pieces
-// of 16 bytes are aligned.
-__device__ __forceinline__ void finish8(const Out& o, bool wide, int m, int c, int columns, float* t)
-{
-    if (wide && c + 8 <= columns) {
-        u32x4_t v;
-        if (o.residual) {
-            v = *reinterpret_cast<const u32x4_t*>(o.residual + m * o.ldr + c);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                t[2 * e] += __uint_as_float(v[e] << 16);
-                t[2 * e + 1] += __uint_as_float(v[e] & 0xFFFF0000u);
-            }
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            v[e] = f32_to_bf16_rne2(t[2 * e], t[2 * e + 1]);
-        *reinterpret_cast<u32x4_t*>(o.y + m * o.ldy + c) = v;
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (c + e < columns)
-            o.y[m * o.ldy + c + e] = f32_to_bf16_rne(o.residual ? t[e] + bf16_bits_to_f32(o.residual[m * o.ldr + c + e]) : t[e]);
-}
+constexpr int lds_bytes(int bm, int bn, int d) { return d * lds_buffer(bm, bn) + 2 * 16 * (bm + bn); }
 
 // 16 scale bytes of a row from block `at` on; zeros past its end.  No byte outside the row is read.
 __device__ __forceinline__ u32x4_t scale_bytes(const uint8_t* row, int at, int nblk)
@@ -84,15 +44,16 @@ __device__ __forceinline__ u32x4_t scale_bytes(const uint8_t* row, int at, int n
     return v;
 }
 
-template <int WM, int WN, int MF, int NF>
-__global__ __launch_bounds__(512, 2) void w4a8_block_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ xs,
+template <int WM, int WN, int MF, int NF, int D>
+__global__ __launch_bounds__(WM * WN * 64, D == 2 ? 4 : WM * WN / 4) void w4a8_block_kernel(const uint8_t* __restrict__ x, const uint8_t* __restrict__ xs,
                                                             const uint8_t* __restrict__ q, const uint8_t* __restrict__ s, int k, int tiles_m,
                                                             int tiles_n, bool wide, Out out)
 {
-    static_assert(WM * WN == 8, "eight waves");
-    constexpr int BM = WM * MF * 32, BN = WN * NF * 32, CX = BM / 64, CW = BN / 128;
+    constexpr int kWaves = WM * WN, kThreads = kWaves * 64;
+    constexpr int BM = WM * MF * 32, BN = WN * NF * 32, CX = BM / 8 / kWaves, CW = BN / 16 / kWaves, kRows = (BM + BN + kThreads - 1) / kThreads;
     constexpr int kBuf = lds_buffer(BM, BN), kScales = 16 * (BM + BN);
-    static_assert(lds_bytes(BM, BN) <= 160 * 1024 && BN % 128 == 0 && BM + BN <= 512, "the LDS; whole instructions a wave; a row a thread");
+    static_assert(lds_bytes(BM, BN, D) <= (D == 2 ? 80 : 160) * 1024 && CX * 8 * kWaves == BM && CW * 16 * kWaves == BN && (D == 2 || (kRows * kThreads == BM + BN && BM == BN)),
+                  "the LDS; whole instructions a wave; whole rows of scales a thread");
     extern __shared__ __align__(16) uint8_t smem[];
     const int tid = threadIdx.x, lane = tid & 63, li = lane & 31, lh = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -100,77 +61,68 @@ __global__ __launch_bounds__(512, 2) void w4a8_block_kernel(const uint8_t* __res
     const int nblk = k >> 5, steps = (k + 127) >> 7;
     const bool ragged = (k & 127) != 0;
 
-    // Blocks that run together on a die share rows of x and of the weights: columns of up to eight blocks of rows.
-    const int at = blockIdx.x, band = at / (8 * tiles_n), band_m = min(8, tiles_m - 8 * band), in_band = at - band * 8 * tiles_n;
-    const int m0 = (8 * band + in_band % band_m) * BM, n0 = in_band / band_m * BN;
+    // The 32 blocks that a die runs at once are four rows of blocks by eight columns: they read 4 x 32 and 8 x 16 KiB a step through the die's L2.
+    const int at = block_on_die(tiles_m * tiles_n, blockIdx.x), band = at / (4 * tiles_n), band_m = min(4, tiles_m - 4 * band), in_band = at - band * 4 * tiles_n;
+    const int m0 = (4 * band + in_band % band_m) * BM, n0 = in_band / band_m * BN;
     const int rows = min(BM, out.m - m0), cols = min(BN, out.n - n0);
 
-    auto words = [](const uint8_t* p, int bytes) {
-        auto uniform = [](uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); };
-        const uint64_t a = reinterpret_cast<uint64_t>(p);
-        return u32x4_t{uniform((uint32_t)a), uniform((uint32_t)(a >> 32) & 0xFFFFu), uniform((uint32_t)bytes), 0x00020000u};
-    };
     const u32x4_t rx = words(x + (int64_t)m0 * k, rows * k), rq = words(q + (int64_t)n0 * (k >> 1), cols * (k >> 1));
-    const uint32_t lds_at = (uint32_t)reinterpret_cast<uint64_t>((__attribute__((address_space(3))) uint8_t*)smem);
+    const uint32_t lds_at = lds_address(smem);
 
-    // Load i of wave w fills KiB 8 i + w of a step's x (8 rows of 128 bytes) or weights (16 rows of 64).
+    // Load i of wave w fills KiB kWaves i + w of a step's x (8 rows of 128 bytes) or weights (16 rows of 64).
     int x_off[CX], x_chunk[CX], w_off[CW], w_chunk[CW];
 #pragma unroll
     for (int i = 0; i < CX; ++i) {
-        const int row = (i * 8 + wave) * 8 + (lane >> 3);
+        const int row = (i * kWaves + wave) * 8 + (lane >> 3);
         x_chunk[i] = (lane & 7) ^ (row >> 1 & 7);
         x_off[i] = (row * k + x_chunk[i] * 16) | past(rows - 1, row);
     }
 #pragma unroll
     for (int i = 0; i < CW; ++i) {
-        const int row = (i * 8 + wave) * 16 + (lane >> 2);
+        const int row = (i * kWaves + wave) * 16 + (lane >> 2);
         w_chunk[i] = (lane & 3) ^ (row >> 2 & 3);
         w_off[i] = (row * (k >> 1) + w_chunk[i] * 16) | past(cols - 1, row);
     }
-    // m0: where in the LDS lane 0's bytes go.  The load reads scalar registers that a vector instruction may have written just in front:
-    // five wait states, which the compiler does not count into assembly.
-    auto direct = [](uint32_t to, int off, const u32x4_t& r, int from) {
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(r), "s"(from)
-                     : "memory", "m0");
-    };
     auto issue = [&](int T, int b) {
         const uint32_t to = lds_at + b * kBuf + wave * 1024;
         const bool tail = ragged && T == steps - 1;
 #pragma unroll
         for (int i = 0; i < CX; ++i)
-            direct(to + i * 8192, x_off[i] | (tail ? past((k >> 4) - 1, T * 8 + x_chunk[i]) : 0), rx, T * 128);
+            direct(to + i * (kWaves * 1024), x_off[i] | (tail ? past((k >> 4) - 1, T * 8 + x_chunk[i]) : 0), rx, T * 128);
 #pragma unroll
         for (int i = 0; i < CW; ++i)
-            direct(to + BM * 128 + i * 8192, w_off[i] | (tail ? past(nblk - 1, T * 4 + w_chunk[i]) : 0), rq, T * 64);
+            direct(to + BM * 128 + i * (kWaves * 1024), w_off[i] | (tail ? past(nblk - 1, T * 4 + w_chunk[i]) : 0), rq, T * 64);
     };
 
-    // This thread's row of scales and where its bytes go (for step t and block b: + (4 t + b) * 32 * tiles of a row or column of waves).
-    const bool of_x = tid < BM;
-    const int s_row = of_x ? tid : tid - BM;
-    const bool s_live = of_x ? s_row < rows : s_row < cols;
-    const uint8_t* s_from = (of_x ? xs + (int64_t)m0 * nblk : s + (int64_t)n0 * nblk) + (int64_t)(s_live ? s_row : 0) * nblk;
-    int s_to, s_step;
-    if (of_x) {
-        const int w = s_row / (32 * MF), f = s_row / 32 % MF, i = s_row & 31;
-        s_to = (w * 32 + i) * MF + f;
-        s_step = BM;
-    } else {
-        const int w = s_row / (32 * NF), f = s_row / 32 % NF, n = s_row & 31, i = 8 * (n >> 2 & 3) + 4 * (n >> 4) + (n & 3);
-        s_to = 16 * BM + (w * 32 + i) * NF + f;
-        s_step = BN;
+    // This thread's rows of scales and where their bytes go (for step t and block b: + (4 t + b) * rows of the operand).
+    uint8_t* scales = smem + D * kBuf;
+    const uint8_t* s_from[kRows];
+    int s_to[kRows];
+    bool s_live[kRows];
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+        const bool of_x = i * kThreads + tid < BM;
+        const int row = i * kThreads + tid - (of_x ? 0 : BM);
+        s_live[i] = i * kThreads + tid < BM + BN && row < (of_x ? rows : cols);
+        s_from[i] = (of_x ? xs + (int64_t)m0 * nblk : s + (int64_t)n0 * nblk) + (int64_t)(s_live[i] ? row : 0) * nblk;
+        const int tiles = of_x ? MF : NF, r = row & 31;
+        const int at32 = of_x ? r : 8 * (r >> 2 & 3) + 4 * (r >> 4) + (r & 3);
+        s_to[i] = (of_x ? 0 : 16 * BM) + (row / (32 * tiles) * 32 + at32) * tiles + row / 32 % tiles;
     }
-    uint8_t* scales = smem + 3 * kBuf;
-    u32x4_t sv = {0, 0, 0, 0};
+    u32x4_t sv[kRows] = {};
     auto load_scales = [&](int group) {
-        if (tid < BM + BN && s_live && group * 16 < nblk)
-            sv = scale_bytes(s_from, group * 16, nblk);
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (s_live[i] && group * 16 < nblk)
+                sv[i] = scale_bytes(s_from[i], group * 16, nblk);
     };
     auto store_scales = [&](int group) {
-        uint8_t* to = scales + (group & 1) * kScales + s_to;
-        if (tid < BM + BN)
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+            if (kRows * kThreads == BM + BN || i * kThreads + tid < BM + BN)
 #pragma unroll
             for (int b = 0; b < 16; ++b)
-                to[b * s_step] = (uint8_t)(sv[b >> 2] >> (8 * (b & 3)));
+                scales[(group & 1) * kScales + s_to[i] + b * (BM == BN || i * kThreads + tid < BM ? BM : BN)] = (uint8_t)(sv[i][b >> 2] >> (8 * (b & 3)));
     };
 
     // The operands of half a step.
@@ -182,31 +134,35 @@ __global__ __launch_bounds__(512, 2) void w4a8_block_kernel(const uint8_t* __res
     const int x_read = (wm * MF * 32 + li) * 128 + (lh ^ (li >> 1 & 7)) * 16;
     const int w_read = BM * 128 + (wn * NF * 32 + wrow) * 64 + (lh ^ a) * 16;
     const int xs_read = (lh * WM * 32 + wm * 32 + li) * MF, ws_read = 16 * BM + (lh * WN * 32 + wn * 32 + li) * NF;
-    auto read = [&](int T, int b, auto kh, Half& h) {
+    // The reads of half kh of step T, which lies in buffer b, one by one: scales, weights, x.
+    constexpr int kReads = 1 + NF + 2 * MF;
+    auto read = [&](int T, int b, auto kh, Half& h, auto which) {
+        constexpr int at = decltype(which)::value;
         const uint8_t* buf = smem + b * kBuf;
-        const uint8_t* sc = scales + (T >> 2 & 1) * kScales;
-        const int part = (T & 3) * 4 + 2 * kh;
-        auto bytes = [](const uint8_t* p, auto n) -> uint32_t {
-            if constexpr (n == 4)
-                return *reinterpret_cast<const uint32_t*>(p);
-            else if constexpr (n == 2)
-                return *reinterpret_cast<const uint16_t*>(p);
-            else
-                return *p;
-        };
-        h.xs = bytes(sc + xs_read + part * BM, std::integral_constant<int, MF>{});
-        h.ws = bytes(sc + ws_read + part * BN, std::integral_constant<int, NF>{});
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-            h.w[f] = *reinterpret_cast<const u32x4_t*>(buf + (w_read ^ (kh * 32)) + f * 2048);
-#pragma unroll
-        for (int f = 0; f < MF; ++f) {
-            h.x[f][0] = *reinterpret_cast<const u32x4_t*>(buf + (x_read ^ (kh * 64)) + f * 4096);
-            h.x[f][1] = *reinterpret_cast<const u32x4_t*>(buf + (x_read ^ (kh * 64 + 32)) + f * 4096);
+        if constexpr (at == 0) {
+            const uint8_t* sc = scales + (T >> 2 & 1) * kScales;
+            const int part = (T & 3) * 4 + 2 * kh;
+            auto bytes = [](const uint8_t* p, auto n) -> uint32_t {
+                if constexpr (n == 4)
+                    return *reinterpret_cast<const uint32_t*>(p);
+                else if constexpr (n == 2)
+                    return *reinterpret_cast<const uint16_t*>(p);
+                else
+                    return *p;
+            };
+            h.xs = bytes(sc + xs_read + part * BM, std::integral_constant<int, MF>{});
+            h.ws = bytes(sc + ws_read + part * BN, std::integral_constant<int, NF>{});
+        } else if constexpr (at <= NF) {
+            h.w[at - 1] = *reinterpret_cast<const u32x4_t*>(buf + (w_read ^ (kh * 32)) + (at - 1) * 2048);
+        } else if constexpr (at < kReads) {
+            constexpr int f = (at - 1 - NF) / 2, hi = (at - 1 - NF) % 2;
+            h.x[f][hi] = *reinterpret_cast<const u32x4_t*>(buf + (x_read ^ (kh * 64 + hi * 32)) + f * 4096);
         }
     };
     f32x16_t acc[MF][NF] = {};
-    auto multiply = [&](const Half& h) {
+    // The instructions of a half, and between(j) behind instruction j: an instruction holds the matrix pipe for 64 cycles, in which what is between
+    // them leaves for free; in front of them all, the reads of eight waves keep the pipe waiting for 640 (the prompt 345 us).
+    auto multiply = [&](const Half& h, auto between) {
         each<MF>([&](auto i) {
             each<NF>([&](auto f) {
                 const u32x4_t w = h.w[f], x0 = h.x[i][0], x1 = h.x[i][1];
@@ -214,108 +170,94 @@ __global__ __launch_bounds__(512, 2) void w4a8_block_kernel(const uint8_t* __res
                 const i32x8_t B = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
                 acc[i][f] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, acc[i][f], 4, 0, decltype(f)::value, (int)h.ws,
                                                                            decltype(i)::value, (int)h.xs);
+                if constexpr (MF * NF == 16)                    // (256 sums a lane: the accumulation registers hold them, and nothing else)
+                    settle_a(acc[i][f]);
+                else
+                    settle(acc[i][f]);
+                if constexpr (D > 2)
+                    __builtin_amdgcn_sched_barrier(0);
+                between(std::integral_constant<int, decltype(i)::value * NF + decltype(f)::value>{});
+                if constexpr (D > 2)
+                    __builtin_amdgcn_sched_barrier(0);
             });
         });
     };
+    constexpr int kEach = (kReads + MF * NF - 2) / (MF * NF - 1);       // reads behind an instruction
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
 
     load_scales(0);
     issue(0, 0);
+    if constexpr (D == 2) {
+        store_scales(0);
+        load_scales(1);
+        for (int T = 0; T < steps; ++T) {
+            drain_vmem();                                       // this step's loads, which left a step ago
+            if ((T & 3) == 3)
+                store_scales((T >> 2) + 1);
+            lds_barrier();
+            if (T + 1 < steps)
+                issue(T + 1, (T + 1) & 1);
+            if ((T & 3) == 3)
+                load_scales((T >> 2) + 2);
+            each<kReads>([&](auto r) { read(T, T & 1, first, half[0], r); });
+            multiply(half[0], [&](auto) {});
+            each<kReads>([&](auto r) { read(T, T & 1, second, half[0], r); });
+            multiply(half[0], [&](auto) {});
+        }
+        __syncthreads();
+        leave<MF, NF>(out, wide, smem + wave * (leave_bytes(NF) / 8), lane, m0 + wm * MF * 32, n0 + wn * NF * 32, acc);
+        return;
+    }
     if (steps > 1)
         issue(1, 1);
     store_scales(0);
     drain_vmem();
     lds_barrier();
     load_scales(1);
-    read(0, 0, first, half[0]);
+    each<kReads>([&](auto r) { read(0, 0, first, half[0], r); });
     int b = 0;                                                  // the step's buffer
     // (Without a condition around what changes registers: behind the last step a buffer is read that nothing uses.)
     for (int T = 0; T < steps; ++T) {
         const int next = b == 2 ? 0 : b + 1, free = next == 2 ? 0 : next + 1;
-        read(T, b, second, half[1]);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(half[0]);
-#pragma unroll
-        for (int i = 0; i < MF; ++i)
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-                asm volatile("" : "+v"(acc[i][f]));             // (else they are moved behind the branches below)
-        __builtin_amdgcn_sched_barrier(0);
-        drain_vmem();                                           // the next step's loads, which left a step ago
-        if ((T & 3) == 2)
-            store_scales((T >> 2) + 1);
-        lds_barrier();
-        if (T + 2 < steps)
-            issue(T + 2, free);
-        if ((T & 3) == 3)
-            load_scales((T >> 2) + 2);
-        read(T + 1, next, first, half[0]);
-        __builtin_amdgcn_sched_barrier(0);
-        multiply(half[1]);
-        __builtin_amdgcn_sched_barrier(0);
+        multiply(half[0], [&](auto j) {
+            each<kEach>([&](auto e) { read(T, b, second, half[1], std::integral_constant<int, decltype(j)::value * kEach + decltype(e)::value>{}); });
+        });
+        multiply(half[1], [&](auto j) {
+            constexpr int at = decltype(j)::value;
+            if constexpr (at == 0) {
+                drain_vmem();                                   // the next step's loads, which left a step ago
+                if ((T & 3) == 2)
+                    store_scales((T >> 2) + 1);
+                lds_barrier();
+                if (T + 2 < steps)
+                    issue(T + 2, free);
+                if ((T & 3) == 3)
+                    load_scales((T >> 2) + 2);
+            } else {
+                each<kEach>([&](auto e) { read(T + 1, next, first, half[0], std::integral_constant<int, (at - 1) * kEach + decltype(e)::value>{}); });
+            }
+        });
         b = next;
     }
-
-    // Out through the LDS, 32 rows at a time, so that whole pieces of rows are stored.  Each wave has a part of its own.
-    constexpr int kCols = 32 * NF, kStride = kCols + 4;
-    static_assert(8 * 32 * kStride * 4 <= 3 * kBuf, "the operands' place");
+    static_assert(leave_bytes(NF) / 8 * kWaves <= lds_bytes(BM, BN, D), "the operands' place");
     __syncthreads();
-    float* tile = reinterpret_cast<float*>(smem) + wave * 32 * kStride;
-    const bool gate = out.act == MXFP4_ACT_SWIGLU;
-    const int columns = gate ? out.n >> 1 : out.n, piece = gate ? 16 : 8, pieces = kCols / piece, n1 = n0 + wn * kCols;
-#pragma unroll
-    for (int i = 0; i < MF; ++i) {
-#pragma unroll
-        for (int f = 0; f < NF; ++f)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4)
-                *reinterpret_cast<f32x4_t*>(tile + li * kStride + f * 32 + 16 * lh + e) =
-                    f32x4_t{acc[i][f][e], acc[i][f][e + 1], acc[i][f][e + 2], acc[i][f][e + 3]};
-        const int m1 = m0 + (wm * MF + i) * 32;
-#pragma unroll 1
-        for (int at = lane; at < 32 * pieces; at += 64) {
-            const int row = at / pieces, n = at % pieces * piece;
-            if (m1 + row >= out.m || n1 + n >= out.n)
-                continue;
-            float z[16];
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                if (e < 8 || gate) {
-                    const f32x4_t v = *reinterpret_cast<const f32x4_t*>(tile + row * kStride + n + e);
-                    z[e] = v[0], z[e + 1] = v[1], z[e + 2] = v[2], z[e + 3] = v[3];
-                }
-            }
-            if (out.bias)
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if ((e < 8 || gate) && n1 + n + e < out.n)
-                        z[e] += bf16_bits_to_f32(out.bias[n1 + n + e]);
-            if (gate)
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    z[e] = silu_gate(z[2 * e], z[2 * e + 1]);
-            finish8(out, wide, m1 + row, (n1 + n) >> (gate ? 1 : 0), columns, z);
-        }
-    }
+    leave<MF, NF>(out, wide, smem + wave * (leave_bytes(NF) / 8), lane, m0 + wm * MF * 32, n0 + wn * NF * 32, acc);
 }
 
-template <int WM, int WN, int MF, int NF>
+template <int WM, int WN, int MF, int NF, int D>
 hipError_t launch(const A8Args& a, hipStream_t stream)
 {
     constexpr int BM = WM * MF * 32, BN = WN * NF * 32;
     static LdsLimit limit;
-    const hipError_t raised = limit.raise(reinterpret_cast<const void*>(w4a8_block_kernel<WM, WN, MF, NF>), lds_bytes(BM, BN));
+    const hipError_t raised = limit.raise(reinterpret_cast<const void*>(w4a8_block_kernel<WM, WN, MF, NF, D>), lds_bytes(BM, BN, D));
     if (raised != hipSuccess)
         return raised;
-    auto aligned = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; };
-    const bool wide = aligned(a.y) && a.ldy % 8 == 0 && aligned(a.epi.residual) && (!a.epi.residual || a.ldr % 8 == 0);
     const int64_t tiles_n = (a.n + BN - 1) / BN, most = max(((int64_t)1 << 22) / tiles_n, (int64_t)1) * BM;
     for (int64_t at = 0; at < a.m; at += most) {
         const int m = (int)min(most, a.m - at), tiles_m = (m + BM - 1) / BM;
-        const Out out = {a.epi.bias, a.epi.residual ? a.epi.residual + at * a.ldr : nullptr, a.y + at * a.ldy, a.ldy, a.ldr, m, a.n, a.epi.act};
-        w4a8_block_kernel<WM, WN, MF, NF><<<dim3((unsigned)(tiles_m * tiles_n)), 512, lds_bytes(BM, BN), stream>>>(
-            a.x + at * a.k, a.xs + at * (a.k >> 5), a.q, a.s, a.k, tiles_m, (int)tiles_n, wide, out);
+        w4a8_block_kernel<WM, WN, MF, NF, D><<<dim3((unsigned)(tiles_m * tiles_n)), WM * WN * 64, lds_bytes(BM, BN, D), stream>>>(
+            a.x + at * a.k, a.xs + at * (a.k >> 5), a.q, a.s, a.k, tiles_m, (int)tiles_n, wide_rows(a), out_of(a, at, m));
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess)
             return e;
@@ -325,18 +267,18 @@ hipError_t launch(const A8Args& a, hipStream_t stream)
 
 }  // namespace
 
-hipError_t launch_block(const A8Args& a, int shape, hipStream_t stream)
+hipError_t launch_block(const A8Args& a, hipStream_t stream)
 {
-    switch (shape) {
-    case 0:
-        return launch<2, 4, 4, 2>(a, stream);
-    case 1:
-        return launch<2, 4, 2, 2>(a, stream);
-    case 2:
-        return launch<2, 4, 2, 1>(a, stream);
-    default:
-        return launch<2, 4, 1, 1>(a, stream);
-    }
+    if (const char* e = knob("MXFP4_A8_BLOCK"))
+        switch (atoi(e)) {
+        case 1:
+            return launch<2, 2, 4, 4, 3>(a, stream);
+        case 2:
+            return launch<2, 4, 2, 2, 2>(a, stream);
+        case 3:
+            return launch<2, 2, 2, 4, 2>(a, stream);
+        }
+    return launch<2, 4, 4, 2, 3>(a, stream);
 }
 
 }  // namespace a8
