@@ -436,17 +436,13 @@ int mxfp4_rms_norm(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, const 
  * in the mean.)
  *   x_e4m3, x_scales_e8m0  in  E4M3 codes uint8 [M, K] (16-byte aligned), scale bytes [M, K/32] (4-byte aligned)
  *   q_packed, scales_e8m0, bias_bf16, act, residual_bf16, ldr, y_bf16, ldy   as in mxfp4_woq_gemm_fused
- *   workspace  optional, mxfp4_w4a8_gemm_workspace_bytes(M, N, K) bytes (0: none is used), 16-byte aligned, contents unspecified before and
- *              after; calls that overlap in time must not share it.  With it, products of few blocks are cut along K (a second kernel adds the
- *              FP32 sums of the parts in order); without it, or with less, the call works too, slower
  * M, N >= 1, K a positive multiple of 32, at most MXFP4_MAX_K.  A scale byte 0xFF or a NaN code makes what it meets NaN: the row m of x or
- * the column n of w that holds it.  The summation order is fixed per (M, N, K, whether there is a workspace), not specified.
+ * the column n of w that holds it.  The summation order is fixed per (M, N, K), not specified.
  */
-size_t mxfp4_w4a8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
 int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M,
                     const void* q_packed, const void* scales_e8m0, int64_t N, int64_t K,
                     const void* bias_bf16, int act, const void* residual_bf16, int64_t ldr,
-                    void* y_bf16, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+                    void* y_bf16, int64_t ldy, void* stream);
 
 /*
  * Low-rank adapters of many requests at once beside a shared projection:

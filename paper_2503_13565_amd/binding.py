@@ -37,7 +37,7 @@ EXPORTS = [
     "mxfp4_woq_gemm_t_workspace_bytes", "mxfp4_woq_gemm_t",
     "mxfp4_kv_append", "mxfp4_kv_read", "mxfp4_kv_attention_workspace_bytes", "mxfp4_kv_attention",
     "mxfp4_kv_fork", "mxfp4_kv_extend", "mxfp4_kv_release", "mxfp4_kv_compact", "mxfp4_kv_copy_pages",
-    "mxfp4_rms_norm", "mxfp4_w4a8_gemm_workspace_bytes", "mxfp4_w4a8_gemm", "mxfp4_lora_workspace_bytes", "mxfp4_lora",
+    "mxfp4_rms_norm", "mxfp4_w4a8_gemm", "mxfp4_lora_workspace_bytes", "mxfp4_lora",
     "mxfp4_tile_repack_q_bytes", "mxfp4_tile_repack_s_bytes", "mxfp4_tile_repack", "mxfp4_woq_gemm_tiled",
     "mxfp4_woq_gemm_tiled_ws",
     "mxfp4_woq_gemm_tiled_argmax", "mxfp4_woq_gemm_tiled_verify", "mxfp4_woq_gemm_tiled_fused",
@@ -267,10 +267,8 @@ def load() -> ctypes.CDLL:
         getattr(lib, "mxfp4_kv_" + name).restype = i32
     lib.mxfp4_rms_norm.argtypes = [vp, i64, i64, i64, vp, i64, vp, ctypes.c_float, vp, i64, vp, i64, vp, vp, vp]
     lib.mxfp4_rms_norm.restype = i32
-    lib.mxfp4_w4a8_gemm.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, vp, i64, vp, i64, vp, sz, vp]
+    lib.mxfp4_w4a8_gemm.argtypes = [vp, vp, i64, vp, vp, i64, i64, vp, i32, vp, i64, vp, i64, vp]
     lib.mxfp4_w4a8_gemm.restype = i32
-    lib.mxfp4_w4a8_gemm_workspace_bytes.argtypes = [i64, i64, i64]
-    lib.mxfp4_w4a8_gemm_workspace_bytes.restype = sz
     lib.mxfp4_lora_workspace_bytes.argtypes = [i64, i64, i64]
     lib.mxfp4_lora_workspace_bytes.restype = sz
     lib.mxfp4_lora.argtypes = [vp, i64, i64, vp, vp, i64, i64, i64, i64, vp, vp, vp, i64, vp, i64, vp, sz, vp]
@@ -1399,17 +1397,11 @@ def mxfp4_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, resid
     return Normed(y, total, q8, s)
 
 
-def mxfp4_w4a8_gemm_workspace_bytes(m: int, n: int, k: int) -> int:
-    return int(load().mxfp4_w4a8_gemm_workspace_bytes(m, n, k))
-
-
 def mxfp4_w4a8_gemm(x8: torch.Tensor, xs: torch.Tensor, q: torch.Tensor, s: torch.Tensor, bias: Optional[torch.Tensor] = None,
-                    act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
-                    workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+                    act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The product of 8-bit rows (``x8 [M, K]``, ``xs [M, K/32]`` from :func:`mxfp4_rms_norm` or :func:`mxfp4_e4m3_direct_cast`) with MXFP4
-    weights, with bias, gate and residual add behind it as in :func:`mxfp4_woq_gemm_fused`; ``residual`` may be ``y`` itself.  A workspace of
-    :func:`mxfp4_w4a8_gemm_workspace_bytes` bytes is allocated unless one is given (an empty one: the call does without)."""
-    if y is None and workspace is None:
+    weights, with bias, gate and residual add behind it as in :func:`mxfp4_woq_gemm_fused`; ``residual`` may be ``y`` itself."""
+    if y is None:
         got = _layer_host().w4a8(x8, xs, q, s, bias, act, residual)
         if got is not None:
             return got
@@ -1428,12 +1420,8 @@ def mxfp4_w4a8_gemm(x8: torch.Tensor, xs: torch.Tensor, q: torch.Tensor, s: torc
     if residual is not None and residual.data_ptr() == y.data_ptr() and ldr != ldy:
         raise ValueError("residual is y with another row stride")
     with _on(dev):
-        if workspace is None:
-            workspace = torch.empty((mxfp4_w4a8_gemm_workspace_bytes(m, n, k),), dtype=torch.uint8, device=dev)
-        elif workspace.device != dev or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous tensor on the device of x8")
         _check(load().mxfp4_w4a8_gemm(_ptr(x8), _ptr(xs), m, _ptr(q), _ptr(s), n, k, _ptr(bias), act, _ptr(residual), ldr, _ptr(y), ldy,
-                                      _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+                                      _stream()))
     return y
 
 

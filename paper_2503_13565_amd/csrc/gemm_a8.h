@@ -99,7 +99,6 @@ typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 // Matrix instructions run with all lanes.  Where their result is used under a condition, the compiler may move them behind it, and the operands of
 // the other lanes with it; this keeps them in front.
 __device__ __forceinline__ void settle(f32x16_t& v) { asm volatile("" : "+v"(v)); }
-__device__ __forceinline__ void settle_a(f32x16_t& v) { asm volatile("" : "+a"(v)); }
 
 template <class F, int... I>
 __device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>)
@@ -143,15 +142,19 @@ __device__ __forceinline__ void finish8(const Out& o, bool wide, int m, int c, i
 constexpr int leave_stride(int nf) { return 32 * nf + 4; }
 constexpr int leave_bytes(int nf) { return 8 * 32 * leave_stride(nf) * 4; }                  // of eight waves
 
-// `piece` sums of row m from z on, weight rows from n on: eight outputs, or with the gate sixteen sums of eight.
-__device__ __forceinline__ void finish_piece(const Out& o, bool wide, int m, int n, const float* from)
+// A piece of row m, weight rows from n on: the sums of eight outputs, or with the gate sixteen sums of eight, as WK parts `stride` floats apart.
+template <int WK>
+__device__ __forceinline__ void finish_piece(const Out& o, bool wide, int m, int n, const float* from, int stride)
 {
     const bool gate = o.act == MXFP4_ACT_SWIGLU;
     float z[16];
 #pragma unroll
     for (int e = 0; e < 16; e += 4) {
         if (e < 8 || gate) {
-            const f32x4_t v = *reinterpret_cast<const f32x4_t*>(from + e);
+            f32x4_t v = *reinterpret_cast<const f32x4_t*>(from + e);
+#pragma unroll
+            for (int w = 1; w < WK; ++w)
+                v += *reinterpret_cast<const f32x4_t*>(from + w * stride + e);
             z[e] = v[0], z[e + 1] = v[1], z[e + 2] = v[2], z[e + 3] = v[3];
         }
     }
@@ -186,7 +189,7 @@ __device__ __forceinline__ void leave(const Out& o, bool wide, uint8_t* lds, int
         for (int at = lane; at < 32 * pieces; at += 64) {
             const int row = at / pieces, n = at % pieces * piece;
             if (m1 + row < o.m && n0 + n < o.n)
-                finish_piece(o, wide, m1 + row, n0 + n, tile + row * kStride + n);
+                finish_piece<1>(o, wide, m1 + row, n0 + n, tile + row * kStride + n, 0);
         }
     }
 }
@@ -204,8 +207,10 @@ inline Out out_of(const A8Args& a, int64_t at, int m)
     return {a.epi.bias, a.epi.residual ? a.epi.residual + at * a.ldr : nullptr, a.y + at * a.ldy, a.ldy, a.ldr, m, a.n, a.epi.act};
 }
 
-hipError_t launch_block(const A8Args& a, hipStream_t stream);
-hipError_t launch_mid(const A8Args& a, int shape, int splits, hipStream_t stream);
+// The kernels' shapes, by the outputs of a workgroup.
+enum Shape { kRows1, kRows4, kRows8, kRows12, kRows16, kRows16Deep, kRows32, kMid32x64, kMid32x64Deep, kMid64x128, kMid128x128, kBlock128x256, kBlock256x256 };
+hipError_t launch_mid(const A8Args& a, Shape shape, hipStream_t stream);
+hipError_t launch_block(const A8Args& a, Shape shape, hipStream_t stream);
 
 }  // namespace a8
 }  // namespace mxfp4

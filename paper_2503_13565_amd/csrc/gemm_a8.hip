@@ -149,7 +149,7 @@ hipError_t launch(const A8Args& a, hipStream_t stream)
     constexpr int BM = WM * MF * 16, BN = WN * NF * 16;
     const int nblk = a.k >> 5, lds = rows_fixed(WK, MF, NF, XR, BN, D) + rows_scales(BN, nblk) + rows_scales(XR, nblk);
     if (lds > 160 * 1024)                                       // (a K so long that the rows' scales leave no room)
-        return launch_mid(a, 3, 1, stream);
+        return launch_mid(a, kMid32x64, stream);
     static LdsLimit limit;
     const hipError_t raised = limit.raise(reinterpret_cast<const void*>(w4a8_rows_kernel<WM, WN, WK, MF, NF, XR, D>), 160 * 1024);
     if (raised != hipSuccess)
@@ -172,60 +172,90 @@ hipError_t launch(const A8Args& a, hipStream_t stream)
 
 namespace {
 
-struct Plan {
-    int shape, splits;
+// Which shape a call takes.  Up to 16 rows: the kernel with that many rows in the LDS; from nine rows on one of 16 weight rows where their blocks fit
+// the device twice (16 rows x 4096 x 4096 5.0 us, 6.8 in blocks of 32; 4096 x 11008 7.2 and 13.4), one of 32 beyond (12288 x 4096 8.3 us, 10.2;
+// 22016 x 4096 at nine rows with the gate 11.6, 16.1).  More rows: the shape whose rounds take the least.  A round (as many blocks as the device holds)
+// takes base + step for every 128 of K, in us, as measured on some seventy sizes from 17 x 23 x 128 to 4003 x 22016 x 4096: `few` with some tens of
+// blocks, `full` with one on every unit, and the last two where two fit a unit and share it.
+struct Rounds {
+    a8::Shape shape;
+    int bm, bn;
+    float base, few, full;
+    float base2, step2;
+};
+constexpr Rounds kRounds[] = {
+    {a8::kRows32, 32, 32, 1.5f, 0.085f, 0.17f, 1.0f, 0.31f},
+    {a8::kMid32x64, 32, 64, 2.9f, 0.115f, 0.17f, 1.5f, 0.28f},
+    {a8::kMid32x64Deep, 32, 64, 2.9f, 0.115f, 0.15f, 0.f, 0.f},
+    {a8::kMid64x128, 64, 128, 3.8f, 0.285f, 0.33f, 0.f, 0.f},
+    {a8::kMid128x128, 128, 128, 5.7f, 0.43f, 0.55f, 0.f, 0.f},
+    {a8::kBlock128x256, 128, 256, 7.5f, 0.745f, 0.80f, 7.0f, 1.45f},
+    {a8::kBlock256x256, 256, 256, 12.5f, 1.06f, 1.20f, 0.f, 0.f},
 };
 
-Plan plan(int64_t m, int64_t n, int64_t k, const DeviceInfo& dev)
+float time_of(const Rounds& r, int64_t blocks, float steps, int cus)
 {
-    Plan p = {m <= 1 ? 10 : m <= 4 ? 11 : m <= 16 ? 30 : m > 512 ? 0 : m > 64 ? 2 : 1, 1};
+    auto one = [&](int64_t some) { return some ? r.base + (r.few + (r.full - r.few) * (some < cus ? (float)some / cus : 1.f)) * steps : 0.f; };
+    if (r.step2 == 0.f)
+        return (float)(blocks / cus) * one(cus) + one(blocks % cus);
+    const int64_t rest = blocks % (2 * cus);
+    const float two = r.base2 + r.step2 * steps;
+    return (float)(blocks / (2 * cus)) * two + (rest > cus ? two : one(rest));
+}
+
+a8::Shape shape_of(int64_t m, int64_t n, int64_t k, const DeviceInfo& dev)
+{
     if (const char* e = knob("MXFP4_A8_SHAPE"))
-        p.shape = atoi(e);
-    if (const char* e = knob("MXFP4_A8_SPLITS"))
-        p.splits = atoi(e);
-    return p;
+        if (atoi(e) >= 0)
+            return (a8::Shape)atoi(e);
+    if (m <= 4)
+        return m == 1 ? a8::kRows1 : a8::kRows4;
+    if (m <= 8)
+        return a8::kRows8;
+    if (m <= 16)
+        return n > (int64_t)32 * dev.cus ? a8::kRows16 : m <= 12 ? a8::kRows12 : a8::kRows16Deep;
+    const float steps = (float)((k + 127) / 128);
+    a8::Shape best = a8::kBlock256x256;
+    float least = INFINITY;
+    for (const Rounds& r : kRounds) {
+        const float time = time_of(r, ((m + r.bm - 1) / r.bm) * ((n + r.bn - 1) / r.bn), steps, dev.cus);
+        if (time < least) {
+            least = time;
+            best = r.shape;
+        }
+    }
+    return best;
 }
 
 }  // namespace
 
-size_t a8_part_bytes(int64_t m, int64_t n, int64_t k, const DeviceInfo& dev)
-{
-    const Plan p = plan(m, n, k, dev);
-    return p.splits > 1 ? (size_t)p.splits * m * ((n + 255) / 256 * 256) * sizeof(float) : 0;
-}
-
 hipError_t launch_w4a8(const A8Args& a, const DeviceInfo& dev, hipStream_t stream)
 {
     using namespace a8;
-    const Plan p = plan(a.m, a.n, a.k, dev);
-    const int shape = p.shape, splits = p.splits > 1 && a.part ? p.splits : 1;
+    const Shape shape = shape_of(a.m, a.n, a.k, dev);
     switch (shape) {
-    case 0:
-        return launch_block(a, stream);
-    case 10:
+    case kRows1:
         return launch<1, 1, 8, 1, 1, 1, 3>(a, stream);
-    case 11:
+    case kRows4:
         return launch<1, 1, 8, 1, 1, 4, 3>(a, stream);
-    case 12:
-        return launch<1, 1, 8, 1, 1, 16, 3>(a, stream);
-    case 23:
-        return launch<1, 2, 4, 1, 1, 2, 3>(a, stream);
-    case 30:
+    case kRows8:
+        return launch<1, 1, 8, 1, 1, 8, 3>(a, stream);
+    case kRows12:
+        return launch<1, 1, 8, 1, 1, 12, 3>(a, stream);
+    case kRows16:
         return launch<1, 2, 4, 1, 1, 16, 2>(a, stream);
-    case 31:
-        return launch<1, 2, 4, 1, 1, 16, 3>(a, stream);
-    case 37:
-        return launch<1, 1, 8, 1, 2, 16, 2>(a, stream);
-    case 38:
-        return launch<1, 1, 8, 1, 1, 16, 2>(a, stream);
-    case 40:
-        return launch<2, 1, 4, 1, 1, 32, 3>(a, stream);
-    case 43:
-        return launch<1, 2, 4, 2, 1, 32, 3>(a, stream);
-    case 47:
-        return launch<1, 2, 4, 2, 2, 32, 3>(a, stream);
+    case kRows16Deep:
+        return launch<1, 1, 8, 1, 1, 16, 3>(a, stream);
+    case kRows32:
+        return launch<1, 2, 4, 2, 1, 32, 2>(a, stream);
+    case kMid32x64:
+    case kMid32x64Deep:
+    case kMid64x128:
+    case kMid128x128:
+        return launch_mid(a, shape, stream);
+    default:
+        return launch_block(a, shape, stream);
     }
-    return launch_mid(a, shape, splits, stream);
 }
 
 }  // namespace mxfp4

@@ -170,10 +170,7 @@ __global__ __launch_bounds__(WM * WN * 64, D == 2 ? 4 : WM * WN / 4) void w4a8_b
                 const i32x8_t B = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
                 acc[i][f] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, acc[i][f], 4, 0, decltype(f)::value, (int)h.ws,
                                                                            decltype(i)::value, (int)h.xs);
-                if constexpr (MF * NF == 16)                    // (256 sums a lane: the accumulation registers hold them, and nothing else)
-                    settle_a(acc[i][f]);
-                else
-                    settle(acc[i][f]);
+                settle(acc[i][f]);
                 if constexpr (D > 2)
                     __builtin_amdgcn_sched_barrier(0);
                 between(std::integral_constant<int, decltype(i)::value * NF + decltype(f)::value>{});
@@ -267,18 +264,9 @@ hipError_t launch(const A8Args& a, hipStream_t stream)
 
 }  // namespace
 
-hipError_t launch_block(const A8Args& a, hipStream_t stream)
+hipError_t launch_block(const A8Args& a, Shape shape, hipStream_t stream)
 {
-    if (const char* e = knob("MXFP4_A8_BLOCK"))
-        switch (atoi(e)) {
-        case 1:
-            return launch<2, 2, 4, 4, 3>(a, stream);
-        case 2:
-            return launch<2, 4, 2, 2, 2>(a, stream);
-        case 3:
-            return launch<2, 2, 2, 4, 2>(a, stream);
-        }
-    return launch<2, 4, 4, 2, 3>(a, stream);
+    return shape == kBlock128x256 ? launch<2, 4, 2, 2, 2>(a, stream) : launch<2, 4, 4, 2, 3>(a, stream);
 }
 
 }  // namespace a8

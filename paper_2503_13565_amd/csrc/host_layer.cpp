@@ -141,16 +141,13 @@ PyObject* w4a8(PyObject*, PyObject* const* args, Py_ssize_t count)
             return left();
         bias = b->data_ptr();
     }
-    at::Tensor y, ws;
+    at::Tensor y;
     int rc;
     {
         pybind11::gil_scoped_release no_gil;
         y = fresh({m, c}, at::kBFloat16, w.device);
-        const size_t spare = mxfp4_w4a8_gemm_workspace_bytes(m, n, k);
-        if (spare)
-            ws = fresh({(int64_t)spare}, at::kByte, w.device);
         rc = mxfp4_w4a8_gemm(x->data_ptr(), xs->data_ptr(), m, q->data_ptr(), s->data_ptr(), n, k, bias, act, r.at, r.ld, y.data_ptr(), c,
-                             spare ? ws.data_ptr() : nullptr, spare, w.stream);
+                             w.stream);
     }
     return finish(rc, wrap_one, &y);
     END_HANDLE_TH_ERRORS

@@ -34,10 +34,8 @@ struct A8Args {
     uint16_t* y;
     int64_t ldy, ldr;
     Epilogue epi;       // (its ldr is not used)
-    float* part;        // sums of parts of K, or null (see gemm_a8_mid.hip)
     int m, n, k;
 };
-size_t a8_part_bytes(int64_t m, int64_t n, int64_t k, const DeviceInfo& dev);
 hipError_t launch_w4a8(const A8Args& a, const DeviceInfo& dev, hipStream_t stream);
 
 // y[m] = base[m] + scale[i] * B_i (A_i x[m]) with i = ids[m]; rows with no such adapter: base[m].

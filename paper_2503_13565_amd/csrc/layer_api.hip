@@ -75,21 +75,9 @@ int mxfp4_rms_norm(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, const 
     return launched(launch_rms_norm(a, static_cast<hipStream_t>(stream)), "norm launch");
 }
 
-size_t mxfp4_w4a8_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K)
-{
-    if (M < 1 || M > kMostRows || N < 1 || N > kMostRows || K < 32 || K % 32 || K > MXFP4_MAX_K)
-        return 0;
-    DeviceInfo dev;
-    if (device_info(&dev) != MXFP4_OK) {
-        dev.cus = 256;
-        begin_call();
-    }
-    return a8_part_bytes(M, N, K, dev);
-}
-
 int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M, const void* q_packed, const void* scales_e8m0, int64_t N,
                     int64_t K, const void* bias_bf16, int act, const void* residual_bf16, int64_t ldr, void* y_bf16, int64_t ldy,
-                    void* workspace, size_t workspace_bytes, void* stream)
+                    void* stream)
 {
     begin_call();
     if (act != MXFP4_ACT_NONE && act != MXFP4_ACT_SWIGLU)
@@ -105,8 +93,8 @@ int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M, co
     if (ldy < C || (residual_bf16 && ldr < C))
         return fail(MXFP4_ERR_SHAPE, "ldy=%lld or ldr=%lld is less than %lld", (long long)ldy, (long long)ldr, (long long)C);
     if (!aligned(x_e4m3, 16) || !aligned(q_packed, 16) || !aligned(x_scales_e8m0, 4) || !aligned(scales_e8m0, 4) || !aligned(bias_bf16, 2) ||
-        !aligned(residual_bf16, 2) || !aligned(y_bf16, 2) || !aligned(workspace, 16))
-        return fail(MXFP4_ERR_ALIGN, "x, q and workspace must be 16-byte aligned, the scales 4-byte, bias, residual and y 2-byte");
+        !aligned(residual_bf16, 2) || !aligned(y_bf16, 2))
+        return fail(MXFP4_ERR_ALIGN, "x and q must be 16-byte aligned, the scales 4-byte, bias, residual and y 2-byte");
     DeviceInfo dev;
     const int rc = device_info(&dev);
     if (rc)
@@ -119,8 +107,6 @@ int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M, co
     a.y = static_cast<uint16_t*>(y_bf16);
     a.ldy = ldy;
     a.ldr = ldr;
-    const size_t need = a8_part_bytes(M, N, K, dev);
-    a.part = need && workspace && workspace_bytes >= need ? static_cast<float*>(workspace) : nullptr;
     a.epi = {static_cast<const uint16_t*>(bias_bf16), static_cast<const uint16_t*>(residual_bf16), 0, act};
     a.m = (int)M;
     a.n = (int)N;

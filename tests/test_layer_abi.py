@@ -27,15 +27,15 @@ def test_norm_refusals(what, code):
     assert code == NONE or binding.load().mxfp4_last_error()
 
 
-def product(x=P, xs=P, m=4, q=P, s=P, n=8, k=64, bias=None, act=0, r=None, ldr=8, y=P, ldy=8, ws=None):
-    return binding.load().mxfp4_w4a8_gemm(x, xs, m, q, s, n, k, bias, act, r, ldr, y, ldy, ws, 0, None)
+def product(x=P, xs=P, m=4, q=P, s=P, n=8, k=64, bias=None, act=0, r=None, ldr=8, y=P, ldy=8):
+    return binding.load().mxfp4_w4a8_gemm(x, xs, m, q, s, n, k, bias, act, r, ldr, y, ldy, None)
 
 
 @pytest.mark.parametrize("what,code", [
     (dict(m=0), SHAPE), (dict(n=0), SHAPE), (dict(k=0), SHAPE), (dict(k=48), SHAPE), (dict(k=131072), SHAPE), (dict(act=2), ARG), (dict(act=1, n=7), SHAPE),
     (dict(x=None), NULL), (dict(xs=None), NULL), (dict(q=None), NULL), (dict(s=None), NULL), (dict(y=None), NULL),
     (dict(ldy=7), SHAPE), (dict(r=P, ldr=7), SHAPE), (dict(act=1, ldy=3), SHAPE), (dict(x=P8), ALIGN), (dict(q=P8), ALIGN), (dict(xs=P2), ALIGN),
-    (dict(s=P2), ALIGN), (dict(ws=P8), ALIGN), (dict(y=ctypes.c_void_p(4097)), ALIGN), (dict(bias=ctypes.c_void_p(4097)), ALIGN), (dict(r=ctypes.c_void_p(4097)), ALIGN),
+    (dict(s=P2), ALIGN), (dict(y=ctypes.c_void_p(4097)), ALIGN), (dict(bias=ctypes.c_void_p(4097)), ALIGN), (dict(r=ctypes.c_void_p(4097)), ALIGN),
 ])
 def test_product_refusals(what, code):
     assert product(**what) == code and binding.load().mxfp4_last_error()
