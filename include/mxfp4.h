@@ -450,7 +450,7 @@ int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M,
  * A_i x, the scaling and the sum are FP32 (A_i x meets B_i as two BF16 numbers, 16 bits together), one rounding to BF16.  Rows whose id is outside
  * [0, adapters) belong to no adapter: they get base[m] (zeros without a base), and where y is base they are left as they are.  A row
  * meets its own adapter only: what others hold (NaN, infinities) does not reach it.
- *   x_bf16     in  BF16 [M, K], row stride ldx, at most 2^23
+ *   x_bf16     in  BF16 [M, K], row stride ldx
  *   a_bf16     in  BF16 [adapters, R, K], b_bf16 BF16 [adapters, N, R] (contiguous; an adapter of smaller rank is padded with zeros)
  *   ids        in  int32 [M] (device); any order, any number of rows of one adapter
  *   scales_f32 in  FP32 [adapters] (device), or NULL (1)
@@ -460,7 +460,8 @@ int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M,
  *   workspace  mxfp4_lora_workspace_bytes(M, K, R) bytes, 16-byte aligned, contents unspecified before and after; calls that overlap in
  *              time must not share it
  * K, N and R multiples of 8, R at most 128 (a larger rank: two calls, the second with y as its base), K at most MXFP4_MAX_K; x, base and y
- * 16-byte aligned with row strides that are multiples of 8.  M may be 0 (no-op).  The summation order follows from the sizes.
+ * 16-byte aligned with row strides that are multiples of 8 and at most 2^23.  M may be 0 (no-op).  The summation order follows from the
+ * sizes.
  */
 size_t mxfp4_lora_workspace_bytes(int64_t M, int64_t K, int64_t R);
 int mxfp4_lora(const void* x_bf16, int64_t M, int64_t ldx, const void* a_bf16, const void* b_bf16,

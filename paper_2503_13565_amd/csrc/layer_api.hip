@@ -24,7 +24,7 @@ static int check_rows(const void* p, int64_t ld, int64_t k, const char* what)
     return MXFP4_OK;
 }
 
-constexpr int64_t kMostRows = 0x7FFFFF00, kMostStride = 1 << 23;     // (64 rows of x are within reach of a 31-bit offset)
+constexpr int64_t kMostRows = 0x7FFFFF00, kMostStride = 1 << 23;     // (64 rows are within reach of a 31-bit offset)
 
 }  // namespace mxfp4
 
@@ -142,8 +142,9 @@ int mxfp4_lora(const void* x_bf16, int64_t M, int64_t ldx, const void* a_bf16, c
     if ((rc = check_rows(x_bf16, ldx, K, "x")) || (base_bf16 && (rc = check_rows(base_bf16, ldb, N, "base"))) ||
         (rc = check_rows(y_bf16, ldy, N, "y")))
         return rc;
-    if (ldx > kMostStride)
-        return fail(MXFP4_ERR_SHAPE, "ldx=%lld is more than %lld", (long long)ldx, (long long)kMostStride);
+    const int64_t most = ldx > ldy ? ldx : ldy;
+    if (most > kMostStride || (base_bf16 && ldb > kMostStride))
+        return fail(MXFP4_ERR_SHAPE, "a row stride of %lld is more than %lld", (long long)(most > kMostStride ? most : ldb), (long long)kMostStride);
     if (base_bf16 == y_bf16 && ldb != ldy)
         return fail(MXFP4_ERR_ARG, "base is y with another row stride");
     if (!aligned(a_bf16, 16) || !aligned(b_bf16, 16) || !aligned(ids, 4) || !aligned(scales_f32, 4) || !aligned(workspace, 16))
@@ -164,7 +165,7 @@ int mxfp4_lora(const void* x_bf16, int64_t M, int64_t ldx, const void* a_bf16, c
     a.y = static_cast<uint16_t*>(y_bf16);
     a.part = static_cast<float*>(workspace);
     a.ldx = ldx;
-    a.ldb = ldb;
+    a.ldb = base_bf16 ? ldb : 0;
     a.ldy = ldy;
     a.m = (int)M;
     a.n = (int)N;

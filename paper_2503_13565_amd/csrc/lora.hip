@@ -1,15 +1,20 @@
 // Low-rank adapters of many requests beside a shared projection:  y[m] = base[m] + scale[i] * B_i (A_i x[m]),  i = ids[m].
 //
-// Two launches.  Both give a workgroup rows of one adapter at a time, as the columns of v_mfma_f32_16x16x32_bf16: what another request's adapter
-// holds (NaN, infinities) never meets a row, and rows may lie in any order.  Below 512 rows a workgroup has an adapter (grid z) and collects
-// its rows from all of the call, so that an adapter's matrices are read once whatever the order; from 512 rows on, where reading all ids would
-// cost more than it saves, it has 16 RT rows side by side and goes through the adapters among them.
+// The products give a workgroup rows of one adapter at a time, as the columns of v_mfma_f32_16x16x32_bf16: what another request's adapter holds
+// (NaN, infinities) never meets a row, and rows may lie in any order.  Below 512 rows a workgroup has an adapter (grid z) and collects its rows from
+// all of the call, so that an adapter's matrices are read once whatever the order (96 rows of 60 adapters at 4096 -> 12288, rank 32: 17 us, and 47
+// with tiles of neighbouring rows); from 512 rows on, where reading all ids would cost more than it saves, it has 16 RT rows side by side and goes
+// through the adapters among them.
 //   shrink  t = A_i x for a part of K (grid y).  Rows of x and of A_i come into the LDS a phase of elements at a time by loads that write it directly,
 //           D - 1 phases ahead, up to 512 bytes of a row side by side (in the layout of the matrix instruction a load touches a line per lane, and a
 //           unit gets 38 bytes a ns instead of up to 150).  The waves that share a phase's elements add their sums in wave order; the parts' sums
 //           lie in the workspace in FP32, side by side.
-//   expand  adds the parts in order, scales t and cuts it into two BF16 numbers (together 16 bits, so that t's rounding does not show beside that of
-//           y), multiplies with B_i's rows, which are one piece of memory, and adds the base to the FP32 sums: one rounding.
+//   sum     adds the parts in order, scales t and cuts it into two BF16 numbers (together 16 bits, so that t's rounding does not show beside that
+//           of y).  Below 512 rows the next step does it: a launch costs more than doing it several times.
+//   expand  multiplies with B_i's rows, which are one piece of memory, and adds the base to the FP32 sums: one rounding.
+// 5003 rows of five adapters, 8192 -> 8192, rank 64: shrink 30 us (x alone is 17 at a copy's rate), sum 5, expand 48 (base and y: 33).  The products
+// by themselves are 25 us of the last, loads and stores 36: they overlap in part.  No gain: 16 or 64 rows a workgroup, two walks or eight, three
+// phases ahead in one workgroup a unit, t's sums in every workgroup of expand (61 us), a whole line of a row an instruction.
 #include "cast_block8.h"
 #include "gemm_a8.h"
 
@@ -21,7 +26,6 @@ using a8::direct;
 using a8::kOob;
 using a8::lds_address;
 using a8::past;
-using a8::turn;
 using a8::words;
 
 __device__ __forceinline__ bf16x8_t load8(const void* p) { return __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const u32x4_t*>(p)); }
@@ -35,7 +39,6 @@ __device__ __forceinline__ u32x4_t words16(const uint16_t* p, int64_t bytes)
     return words(reinterpret_cast<const uint8_t*>(p), (int)min(bytes, (int64_t)0x7FFFFF00));
 }
 
-constexpr int kRanks = 128;             // the largest rank of a call
 constexpr int kLoraSplits = 8;          // parts of K
 
 // The adapter of each of the tile's 16 RT rows, in the lane of its number; -1: none.
@@ -190,128 +193,142 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(LoraArgs a, int k_part
     }
 }
 
+// Four ranks of t: their parts added in order, scaled, and cut into two BF16 numbers each: the four upper ones, the four lower ones.
+__device__ __forceinline__ u32x4_t sum_of(const LoraArgs& a, int64_t at, float scale)
+{
+    f32x4_t v[kLoraSplits], t = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int p = 0; p < kLoraSplits; ++p)                       // (all loads at once; without conditions, which the compiler makes a way each of)
+        v[p] = *reinterpret_cast<const f32x4_t*>(a.part + (int64_t)min(p, a.splits - 1) * a.m * a.r + at);
+#pragma unroll
+    for (int p = 0; p < kLoraSplits; ++p)
+        t += p < a.splits ? v[p] : f32x4_t{0.f, 0.f, 0.f, 0.f};
+    t *= scale;
+    u32x4_t o;
+#pragma unroll
+    for (int e = 0; e < 4; e += 2) {
+        // cut off, not rounded: the largest numbers stay finite; an infinity leaves no rest
+        auto cut = [](float v) { return v == v ? __float_as_uint(v) >> 16 : 0x7FC0u; };
+        auto rest = [](float v) { const float d = v - __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); return d == d ? d : 0.f; };
+        o[e >> 1] = cut(t[e]) | cut(t[e + 1]) << 16;
+        o[2 + (e >> 1)] = f32_to_bf16_rne2(rest(t[e]), rest(t[e + 1]));
+    }
+    return o;
+}
+
+// From 512 rows on: t of every row in place of its first part, eight upper numbers and eight lower ones of a thread's eight ranks, so that the
+// workgroups that share a row's outputs read it once, and as the matrix instructions take it.
+__global__ __launch_bounds__(256) void lora_sum_kernel(LoraArgs a)
+{
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
+    if (at >= (int64_t)a.m * a.r)
+        return;
+    const int id = a.ids[at / a.r];
+    if (id < 0 || id >= a.adapters)
+        return;
+    const float scale = a.scales ? a.scales[id] : 1.f;
+    const u32x4_t low = sum_of(a, at, scale), high = sum_of(a, at + 4, scale);
+    *reinterpret_cast<u32x4_t*>(a.part + at) = u32x4_t{low[0], low[1], high[0], high[1]};
+    *reinterpret_cast<u32x4_t*>(a.part + at + 4) = u32x4_t{low[2], low[3], high[2], high[3]};
+}
+
 // A wave has 64 outputs of the rows at a time; a workgroup's four lie side by side.  Row 16 f + i of the matrix instructions' B is output
 // 32 (f / 2) + 8 (i / 4) + 4 (f % 2) + i % 4 of the 64: so a lane's four sums of two instructions are eight outputs side by side, 16 bytes of y,
 // and four lanes have 64 bytes of a row.
-constexpr int expand_stride(int r) { return ((r + 31) & ~31) + 8; }             // (16 bytes more: rows start in different banks)
-constexpr int expand_t(int rt, int r) { return rt * 16 * expand_stride(r) * 4; }
-constexpr int expand_lds(int rt, int r) { return expand_t(rt, r) + 4 * 128 * r; }
+constexpr int expand_stride(int kc) { return 8 * kc + 8; }                      // (16 bytes more: rows start in different banks)
+constexpr int expand_t(int kc) { return 16 * expand_stride(kc) * 4; }
 
-// LDS: t's two halves [16 RT][ranks + 8], and for each wave B's rows [64][r], chunks turned where their number is a power of two
+// KC chunks of eight ranks, 4, 8 or 16: a smaller rank is padded with zeros (loads past a row's end), so that places are shifts and no divisions.
+// LDS: below 512 rows t's two halves [16][8 KC + 8]; for each wave B's rows [64][8 KC], chunk c of row r at c ^ (r / (16 / KC) % KC).
+template <int KC>
 struct Expand {
     const LoraArgs& a;
     uint8_t* smem;
     int lane, wave;
-
-    __device__ __forceinline__ int place(int row, int c) const
-    {
-        const int chunks = a.r >> 3;
-        if (chunks & (chunks - 1))
-            return c;
-        return c ^ (chunks >= 16 ? row & 15 : row / (16 / chunks) & (chunks - 1));
-    }
+    static constexpr int kStride = expand_stride(KC), kTurn = 16 / KC;
 
     // B's rows n0 .. n0 + 63: one piece of memory, 1 KiB a load, each chunk to its place
     __device__ __forceinline__ void fetch(uint32_t to, int cur, int n0) const
     {
-        const int chunks = a.r >> 3, cols = max(min(64, a.n - n0), 0);
+        const int cols = max(min(64, a.n - n0), 0);
         const u32x4_t rb = words16(a.b + ((int64_t)cur * a.n + n0) * a.r, (int64_t)cols * a.r * 2);
-        for (int u = 0; u < chunks; ++u) {
-            const int slot = u * 64 + lane, row = slot / chunks, f = row >> 4, i = row & 15;
+#pragma unroll
+        for (int u = 0; u < KC; ++u) {
+            const int slot = u * 64 + lane, row = slot / KC, f = row >> 4, i = row & 15, c = (slot % KC) ^ (row / kTurn % KC);
             const int out = 32 * (f >> 1) + 8 * (i >> 2) + 4 * (f & 1) + (i & 3);
-            direct(to + u * 1024, (out * chunks + place(row, slot - row * chunks)) * 16, rb, 0);
+            direct(to + u * 1024, c * 8 < a.r ? out * (a.r * 2) + c * 16 : kOob, rb, 0);
         }
     }
 
-    template <int RT, class RowOf>
-    __device__ __forceinline__ void sums(float scale, int64_t m0, RowOf row_of) const
+    // t of a tile's rows
+    template <class RowOf>
+    __device__ __forceinline__ void sums(float scale, RowOf row_of) const
     {
-        const int quads = ((a.r + 31) & ~31) / 4, stride = expand_stride(a.r);
-        uint16_t *hi = reinterpret_cast<uint16_t*>(smem), *lo = hi + RT * 16 * stride;
-        for (int at = threadIdx.x; at < RT * 16 * quads; at += 256) {
-            const int j = at / quads, rank = (at - j * quads) * 4, row = row_of(j);
-            f32x4_t t = {0.f, 0.f, 0.f, 0.f};
-            if (row >= 0 && rank < a.r) {
-                const float* from = a.part + (m0 + row) * a.r + rank;
-                f32x4_t v[kLoraSplits];
-#pragma unroll
-                for (int p = 0; p < kLoraSplits; ++p)
-                    if (p < a.splits)
-                        v[p] = *reinterpret_cast<const f32x4_t*>(from + (int64_t)p * a.m * a.r);
-#pragma unroll
-                for (int p = 0; p < kLoraSplits; ++p)
-                    if (p < a.splits)
-                        t += v[p];
-                t *= scale;
-            }
-            u32x2_t h, l;
-#pragma unroll
-            for (int e = 0; e < 4; e += 2) {
-                // cut off, not rounded: the largest numbers stay finite; an infinity leaves no rest
-                auto cut = [](float v) { return v == v ? __float_as_uint(v) >> 16 : 0x7FC0u; };
-                auto rest = [](float v) { const float d = v - __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); return d == d ? d : 0.f; };
-                h[e >> 1] = cut(t[e]) | cut(t[e + 1]) << 16;
-                l[e >> 1] = f32_to_bf16_rne2(rest(t[e]), rest(t[e + 1]));
-            }
-            *reinterpret_cast<u32x2_t*>(hi + j * stride + rank) = h;
-            *reinterpret_cast<u32x2_t*>(lo + j * stride + rank) = l;
+        uint16_t *hi = reinterpret_cast<uint16_t*>(smem), *lo = hi + 16 * kStride;
+        for (int at = threadIdx.x; at < 16 * 2 * KC; at += 256) {
+            const int j = at / (2 * KC), rank = at % (2 * KC) * 4, row = row_of(j);
+            const u32x4_t t = row >= 0 && rank < a.r ? sum_of(a, (int64_t)row * a.r + rank, scale) : u32x4_t{0, 0, 0, 0};
+            *reinterpret_cast<u32x2_t*>(hi + j * kStride + rank) = u32x2_t{t[0], t[1]};
+            *reinterpret_cast<u32x2_t*>(lo + j * kStride + rank) = u32x2_t{t[2], t[3]};
         }
     }
 
-    // This lane's outputs of the rows: 16 i + lane % 16, outputs n .. n + 7 and n + 32 .. n + 39, n = n0 + 8 (lane / 16)
-    template <int RT, class RowOf>
-    __device__ __forceinline__ void load(u32x4_t (&base)[RT][2], int64_t m0, int n0, RowOf row_of) const
+    // This lane's outputs of the rows: 16 i + lane % 16, outputs n .. n + 7 and n + 32 .. n + 39, n = n0 + 8 (lane / 16).  Buffer instructions, which
+    // leave out what lies past a descriptor's end: a condition would be a branch each, with a wait for its load at its end.
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const uint16_t* p, int64_t ld, int rows) const
     {
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const int row = row_of(16 * i + (lane & 15)), n = n0 + 8 * (lane >> 4);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                base[i][h] = u32x4_t{0, 0, 0, 0};
-                if (a.base && row >= 0 && n + 32 * h < a.n)
-                    base[i][h] = *reinterpret_cast<const u32x4_t*>(a.base + (m0 + row) * a.ldb + n + 32 * h);
-            }
-        }
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(p), 0, p ? (int)(rows * ld * 2) : 0, 0x00020000);
     }
 
-    template <int RT, class RowOf>
-    __device__ __forceinline__ void store(const u32x4_t (&v)[RT][2], int64_t m0, int n0, RowOf row_of) const
-    {
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const int row = row_of(16 * i + (lane & 15)), n = n0 + 8 * (lane >> 4);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-                if (row >= 0 && n + 32 * h < a.n)
-                    *reinterpret_cast<u32x4_t*>(a.y + (m0 + row) * a.ldy + n + 32 * h) = v[i][h];
-        }
-    }
+    __device__ __forceinline__ int offset(int row, int64_t ld) const { return row >= 0 ? row * (int)(ld * 2) : kOob; }
 
-    // v + t B, B's rows at `b` in the LDS
     template <int RT>
-    __device__ __forceinline__ void product(u32x4_t (&v)[RT][2], const uint8_t* b) const
+    __device__ __forceinline__ void load(u32x4_t (&v)[RT][2], __amdgpu_buffer_rsrc_t base, int n0, const int (&off)[RT]) const
     {
-        const int li = lane & 15, lg = lane >> 4, chunks = a.r >> 3, stride = expand_stride(a.r);
-        const uint16_t *hi = reinterpret_cast<const uint16_t*>(smem), *lo = hi + RT * 16 * stride;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int n = n0 + 32 * h + 8 * (lane >> 4);
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+                v[i][h] = __builtin_amdgcn_raw_buffer_load_b128(base, n < a.n ? (int)((uint32_t)off[i] + n * 2) : kOob, 0, 0);
+        }
+    }
+
+    template <int RT>
+    __device__ __forceinline__ void store(const u32x4_t (&v)[RT][2], __amdgpu_buffer_rsrc_t y, int n0, const int (&off)[RT]) const
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int n = n0 + 32 * h + 8 * (lane >> 4);
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+                __builtin_amdgcn_raw_buffer_store_b128(v[i][h], y, n < a.n ? (int)((uint32_t)off[i] + n * 2) : kOob, 0, 0);
+        }
+    }
+
+    // out = v + t B, B's rows at `b` in the LDS; t's numbers of row 16 i + lane % 16 and ranks 32 q + 8 (lane / 16) .. + 7: ranks_of(i, q, upper or lower)
+    template <int RT, class RanksOf>
+    __device__ __forceinline__ void product(u32x4_t (&out)[RT][2], const u32x4_t (&v)[RT][2], const uint8_t* b, RanksOf ranks_of) const
+    {
+        const int li = lane & 15, lg = lane >> 4;
         f32x4_t acc[RT][4] = {};
-        for (int kk = 0; kk < a.r; kk += 32) {
+#pragma unroll
+        for (int q = 0; q < KC / 4; ++q) {
             bf16x8_t w[4];
 #pragma unroll
             for (int f = 0; f < 4; ++f) {
-                const int row = 16 * f + li, c = (kk >> 3) + lg;
-                w[f] = load8(b + (row * chunks + place(row, min(c, chunks - 1))) * 16);     // (past the rank, t is zero; infinities are not multiplied with it)
-                if (c >= chunks)
-                    w[f] = bf16x8_t{};
+                const int row = 16 * f + li;
+                w[f] = load8(b + (row * KC + ((4 * q + lg) ^ (row / kTurn % KC))) * 16);
             }
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                const bf16x8_t th = load8(hi + (i * 16 + li) * stride + kk + 8 * lg), tl = load8(lo + (i * 16 + li) * stride + kk + 8 * lg);
+            for (int part = 1; part >= 0; --part)               // (the lower numbers first: small before large)
 #pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[f], tl, acc[i][f], 0, 0, 0);
-                    acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[f], th, acc[i][f], 0, 0, 0);
+                for (int i = 0; i < RT; ++i) {
+                    const bf16x8_t t = ranks_of(i, q, part);
+#pragma unroll
+                    for (int f = 0; f < 4; ++f)
+                        acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[f], t, acc[i][f], 0, 0, 0);
                 }
-            }
         }
 #pragma unroll
         for (int i = 0; i < RT; ++i)
@@ -321,18 +338,24 @@ struct Expand {
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const uint32_t o = v[i][f >> 1][2 * (f & 1) + e];
-                    v[i][f >> 1][2 * (f & 1) + e] = f32_to_bf16_rne2(__uint_as_float(o << 16) + acc[i][f][2 * e], __uint_as_float(o & 0xFFFF0000u) + acc[i][f][2 * e + 1]);
+                    out[i][f >> 1][2 * (f & 1) + e] = f32_to_bf16_rne2(__uint_as_float(o << 16) + acc[i][f][2 * e], __uint_as_float(o & 0xFFFF0000u) + acc[i][f][2 * e + 1]);
                 }
             }
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                asm volatile("" : "+v"(out[i][h]));             // (here, not behind the loads of the next v)
     }
 };
 
 // Below 512 rows: grid z an adapter, x 256 outputs of one of its tiles of 16 rows (and every gridDim.y-th), y the tile.  B's rows stay for all tiles.
+template <int KC>
 __global__ __launch_bounds__(256, 4) void lora_expand_few_kernel(LoraArgs a)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Expand e{a, smem + kListBytes, (int)threadIdx.x & 63, wave};
+    const Expand<KC> e{a, smem + kListBytes, (int)threadIdx.x & 63, wave};
     uint16_t* list = reinterpret_cast<uint16_t*>(smem);
     int cur;
     const int count = collect(a, (int)blockIdx.z + 1 < (int)gridDim.z ? (int)blockIdx.z : -1, e.lane, list, cur);
@@ -340,98 +363,125 @@ __global__ __launch_bounds__(256, 4) void lora_expand_few_kernel(LoraArgs a)
     int first = (int)blockIdx.y * 16;
     if (first >= count || (cur < 0 && a.base == a.y))
         return;
-    const int own = expand_t(1, a.r) + wave * (128 * a.r);
+    const int own = expand_t(KC) + wave * (1024 * KC);
     if (cur >= 0)
         e.fetch(lds_address(e.smem) + own, cur, n0);
     const float scale = a.scales && cur >= 0 ? a.scales[cur] : 1.f;
+    const auto base = e.rows_of(a.base, a.ldb, a.m), y = e.rows_of(a.y, a.ldy, a.m);
     __syncthreads();
     for (bool next = false; first < count; first += (int)gridDim.y * 16, next = true) {
         auto row_of = [&](int j) { return first + j < count ? (int)list[first + j] : -1; };
-        u32x4_t v[1][2];
-        e.load<1>(v, 0, n0, row_of);
+        const int row = row_of(e.lane & 15), from[1] = {e.offset(row, a.ldb)}, to[1] = {e.offset(row, a.ldy)};
+        u32x4_t v[1][2], out[1][2];
+        e.load(v, base, n0, from);
         if (cur >= 0) {
             if (next)
                 __syncthreads();                                // (t has been read)
-            e.sums<1>(scale, 0, row_of);
+            e.sums(scale, row_of);
             drain_vmem();
             __syncthreads();
-            e.product<1>(v, e.smem + own);
+            e.product(out, v, e.smem + own, [&](int, int q, int part) {
+                return load8(reinterpret_cast<const uint16_t*>(e.smem) + (16 * part + (e.lane & 15)) * e.kStride + 32 * q + 8 * (e.lane >> 4));
+            });
         }
-        e.store<1>(v, 0, n0, row_of);
+        e.store(cur >= 0 ? out : v, y, n0, to);
     }
 }
 
 // Grid x: `walks` times 256 outputs, those of 16 RT rows side by side, then the next rows' (a piece of B stays with a die); the adapters among the rows are
 // shared out over grid z.
-template <int RT>
-__global__ __launch_bounds__(256, RT == 4 ? 2 : 4) void lora_expand_kernel(LoraArgs a, int walks, int chunks)
+template <int KC, int RT>
+__global__ __launch_bounds__(256, KC == 16 ? 2 : 3) void lora_expand_kernel(LoraArgs a, int walks, int chunks)
 {
     extern __shared__ __align__(16) uint8_t smem[];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Expand e{a, smem, (int)threadIdx.x & 63, wave};
+    const Expand<KC> e{a, smem, (int)threadIdx.x & 63, wave};
     const int64_t m0 = (int64_t)(blockIdx.x / chunks) * (16 * RT);
     const int rows = (int)min((int64_t)16 * RT, a.m - m0);
     const int id = tile_ids(a, m0, rows, e.lane);
-    const int own = expand_t(RT, a.r) + wave * (128 * a.r);
+    const int own = wave * (1024 * KC);
     const uint64_t some = __ballot(id >= 0);
     const uint64_t none = blockIdx.z == 0 && a.base != a.y ? __ballot(id < 0 && e.lane < rows) : 0;    // rows of no adapter: the base as it is
-    bool used = false;                                          // whether the LDS has been written
-    int has = -1;                                               // whose t it holds
-    for (int walk = 0; walk < walks; ++walk) {
-        const int n0 = (((int)(blockIdx.x % chunks) * walks + walk) * 4 + wave) * 64;
-        u32x4_t v[RT][2];
-        if (none) {
-            auto row_of = [&](int j) { return none >> j & 1 ? j : -1; };
-            e.load<RT>(v, m0, n0, row_of);
-            e.store<RT>(v, m0, n0, row_of);
+    const auto output = [&](int walk) { return (((int)(blockIdx.x % chunks) * walks + walk) * 4 + wave) * 64; };
+    const auto base = e.rows_of(a.base ? a.base + m0 * a.ldb : nullptr, a.ldb, rows), y = e.rows_of(a.y + m0 * a.ldy, a.ldy, rows);
+    u32x4_t v[RT][2], out[RT][2];
+    int from[RT], to[RT];
+    const auto take = [&](uint64_t mine) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int row = mine >> (16 * i + (e.lane & 15)) & 1 ? 16 * i + (e.lane & 15) : -1;
+            from[i] = e.offset(row, a.ldb);
+            to[i] = e.offset(row, a.ldy);
         }
-        uint64_t todo = some;
-        for (int nth = 0; todo; ++nth) {
-            const int cur = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
-            const uint64_t mine = __ballot(id == cur);
-            todo &= ~mine;
-            if (nth % (int)gridDim.z != (int)blockIdx.z)
-                continue;
-            auto row_of = [&](int j) { return mine >> j & 1 ? j : -1; };
-            e.load<RT>(v, m0, n0, row_of);
-            if (used)
-                __syncthreads();                                // (it has been read)
-            used = true;
-            e.fetch(lds_address(smem) + own, cur, n0);
-            if (has != cur)                                     // (one adapter all walks long: t is there)
-                e.sums<RT>(a.scales ? a.scales[cur] : 1.f, m0, row_of);
-            has = cur;
-            drain_vmem();
-            __syncthreads();
-            e.product<RT>(v, smem + own);
-            e.store<RT>(v, m0, n0, row_of);
+    };
+    take(none);
+    for (int walk = 0; none && walk < walks; ++walk) {
+        e.load(v, base, output(walk), from);
+        e.store(v, y, output(walk), to);
+    }
+    if (!some)
+        return;
+    // t of all rows: what a row is of another adapter than the one whose B is multiplied meets no row of that one.
+    const auto sums = __builtin_amdgcn_make_buffer_rsrc(a.part + m0 * a.r, 0, rows * a.r * 4, 0x00020000);
+    bf16x8_t t[RT][KC / 4][2];
+    uint64_t todo = some;
+    bool first = true;
+    for (int nth = 0; todo; ++nth) {
+        const int cur = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
+        const uint64_t mine = __ballot(id == cur);
+        todo &= ~mine;
+        if (nth % (int)gridDim.z != (int)blockIdx.z)
+            continue;
+        take(mine);
+        e.fetch(lds_address(smem) + own, cur, output(0));
+        e.load(v, base, output(0), from);
+        if (first) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int q = 0; q < KC / 4; ++q)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        const int row = 16 * i + (e.lane & 15), rank = 32 * q + 8 * (e.lane >> 4);
+                        t[i][q][part] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(sums, rank < a.r ? (row * a.r + rank + 4 * part) * 4 : kOob, 0, 0));
+                    }
+            first = false;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // The next outputs' rows of B and base are on their way before this walk's outputs leave, and the wait for them does not wait for the stores.
+        for (int walk = 0; walk < walks; ++walk) {
+            e.product(out, v, smem + own, [&](int i, int q, int part) { return t[i][q][part]; });
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's part has been read)
+            if (walk + 1 < walks) {
+                e.fetch(lds_address(smem) + own, cur, output(walk + 1));
+                e.load(v, base, output(walk + 1), from);
+            }
+            e.store(out, y, output(walk), to);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * RT) : "memory");
         }
     }
 }
 
-#ifndef LORA_ET
-#define LORA_ET 2
-#endif
-constexpr int kExpandTiles = LORA_ET;
 
-// Workgroups of a grid are limited, and so is the reach of an offset into x: very many rows, and rows very far apart, are several pairs of launches.
+// Workgroups of a grid are limited, and so is the reach of an offset into x, base and y: very many rows, and rows very far apart, are several pairs of launches.
 template <int RT, int RG, int WK, int D, bool kFew>
 hipError_t launch(LoraArgs a, hipStream_t stream)
 {
-    constexpr int ET = kFew ? 1 : kExpandTiles;
+    constexpr int KC = RG <= 2 ? 4 : RG <= 4 ? 8 : 16, ET = kFew ? 1 : 2;
     static LdsLimit shrink, expand;
-    const int list = kFew ? kListBytes : 0, shrink_bytes = shrink_lds(RT, RG, WK, D) + list, expand_bytes = expand_lds(ET, a.r) + list;
+    const int list = kFew ? kListBytes : 0, shrink_bytes = shrink_lds(RT, RG, WK, D) + list, expand_bytes = 4 * 1024 * KC + (kFew ? list + expand_t(KC) : 0);
     const void* second;
     if constexpr (kFew)
-        second = reinterpret_cast<const void*>(lora_expand_few_kernel);
+        second = reinterpret_cast<const void*>(lora_expand_few_kernel<KC>);
     else
-        second = reinterpret_cast<const void*>(lora_expand_kernel<ET>);
+        second = reinterpret_cast<const void*>(lora_expand_kernel<KC, ET>);
     hipError_t e = shrink.raise(reinterpret_cast<const void*>(lora_shrink_kernel<RT, RG, WK, D, kFew>), shrink_bytes);
     if (e == hipSuccess)
-        e = expand.raise(second, expand_lds(ET, kRanks) + list);
+        e = expand.raise(second, expand_bytes);
     const int k_part = ((a.k + a.splits - 1) / a.splits + phase_of(WK) - 1) / phase_of(WK) * phase_of(WK);
-    const int walks = !kFew && a.n >= 2048 ? 4 : 1, step = 256 * walks, chunks = (int)(((int64_t)a.n + step - 1) / step);
-    const int64_t all = a.m, most = kFew ? min(all, ((int64_t)1 << 29) / a.ldx) : max((1 << 21) / chunks, 1) * (16 * RT * ET);
+    const int64_t pieces = ((int64_t)a.m + 16 * ET - 1) / (16 * ET) * (((int64_t)a.n + 255) / 256);
+    const int walks = kFew ? 1 : (int)min(max(pieces / 768, (int64_t)1), (int64_t)4), step = 256 * walks, chunks = (int)(((int64_t)a.n + step - 1) / step);
+    const int64_t all = a.m, most = kFew ? min(all, ((int64_t)1 << 29) / max(a.ldx, max(a.ldb, a.ldy))) : max((1 << 21) / chunks, 1) * (16 * RT * ET);
     for (int64_t at = 0; at < all && e == hipSuccess; at += most) {
         LoraArgs b = a;
         b.m = (int)min(all - at, most);
@@ -443,11 +493,13 @@ hipError_t launch(LoraArgs a, hipStream_t stream)
         if constexpr (kFew) {
             const int groups = min(a.adapters, b.m), share = min(tiles, (2 * tiles + groups - 1) / groups);
             lora_shrink_kernel<RT, RG, WK, D, true><<<dim3(share, a.splits, groups), 512, shrink_bytes, stream>>>(b, k_part);
-            lora_expand_few_kernel<<<dim3(chunks, share, groups + 1), 256, expand_bytes, stream>>>(b);
+            lora_expand_few_kernel<KC><<<dim3(chunks, share, groups + 1), 256, expand_bytes, stream>>>(b);
         } else {
-            const int slots = min(a.adapters, 2), wide = (b.m + ET * 16 - 1) / (ET * 16);
-            lora_shrink_kernel<RT, RG, WK, D, false><<<dim3(tiles, a.splits, slots), 512, shrink_bytes, stream>>>(b, k_part);
-            lora_expand_kernel<ET><<<dim3(wide * chunks, 1, slots), 256, expand_bytes, stream>>>(b, walks, chunks);
+            const int wide = (b.m + ET * 16 - 1) / (ET * 16);
+            const auto slots = [&](int64_t others) { return (int)max(min(min((int64_t)a.adapters, (int64_t)16), 1024 / others), (int64_t)1); };
+            lora_shrink_kernel<RT, RG, WK, D, false><<<dim3(tiles, a.splits, slots((int64_t)tiles * a.splits)), 512, shrink_bytes, stream>>>(b, k_part);
+            lora_sum_kernel<<<(unsigned)(((int64_t)b.m * (a.r / 8) + 255) / 256), 256, 0, stream>>>(b);
+            lora_expand_kernel<KC, ET><<<dim3(wide * chunks, 1, slots((int64_t)wide * chunks)), 256, expand_bytes, stream>>>(b, walks, chunks);
         }
         e = hipGetLastError();
     }

@@ -279,6 +279,33 @@ def test_adapters_strides():
         binding.mxfp4_lora(x, a, b, ids, base=base, workspace=ws[:64])
 
 
+@pytest.mark.parametrize("m,ldx,ldb,ldy", [(140, 1 << 22, 72, 1 << 23), (300, 264, 1 << 21, 72), (520, 1 << 21, 1 << 22, 1 << 20)])
+def test_adapters_of_rows_far_apart(m, ldx, ldb, ldy):
+    """Offsets past 2^31 bytes, several launches below 512 rows."""
+    n, k, rank = 72, 264, 24
+    x, base = _bf16((m, k), 3), _bf16((m, n), 4)
+    a, b, scales = _stack(4, rank, n, k, 5)
+    ids = _ids(m, 4, "mixed", 6)
+    far = []
+    for t, ld in ((x, ldx), (base, ldb), (torch.zeros_like(base), ldy)):
+        far.append(torch.empty((m - 1) * ld + t.shape[1], dtype=torch.bfloat16, device=DEV).as_strided(t.shape, (ld, 1)))
+        far[-1].copy_(t)
+    binding.mxfp4_lora(far[0], a, b, ids, base=far[1], scales=scales, y=far[2])
+    plain.near(far[2], *plain.adapters(x, a, b, ids, base, scales))
+
+
+def test_adapters_of_every_row_its_own_and_of_one():
+    """More adapters than rows, each used once, from the last on; then all rows of one among many."""
+    n, k, rank, many = 264, 520, 16, 700
+    for m in (300, 600):
+        x, base = _bf16((m, k), 3), _bf16((m, n), 4)
+        a, b, scales = _stack(many, rank, n, k, 5)
+        ids = (many - 1 - torch.arange(m, dtype=torch.int32)).to(DEV)
+        plain.near(binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales), *plain.adapters(x, a, b, ids, base, scales))
+        ids.fill_(many - 2)
+        plain.near(binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales), *plain.adapters(x, a, b, ids, base, scales))
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------
 
 def _layer(x, r, w, q, s, a, b, ids, scales):
