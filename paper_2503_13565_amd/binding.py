@@ -81,7 +81,7 @@ def _kv_host():
 
 class _Layer:
     """The extension's calls of what surrounds a layer's products, in the same way."""
-    rms_norm = w4a8 = lora = staticmethod(lambda *args: None)
+    rms_norm = w4a8 = lora = e4m3_dequant = staticmethod(lambda *args: None)
 
 
 _layer = None
@@ -303,7 +303,7 @@ def _host_calls():
         append, read, attention, pages, compact = _host.kv_append, _host.kv_read, _host.kv_attention, _host.kv_pages, _host.kv_compact
 
     class layer(_Layer):
-        rms_norm, w4a8, lora = _host.rms_norm, _host.w4a8, _host.lora
+        rms_norm, w4a8, lora, e4m3_dequant = _host.rms_norm, _host.w4a8, _host.lora, _host.e4m3_dequant
     return _host.product, _host.verify, _host.cast, kv, layer
 
 
@@ -552,6 +552,9 @@ def mxfp4_e4m3_direct_cast(w: torch.Tensor, integer_rule: bool = False) -> Tuple
 
 
 def mxfp4_e4m3_dequant(q8: torch.Tensor, s: torch.Tensor) -> torch.Tensor:
+    w = _layer_host().e4m3_dequant(q8, s)
+    if w is not None:
+        return w
     _dev(q8)
     n, k = q8.shape
     w = torch.empty((n, k), dtype=torch.bfloat16, device=q8.device)

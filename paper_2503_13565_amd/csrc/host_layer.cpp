@@ -114,6 +114,33 @@ PyObject* rms_norm(PyObject*, PyObject* const* args, Py_ssize_t count)
     END_HANDLE_TH_ERRORS
 }
 
+// e4m3_dequant(q8, s) -> w, or None
+PyObject* e4m3_dequant(PyObject*, PyObject* const* args, Py_ssize_t count)
+{
+    HANDLE_TH_ERRORS
+    if (!counted(count, 2, "e4m3_dequant"))
+        return nullptr;
+    Where w;
+    if (!where(args[0], &w))
+        return left();
+    const at::Tensor* q = plain(args[0], at::kByte, w.device);
+    if (!q || q->dim() != 2 || !q->is_contiguous())
+        return left();
+    const int64_t m = q->size(0), k = q->size(1);
+    const at::Tensor* s = m < 1 || k < 32 || k % 32 ? nullptr : whole_of(args[1], at::kByte, w.device, m, k / 32);
+    if (!s)
+        return left();
+    at::Tensor y;
+    int rc;
+    {
+        pybind11::gil_scoped_release no_gil;
+        y = fresh({m, k}, at::kBFloat16, w.device);
+        rc = mxfp4_e4m3_dequant(q->data_ptr(), s->data_ptr(), m, k, y.data_ptr(), k, w.stream);
+    }
+    return finish(rc, wrap_one, &y);
+    END_HANDLE_TH_ERRORS
+}
+
 // w4a8(x8, xs, q, s, bias, act, residual) -> y, or None
 PyObject* w4a8(PyObject*, PyObject* const* args, Py_ssize_t count)
 {
@@ -202,6 +229,7 @@ PyMethodDef layer_methods[] = {
     {"rms_norm", (PyCFunction)(void (*)(void))rms_norm, METH_FASTCALL, nullptr},
     {"w4a8", (PyCFunction)(void (*)(void))w4a8, METH_FASTCALL, nullptr},
     {"lora", (PyCFunction)(void (*)(void))lora, METH_FASTCALL, nullptr},
+    {"e4m3_dequant", (PyCFunction)(void (*)(void))e4m3_dequant, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

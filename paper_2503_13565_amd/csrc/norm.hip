@@ -63,21 +63,24 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rms_norm_kernel(NormArgs a,
     const uint16_t* r = a.r ? a.r + row * a.ldr : nullptr;
     auto chunk = [](const uint16_t* p, int c) { return *reinterpret_cast<const u32x4_t*>(p + (int64_t)c * 8); };
 
+    // All loads at once: without conditions (a branch each, with a wait at its end), what is not there read from x and replaced.
+    const uint16_t *r_at = r ? r : x, *w_at = a.w ? a.w : x;
     float h[C][8];
-    u32x4_t w[C];
+    u32x4_t w[C], vs[C], us[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int c = min(t + i * T, chunks - 1);
+        vs[i] = chunk(x, c);
+        us[i] = chunk(r_at, c);
+        w[i] = chunk(w_at, c);
+    }
     float ss = 0.f;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        const int c = t + i * T;
-        u32x4_t v = {0, 0, 0, 0}, u = {0, 0, 0, 0};
-        w[i] = u32x4_t{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
-        if (c < chunks) {
-            v = chunk(x, c);
-            if (r)
-                u = chunk(r, c);
-            if (a.w)
-                w[i] = chunk(a.w, c);
-        }
+        const bool inside = t + i * T < chunks;
+        const u32x4_t none = {0, 0, 0, 0}, ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+        const u32x4_t v = inside ? vs[i] : none, u = inside && r ? us[i] : none;
+        w[i] = a.w ? w[i] : ones;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             h[i][2 * e] = low(v[e]);
