@@ -107,6 +107,20 @@ def test_norm_of_any_finite_row(k):
         plain.near(got.total, h, torch.where(h.isinf(), 0.0, h_off), "sum")
 
 
+@pytest.mark.parametrize("m,k", [(256, 2048), (300, 1096), (257, 4096), (264, 8192), (256, 3000), (270, 6016), (300, 10016)])
+def test_norm_of_many_rows(m, k):
+    x, r, w = _bf16((m, k), 5), _bf16((m, k), 6, 0.3), _bf16((k,), 7)
+    x[3] *= 2.0 ** 100
+    x[m - 1] *= 2.0 ** -100
+    r[m - 1] = 0
+    _check_norm(x, w, r, 1e-30, binding.mxfp4_rms_norm(x, w, residual=r, eps=1e-30))
+    got = binding.mxfp4_rms_norm(x, None, eps=1e-30, out="both" if k % 32 == 0 else "bf16")
+    _check_norm(x, None, None, 1e-30, got)
+    if k % 32 == 0:
+        code, scale = binding.mxfp4_e4m3_direct_cast(got.y)
+        assert torch.equal(got.q8, code) and torch.equal(got.s, scale)
+
+
 def test_norm_of_rows_that_are_not_finite():
     x = _bf16((4, 4096), 6).cpu()
     x[0, 7], x[1, 9], x[2, 11] = NAN, INF, -INF
@@ -146,6 +160,26 @@ def test_product(m, n, k, more):
     plain.near(y, want, off)
     again = binding.mxfp4_w4a8_gemm(x8, xs, q, s, bias=bias, act=act, residual=residual)
     assert torch.equal(y, again)
+
+
+@pytest.mark.parametrize("m,n,k", [
+    (6, 300, 1024), (8, 9002, 96), (12, 640, 544), (13, 330, 4096), (16, 8226, 416), (17, 16486, 160), (20, 8522, 1312), (35, 17294, 96), (98, 16820, 64),
+    (230, 16646, 96), (433, 16618, 2272), (1025, 8194, 4192), (2050, 4098, 1056), (5, 130, 65536), (40, 130, 65536), (300, 700, 32768), (1100, 2570, 16416)])
+@pytest.mark.parametrize("more", ["", "bias gate residual"])
+def test_product_of_every_block(m, n, k, more):
+    """Blocks of every size that a call may be cut into, with rows and columns behind the last whole block; y in the middle of something larger."""
+    x8, xs = _eight(m, k, m + k)
+    q, s = _weights(n, k, n + k)
+    c = n // 2 if more else n
+    bias, residual = (_bf16((n,), 3), _bf16((m, c), 4)) if more else (None, None)
+    act = binding.ACT_SWIGLU if more else binding.ACT_NONE
+    held = torch.full((m + 2, c + 8), NAN, dtype=torch.bfloat16, device=DEV)
+    y = held[1 : m + 1, 3 : c + 3]
+    assert binding.mxfp4_w4a8_gemm(x8, xs, q, s, bias=bias, act=act, residual=residual, y=y) is y
+    plain.near(y, *plain.product(x8, xs, q, s, bias, bool(more), residual, device=DEV))
+    assert torch.equal(binding.mxfp4_w4a8_gemm(x8, xs, q, s, bias=bias, act=act, residual=residual), y)
+    y.fill_(NAN)
+    assert bool(torch.isnan(held).all())
 
 
 @pytest.mark.parametrize("m,n,k", [(3, 40, 128), (40, 90, 1024), (300, 514, 640)])
