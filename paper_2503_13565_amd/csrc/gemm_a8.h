@@ -47,7 +47,7 @@ __device__ __forceinline__ void direct(uint32_t to, int off, const u32x4_t& r, i
 }
 
 // silu(g) * u as common.h has it, with the hardware's reciprocal (off by one step) in place of the division, whose ten instructions for every
-// output are 7 us of a prompt's 22016 x 4096.
+// output are 18 of the 337 us that 4003 rows x 22016 x 4096 took with it.
 __device__ __forceinline__ float gate_of(float g, float u) { return g * __builtin_amdgcn_rcpf(1.f + __expf(-g)) * u; }
 
 // Four finished sums of row m, weight rows n .. n + 3 (n a multiple of 4), on their way out.
