@@ -55,6 +55,12 @@ int mxfp4_rms_norm(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, const 
     if ((rc = check_rows(x_bf16, ldx, K, "x")) || (residual_bf16 && (rc = check_rows(residual_bf16, ldr, K, "residual"))) ||
         (sum_bf16 && (rc = check_rows(sum_bf16, lds, K, "sum"))) || (y_bf16 && (rc = check_rows(y_bf16, ldy, K, "y"))))
         return rc;
+    // in place of an input, but not of other rows of it than the row that is read
+    auto crosses = [&](const void* out, int64_t ld) {
+        return out && M > 1 && ((out == x_bf16 && ld != ldx) || (out == residual_bf16 && ld != ldr));
+    };
+    if (crosses(sum_bf16, lds) || crosses(y_bf16, ldy) || (sum_bf16 && sum_bf16 == y_bf16))
+        return fail(MXFP4_ERR_ARG, "sum or y is an input with another row stride, or both are the same");
     if (!aligned(weight_bf16, 16) || !aligned(q8, 8))
         return fail(MXFP4_ERR_ALIGN, "weight must be 16-byte aligned, q8 8-byte");
     NormArgs a = {};
@@ -92,6 +98,8 @@ int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M, co
     const int64_t C = act == MXFP4_ACT_SWIGLU ? N / 2 : N;
     if (ldy < C || (residual_bf16 && ldr < C))
         return fail(MXFP4_ERR_SHAPE, "ldy=%lld or ldr=%lld is less than %lld", (long long)ldy, (long long)ldr, (long long)C);
+    if (M > 1 && residual_bf16 == y_bf16 && ldr != ldy)
+        return fail(MXFP4_ERR_ARG, "residual is y with another row stride");
     if (!aligned(x_e4m3, 16) || !aligned(q_packed, 16) || !aligned(x_scales_e8m0, 4) || !aligned(scales_e8m0, 4) || !aligned(bias_bf16, 2) ||
         !aligned(residual_bf16, 2) || !aligned(y_bf16, 2))
         return fail(MXFP4_ERR_ALIGN, "x and q must be 16-byte aligned, the scales 4-byte, bias, residual and y 2-byte");

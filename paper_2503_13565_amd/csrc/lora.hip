@@ -481,7 +481,7 @@ hipError_t launch(LoraArgs a, hipStream_t stream)
     const int k_part = ((a.k + a.splits - 1) / a.splits + phase_of(WK) - 1) / phase_of(WK) * phase_of(WK);
     const int64_t pieces = ((int64_t)a.m + 16 * ET - 1) / (16 * ET) * (((int64_t)a.n + 255) / 256);
     const int walks = kFew ? 1 : (int)min(max(pieces / 768, (int64_t)1), (int64_t)4), step = 256 * walks, chunks = (int)(((int64_t)a.n + step - 1) / step);
-    const int64_t all = a.m, most = kFew ? min(all, ((int64_t)1 << 29) / max(a.ldx, max(a.ldb, a.ldy))) : max((1 << 21) / chunks, 1) * (16 * RT * ET);
+    const int64_t all = a.m, most = kFew ? min(all, ((int64_t)1 << 29) / max(a.ldx, max(a.ldb, a.ldy))) : max((1 << 20) / chunks, 1) * (16 * RT * ET);
     for (int64_t at = 0; at < all && e == hipSuccess; at += most) {
         LoraArgs b = a;
         b.m = (int)min(all - at, most);

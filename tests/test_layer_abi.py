@@ -6,7 +6,7 @@ import torch
 
 from paper_2503_13565_amd import binding
 
-P, P2, P8 = (ctypes.c_void_p(v) for v in (4096, 4098, 4104))      # fake pointers: 16-, 2- and 8-byte aligned, never followed
+P, Q, P2, P8 = (ctypes.c_void_p(v) for v in (4096, 1 << 20, 4098, 4104))    # fake pointers: 16-, 2- and 8-byte aligned, never followed
 NONE, NULL, SHAPE, ALIGN, WORKSPACE, ARG = 0, 1, 2, 3, 4, 6
 
 
@@ -20,6 +20,7 @@ def norm(x=P, m=4, k=64, ldx=64, r=None, ldr=64, w=None, eps=1e-6, total=None, l
     (dict(eps=-1.0), ARG), (dict(eps=float("nan")), ARG), (dict(eps=float("inf")), ARG),
     (dict(ldx=56), SHAPE), (dict(ldx=68), ALIGN), (dict(x=P8), ALIGN), (dict(r=P8), ALIGN), (dict(r=P, ldr=56), SHAPE), (dict(r=P, ldr=65), ALIGN),
     (dict(r=P, total=P8), ALIGN), (dict(r=P, total=P, lds=8), SHAPE), (dict(y=P2), ALIGN), (dict(ldy=63), SHAPE), (dict(ldy=65), ALIGN),
+    (dict(ldy=72), ARG), (dict(r=Q, ldr=72, y=Q), ARG), (dict(r=Q, total=P, lds=72, y=Q), ARG), (dict(r=Q, total=Q, lds=80), ARG), (dict(r=Q, total=P), ARG),
     (dict(w=P2), ALIGN), (dict(q8=P2, s=P), ALIGN), (dict(k=40, ldx=40, ldy=40, q8=P, s=P), SHAPE),
 ])
 def test_norm_refusals(what, code):
@@ -34,7 +35,7 @@ def product(x=P, xs=P, m=4, q=P, s=P, n=8, k=64, bias=None, act=0, r=None, ldr=8
 @pytest.mark.parametrize("what,code", [
     (dict(m=0), SHAPE), (dict(n=0), SHAPE), (dict(k=0), SHAPE), (dict(k=48), SHAPE), (dict(k=131072), SHAPE), (dict(act=2), ARG), (dict(act=1, n=7), SHAPE),
     (dict(x=None), NULL), (dict(xs=None), NULL), (dict(q=None), NULL), (dict(s=None), NULL), (dict(y=None), NULL),
-    (dict(ldy=7), SHAPE), (dict(r=P, ldr=7), SHAPE), (dict(act=1, ldy=3), SHAPE), (dict(x=P8), ALIGN), (dict(q=P8), ALIGN), (dict(xs=P2), ALIGN),
+    (dict(ldy=7), SHAPE), (dict(r=P, ldr=7), SHAPE), (dict(r=P, ldr=9), ARG), (dict(act=1, ldy=3), SHAPE), (dict(x=P8), ALIGN), (dict(q=P8), ALIGN), (dict(xs=P2), ALIGN),
     (dict(s=P2), ALIGN), (dict(y=ctypes.c_void_p(4097)), ALIGN), (dict(bias=ctypes.c_void_p(4097)), ALIGN), (dict(r=ctypes.c_void_p(4097)), ALIGN),
 ])
 def test_product_refusals(what, code):
