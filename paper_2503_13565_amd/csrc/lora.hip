@@ -97,12 +97,13 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(LoraArgs a, int k_part
     constexpr int kPhase = phase_of(WK), kBuf = shrink_buffer(RT, RG, WK), kRow = 64 * WK, kChunks = kRow / 16;
     constexpr int WR = 8 / WK, MR = RT / WR, C = (RT + RG) * WK / 8, kX = RT * WK;           // loads of a wave, KiB of x
     static_assert(MR * WR == RT && C * 8 == (RT + RG) * WK && kX % 8 == 0, "whole tiles and loads a wave");
+    const int part = kFew ? (int)blockIdx.y : (int)(blockIdx.x % a.splits);
     extern __shared__ __align__(16) uint8_t all_lds[];
     uint16_t* list = reinterpret_cast<uint16_t*>(all_lds);
     uint8_t* smem = all_lds + (kFew ? kListBytes : 0);
     const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % WK, wr = wave / WK;
-    const int k0 = (int)blockIdx.y * k_part, k1 = min(a.k, k0 + k_part), phases = (k1 - k0 + kPhase - 1) / kPhase;
+    const int k0 = part * k_part, k1 = min(a.k, k0 + k_part), phases = (k1 - k0 + kPhase - 1) / kPhase;
     const uint32_t lds_at = lds_address(smem);
     bool used = false;
 
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(LoraArgs a, int k_part
             for (int w = 1; w < WK; ++w)
                 sum += red[w * (RT * RG * 64) + at];
             if (row >= 0 && rank < a.r)
-                *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)blockIdx.y * a.m + m0 + row) * a.r + rank) = sum;
+                *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)part * a.m + m0 + row) * a.r + rank) = sum;
         }
     };
 
@@ -180,7 +181,7 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(LoraArgs a, int k_part
         for (int first = (int)blockIdx.x * (16 * RT); first < count; first += (int)gridDim.x * (16 * RT))
             tile(cur, 0, a.m, [&](int j) { return first + j < count ? (int)list[first + j] : -1; });
     } else {
-        const int64_t m0 = (int64_t)blockIdx.x * (16 * RT);
+        const int64_t m0 = (int64_t)(blockIdx.x / a.splits) * (16 * RT);
         const int rows = (int)min((int64_t)16 * RT, a.m - m0), id = tile_ids(a, m0, rows, lane);
         uint64_t todo = __ballot(id >= 0);
         for (int nth = 0; todo; ++nth) {
@@ -496,10 +497,11 @@ hipError_t launch(LoraArgs a, hipStream_t stream)
             lora_expand_few_kernel<KC><<<dim3(chunks, share, groups + 1), 256, expand_bytes, stream>>>(b);
         } else {
             const int wide = (b.m + ET * 16 - 1) / (ET * 16);
-            const auto slots = [&](int64_t others) { return (int)max(min(min((int64_t)a.adapters, (int64_t)16), 1024 / others), (int64_t)1); };
-            lora_shrink_kernel<RT, RG, WK, D, false><<<dim3(tiles, a.splits, slots((int64_t)tiles * a.splits)), 512, shrink_bytes, stream>>>(b, k_part);
+            // (tiles with rows of several adapters: two workgroups share them in shrink, 24 us for 27; in expand one goes through them, 48 for 52)
+            const auto slots = [&](int64_t least, int64_t others) { return (int)min((int64_t)min(a.adapters, 16), max(1024 / others, least)); };
+            lora_shrink_kernel<RT, RG, WK, D, false><<<dim3(tiles * a.splits, 1, slots(2, (int64_t)tiles * a.splits)), 512, shrink_bytes, stream>>>(b, k_part);
             lora_sum_kernel<<<(unsigned)(((int64_t)b.m * (a.r / 8) + 255) / 256), 256, 0, stream>>>(b);
-            lora_expand_kernel<KC, ET><<<dim3(wide * chunks, 1, slots((int64_t)wide * chunks)), 256, expand_bytes, stream>>>(b, walks, chunks);
+            lora_expand_kernel<KC, ET><<<dim3(wide * chunks, 1, slots(1, (int64_t)wide * chunks)), 256, expand_bytes, stream>>>(b, walks, chunks);
         }
         e = hipGetLastError();
     }
@@ -513,10 +515,13 @@ constexpr bool few(int64_t m) { return m < kFewRows; }
 int lora_splits(int64_t m, int64_t k, int64_t r)
 {
     const int64_t rows = r > 64 ? 32 : 64, tiles = (m + rows - 1) / rows, phase = phase_of(few(m) ? 8 : 4), most = (k + phase - 1) / phase;
-    int64_t s = few(m) ? kLoraSplits : 512 / tiles;
-    s = s > kLoraSplits ? kLoraSplits : s;
-    s = s > most ? most : s;
-    return (int)(s < 1 ? 1 : s);
+    if (few(m))
+        return (int)(most < kLoraSplits ? most : kLoraSplits);
+    // a power of two: neighbouring workgroups have the parts in turn, so a part of A's columns stays with the dies that have it
+    int s = kLoraSplits;
+    while (s > 1 && (s > most || s * tiles > 1024))
+        s /= 2;
+    return s;
 }
 
 hipError_t launch_lora(const LoraArgs& a, const DeviceInfo&, hipStream_t stream)
@@ -528,7 +533,7 @@ hipError_t launch_lora(const LoraArgs& a, const DeviceInfo&, hipStream_t stream)
                : groups <= 4 ? launch<1, 4, 8, 2, true>(a, stream)
                              : launch<1, 8, 8, 2, true>(a, stream);
     return groups <= 2   ? launch<4, 2, 4, 2, false>(a, stream)
-           : groups <= 4 ? launch<4, 4, 4, 2, false>(a, stream)
+           : groups <= 4 ? launch<4, 4, 2, 3, false>(a, stream)
                          : launch<2, 8, 4, 2, false>(a, stream);
 }
 
