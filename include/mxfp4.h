@@ -459,7 +459,8 @@ int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M,
  *   y_bf16     out BF16 [M, N], row stride ldy
  *   workspace  mxfp4_lora_workspace_bytes(M, K, R) bytes, 16-byte aligned, contents unspecified before and after; calls that overlap in
  *              time must not share it
- * K, N and R multiples of 8, R at most 128 (a larger rank: two calls, the second with y as its base), K at most MXFP4_MAX_K; x, base and y
+ * K, N and R multiples of 8, R at most 128 (a larger rank: two calls, the second with y as its base), K at most MXFP4_MAX_K; 1 to 8192
+ * adapters; x, base and y
  * 16-byte aligned with row strides that are multiples of 8 and at most 2^23.  M may be 0 (no-op).  The summation order follows from the
  * sizes.
  */

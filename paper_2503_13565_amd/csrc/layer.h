@@ -51,7 +51,8 @@ struct LoraArgs {
     int64_t ldx, ldb, ldy;
     int m, n, k, r, adapters, splits;
 };
-int lora_splits(int64_t m, int64_t k, int64_t r);
+constexpr int kMostAdapters = 8192;     // (four numbers of each lie in the LDS)
+size_t lora_workspace(int64_t m, int64_t k, int64_t r);
 hipError_t launch_lora(const LoraArgs& a, const DeviceInfo& dev, hipStream_t stream);
 
 }  // namespace mxfp4

@@ -129,7 +129,7 @@ static bool lora_sizes(int64_t M, int64_t K, int64_t R)
 
 size_t mxfp4_lora_workspace_bytes(int64_t M, int64_t K, int64_t R)
 {
-    return lora_sizes(M, K, R) && M ? (size_t)lora_splits(M, K, R) * M * R * sizeof(float) : 0;
+    return lora_sizes(M, K, R) && M ? lora_workspace(M, K, R) : 0;
 }
 
 int mxfp4_lora(const void* x_bf16, int64_t M, int64_t ldx, const void* a_bf16, const void* b_bf16, int64_t adapters, int64_t R, int64_t N,
@@ -140,8 +140,8 @@ int mxfp4_lora(const void* x_bf16, int64_t M, int64_t ldx, const void* a_bf16, c
     if (!lora_sizes(M, K, R) || N < 8 || N % 8 || N > kMostRows)
         return fail(MXFP4_ERR_SHAPE, "M=%lld, N=%lld, K=%lld or R=%lld out of range (N, K, R multiples of 8, K at most %d, R at most 128)",
                     (long long)M, (long long)N, (long long)K, (long long)R, MXFP4_MAX_K);
-    if (adapters < 1 || adapters > 0x7FFFFFFF)
-        return fail(MXFP4_ERR_SHAPE, "adapters=%lld out of range", (long long)adapters);
+    if (adapters < 1 || adapters > kMostAdapters)
+        return fail(MXFP4_ERR_SHAPE, "adapters=%lld out of range (at most %d)", (long long)adapters, kMostAdapters);
     if (M == 0)
         return MXFP4_OK;
     if (!x_bf16 || !a_bf16 || !b_bf16 || !ids || !y_bf16)
@@ -180,7 +180,6 @@ int mxfp4_lora(const void* x_bf16, int64_t M, int64_t ldx, const void* a_bf16, c
     a.k = (int)K;
     a.r = (int)R;
     a.adapters = (int)adapters;
-    a.splits = lora_splits(M, K, R);
     return launched(launch_lora(a, dev, static_cast<hipStream_t>(stream)), "adapter launch");
 }
 

@@ -1,20 +1,23 @@
 // Low-rank adapters of many requests beside a shared projection:  y[m] = base[m] + scale[i] * B_i (A_i x[m]),  i = ids[m].
 //
-// The products give a workgroup rows of one adapter at a time, as the columns of v_mfma_f32_16x16x32_bf16: what another request's adapter holds
-// (NaN, infinities) never meets a row, and rows may lie in any order.  Below 512 rows a workgroup has an adapter (grid z) and collects its rows from
-// all of the call, so that an adapter's matrices are read once whatever the order (96 rows of 60 adapters at 4096 -> 12288, rank 32: 17 us, and 47
-// with tiles of neighbouring rows); from 512 rows on, where reading all ids would cost more than it saves, it has 16 RT rows side by side and goes
-// through the adapters among them.
-//   shrink  t = A_i x for a part of K (grid y).  Rows of x and of A_i come into the LDS a phase of elements at a time by loads that write it directly,
+// A workgroup of the products has rows of one adapter, as the columns of v_mfma_f32_16x16x32_bf16: what another request's adapter holds (NaN,
+// infinities) never meets a row, rows may lie in any order, and an adapter's matrices are read once for all its rows (up to a workgroup's).
+//   group   sorts the rows by adapter, in one workgroup: counts, sums over the adapters, places.  Rows of an adapter come in any order, which no output
+//           depends on.  It costs 3 us for hundreds of rows and 7 for 5003, so up to 128 rows the products find theirs themselves (96 rows of 60
+//           adapters at 4096 -> 12288, rank 32: 18 us for 20.4); with more of them, the sixteens of an adapter that has most of the rows would come one
+//           after the other (256 rows of one among 60, 4096 -> 4096, rank 16: 12.3 us for 45), and tiles of neighbouring rows would read many
+//           adapters' matrices each (512 rows of 60, 4096 -> 12288, rank 64: 47 us for 118).
+//   shrink  t = A_i x for a part of K.  Rows of x and of A_i come into the LDS a phase of elements at a time by loads that write it directly,
 //           D - 1 phases ahead, up to 512 bytes of a row side by side (in the layout of the matrix instruction a load touches a line per lane, and a
 //           unit gets 38 bytes a ns instead of up to 150).  The waves that share a phase's elements add their sums in wave order; the parts' sums
 //           lie in the workspace in FP32, side by side.
 //   sum     adds the parts in order, scales t and cuts it into two BF16 numbers (together 16 bits, so that t's rounding does not show beside that
 //           of y).  Below 512 rows the next step does it: a launch costs more than doing it several times.
 //   expand  multiplies with B_i's rows, which are one piece of memory, and adds the base to the FP32 sums: one rounding.
-// 5003 rows of five adapters, 8192 -> 8192, rank 64: shrink 30 us (x alone is 17 at a copy's rate), sum 5, expand 48 (base and y: 33).  The products
-// by themselves are 25 us of the last, loads and stores 36: they overlap in part.  No gain: 16 or 64 rows a workgroup, two walks or eight, three
-// phases ahead in one workgroup a unit, t's sums in every workgroup of expand (61 us), a whole line of a row an instruction.
+// 5003 rows of five adapters, 8192 -> 8192, rank 64: group 7 us, shrink 24 (x alone is 17 at a copy's rate), sum 5, expand 46 (base and y: 33; the
+// products by themselves are 25, loads and stores 36: they overlap in part).  No gain in expand: 16 or 64 rows a workgroup, two walks or eight, t's
+// sums in every workgroup (61 us), a whole line of a row an instruction.  In one token's call (8 us) each launch is a chain of three loads;
+// both products in one launch, with t made again by every workgroup, were as long at 4096 and longer beyond.
 #include "cast_block8.h"
 #include "gemm_a8.h"
 
@@ -40,45 +43,182 @@ __device__ __forceinline__ u32x4_t words16(const uint16_t* p, int64_t bytes)
 }
 
 constexpr int kLoraSplits = 8;          // parts of K
+constexpr int kAlone = 128;             // the most rows of a call whose products find their rows themselves
+constexpr int kSmall = 512;             // rows from which on workgroups have 64 (32 where ranks are many) and 32 rows in place of 16
+constexpr int kWindow = 1 << 13;        // the most rows of one set of launches
 
-// The adapter of each of the tile's 16 RT rows, in the lane of its number; -1: none.
-__device__ __forceinline__ int tile_ids(const LoraArgs& a, int64_t m0, int rows, int lane)
+// Rows order[first] .. of one adapter (-1: rows of none); count 0: nothing.
+struct Item {
+    int id, first, count, unused;
+};
+
+// What the launches of a window share, in the workspace
+struct Lists {
+    Item *in, *out;                     // for shrink and for expand
+    int* order;
+};
+
+constexpr int rows_in(int64_t m, int64_t r) { return m < kSmall ? 16 : r > 64 ? 32 : 64; }
+constexpr int rows_out(int64_t m) { return m < kSmall ? 16 : 32; }
+
+__device__ __forceinline__ int adapter_of(const LoraArgs& a, int row, int none)
 {
-    const int id = lane < rows ? a.ids[m0 + lane] : -1;
-    return id >= 0 && id < a.adapters ? id : -1;
+    const int id = a.ids[row];
+    return id >= 0 && id < a.adapters ? id : none;
 }
 
-// Below 512 rows: grid z is an adapter, or where there are more adapters than rows, the row that is its adapter's first.  The adapter's rows, in order,
-// go into `list` (every wave writes the same), their number comes back; z of gridDim.z - 1 has the rows of no adapter.
-constexpr int kFewRows = 512, kListBytes = kFewRows * 2;
-__device__ __forceinline__ int collect(const LoraArgs& a, int z, int lane, uint16_t* list, int& cur)
+// T threads with U rows each, all ids at once.  `lds`: four numbers an adapter (and as many for none), kGroupBytes in front.  Items of 2^in_shift and
+// 2^out_shift rows, in_most and out_most of them (those behind the last: nothing).
+constexpr int kGroupBytes = 3 * 16 * 4;
+constexpr int group_lds(int adapters) { return kGroupBytes + (4 * (adapters + 1) + 1) * 4; }
+
+template <int T, int U>
+__device__ __forceinline__ void group_rows(const LoraArgs& a, const Lists& lists, int in_shift, int out_shift, int in_most, int out_most, uint8_t* lds)
 {
-    int id[kFewRows / 64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = a.adapters + 1;
+    int *waves = reinterpret_cast<int*>(lds), *next = waves + 3 * 16, *begins = next + n, *in = begins + n + 1, *out = in + n;
+    int id[U];
 #pragma unroll
-    for (int u = 0; u < kFewRows / 64; ++u) {
-        const int row = u * 64 + lane, v = row < a.m ? a.ids[row] : -2;
-        id[u] = v == -2 && row >= a.m ? -2 : v >= 0 && v < a.adapters ? v : -1;
+    for (int u = 0; u < U; ++u)
+        id[u] = a.ids[min(u * T + (int)threadIdx.x, a.m - 1)];
+    for (int i = threadIdx.x; i < n; i += T)
+        next[i] = 0;
+    __syncthreads();
+    // Runs of one adapter: one addition a wave.
+    const auto each = [&](auto take) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u * T >= a.m)
+                break;
+            const int row = u * T + (int)threadIdx.x, first = __builtin_amdgcn_readfirstlane(id[u]);
+            if (__all(id[u] == first && row < a.m))
+                take(row, first, true);
+            else if (row < a.m)
+                take(row, id[u], false);
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        id[u] = id[u] >= 0 && id[u] < a.adapters ? id[u] : a.adapters;
+    each([&](int, int of, bool run) {
+        if (!run || lane == 0)
+            atomicAdd(&next[of], run ? 64 : 1);
+    });
+    __syncthreads();
+    const int per = (n + T - 1) / T, from = threadIdx.x * per, to = min(n, from + per);
+    int sum[3] = {0, 0, 0}, all[3] = {0, 0, 0};                 // rows, items for shrink, items for expand in front of this thread's adapters; and of all
+    const auto items = [](int rows, int shift) { return (rows + (1 << shift) - 1) >> shift; };
+    for (int i = from; i < to; ++i) {
+        sum[0] += next[i];
+        sum[1] += i < a.adapters ? items(next[i], in_shift) : 0;
+        sum[2] += items(next[i], out_shift);
     }
-    const bool by_row = a.adapters > a.m;
-    cur = z;
-    if (z < 0)
-        cur = -1;
-    else if (by_row)
-        cur = a.ids[z];
-    if (z >= 0 && (cur < 0 || cur >= a.adapters))
-        return 0;
+#pragma unroll
+    for (int v = 0; v < 3; ++v) {
+        int upto = sum[v];
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int other = __shfl_up(upto, d);
+            upto += lane >= d ? other : 0;
+        }
+        if (lane == 63)
+            waves[v * 16 + wave] = upto;
+        sum[v] = upto - sum[v];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < 3; ++v)
+#pragma unroll
+        for (int i = 0; i < T / 64; ++i) {
+            sum[v] += i < wave ? waves[v * 16 + i] : 0;
+            all[v] += waves[v * 16 + i];
+        }
+    for (int i = from; i < to; ++i) {
+        const int rows = next[i];
+        in[i] = sum[1];
+        out[i] = sum[2];
+        begins[i] = next[i] = sum[0];
+        sum[0] += rows;
+        sum[1] += i < a.adapters ? items(rows, in_shift) : 0;
+        sum[2] += items(rows, out_shift);
+    }
+    if (threadIdx.x == 0)
+        begins[n] = a.m;
+    for (int i = all[1] + (int)threadIdx.x; i < in_most; i += T)
+        lists.in[i] = Item{-1, 0, 0, 0};
+    for (int i = all[2] + (int)threadIdx.x; i < out_most; i += T)
+        lists.out[i] = Item{-1, 0, 0, 0};
+    __syncthreads();
+    each([&](int row, int of, bool run) {
+        int place = !run || lane == 0 ? atomicAdd(&next[of], run ? 64 : 1) : 0;
+        if (run)
+            place = __builtin_amdgcn_readfirstlane(place) + lane;
+        lists.order[place] = row;
+        // the rows that come to an item's first place write it
+        const int at = place - begins[of], left = begins[of + 1] - place, owner = of < a.adapters ? of : -1;
+        if (owner >= 0 && (at & ((1 << in_shift) - 1)) == 0)
+            lists.in[in[of] + (at >> in_shift)] = Item{owner, place, min(1 << in_shift, left), 0};
+        if ((at & ((1 << out_shift) - 1)) == 0)
+            lists.out[out[of] + (at >> out_shift)] = Item{owner, place, min(1 << out_shift, left), 0};
+    });
+}
+
+__global__ __launch_bounds__(1024) void lora_group_kernel(LoraArgs a, Lists lists, int in_shift, int in_most, int out_most)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    group_rows<1024, kWindow / 1024>(a, lists, in_shift, 5, in_most, out_most, smem);
+}
+
+__global__ __launch_bounds__(512) void lora_group_few_kernel(LoraArgs a, Lists lists, int in_most, int out_most)
+{
+    extern __shared__ __align__(16) uint8_t smem[];
+    group_rows<512, 1>(a, lists, 4, 4, in_most, out_most, smem);
+}
+
+// The rows of a workgroup of a product into `rows`, in the order of the call or the list; their adapter; how many they are.  Listed: item w.  Else: w has the
+// adapter of that number, or where there are more adapters than rows, of the row of that number if it is the adapter's first; the number behind
+// the last adapter (or row) has the rows of none.
+constexpr int kListBytes = kAlone * 4;
+template <bool kListed>
+__device__ __forceinline__ int find(const LoraArgs& a, const Item* items, const int* order, int w, int* rows, int& cur)
+{
     int count = 0;
+    if constexpr (kListed) {
+        const Item item = items[w];
+        cur = item.id;
+        count = item.count;
+        if ((int)threadIdx.x < count)
+            rows[threadIdx.x] = order[item.first + threadIdx.x];
+    } else {
+        const int lane = threadIdx.x & 63, most = min(a.adapters, a.m);
+        const bool by_row = a.adapters > a.m;
+        int id[kAlone / 64];
 #pragma unroll
-    for (int u = 0; u < kFewRows / 64; ++u) {
-        if (u * 64 >= a.m)
-            break;
-        const uint64_t mine = __ballot(id[u] == cur);
-        if (by_row && z >= 0 && count == 0 && mine && u * 64 + __builtin_ctzll(mine) != z)
-            return 0;
-        if (id[u] == cur)
-            list[count + __builtin_popcountll(mine & ((1ull << lane) - 1))] = (uint16_t)(u * 64 + lane);
-        count += __builtin_popcountll(mine);
+        for (int u = 0; u < kAlone / 64; ++u) {
+            id[u] = a.ids[min(u * 64 + lane, a.m - 1)];
+            id[u] = u * 64 + lane >= a.m ? -2 : id[u] >= 0 && id[u] < a.adapters ? id[u] : -1;
+        }
+        cur = w == most ? -1 : w;
+        if (by_row && w < most) {
+#pragma unroll
+            for (int u = 0; u < kAlone / 64; ++u)
+                if (w >> 6 == u)
+                    cur = __builtin_amdgcn_readlane(id[u], w & 63);
+            if (cur < 0)
+                return 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kAlone / 64; ++u) {
+            const uint64_t mine = __ballot(id[u] == cur);
+            if (by_row && w < most && count == 0 && mine && u * 64 + __builtin_ctzll(mine) != w)
+                return 0;
+            if (id[u] == cur)                                   // (every wave writes the same)
+                rows[count + __builtin_popcountll(mine & ((1ull << lane) - 1))] = u * 64 + lane;
+            count += __builtin_popcountll(mine);
+        }
     }
+    if (count)
+        __syncthreads();
     return count;
 }
 
@@ -91,25 +231,27 @@ constexpr int shrink_lds(int rt, int rg, int wk, int d)
     return buffers > sums ? buffers : sums;
 }
 
-template <int RT, int RG, int WK, int D, bool kFew>
-__global__ __launch_bounds__(512) void lora_shrink_kernel(LoraArgs a, int k_part)
+template <int RT, int RG, int WK, int D, bool kListed>
+__global__ __launch_bounds__(512) void lora_shrink_kernel(LoraArgs a, Lists lists, int k_part, int owners, int share)
 {
     constexpr int kPhase = phase_of(WK), kBuf = shrink_buffer(RT, RG, WK), kRow = 64 * WK, kChunks = kRow / 16;
     constexpr int WR = 8 / WK, MR = RT / WR, C = (RT + RG) * WK / 8, kX = RT * WK;           // loads of a wave, KiB of x
     static_assert(MR * WR == RT && C * 8 == (RT + RG) * WK && kX % 8 == 0, "whole tiles and loads a wave");
-    const int part = kFew ? (int)blockIdx.y : (int)(blockIdx.x % a.splits);
     extern __shared__ __align__(16) uint8_t all_lds[];
-    uint16_t* list = reinterpret_cast<uint16_t*>(all_lds);
-    uint8_t* smem = all_lds + (kFew ? kListBytes : 0);
+    int* list = reinterpret_cast<int*>(all_lds);
+    uint8_t* smem = all_lds + kListBytes;
     const int lane = threadIdx.x & 63, li = lane & 15, lg = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % WK, wr = wave / WK;
+    // Neighbouring workgroups have the parts of K in turn: a part of A's columns stays with the dies that have it.
+    const int part = (int)(blockIdx.x % a.splits);
     const int k0 = part * k_part, k1 = min(a.k, k0 + k_part), phases = (k1 - k0 + kPhase - 1) / kPhase;
     const uint32_t lds_at = lds_address(smem);
-    bool used = false;
-
-    // Row j of the tile's is row_of(j) of x, behind row m0; below 0: none.
-    auto tile = [&](int cur, int64_t m0, int reach, auto row_of) {
-        const u32x4_t rx = words16(a.x + m0 * a.ldx, (int64_t)reach * a.ldx * 2), ra = words16(a.a + (int64_t)cur * a.r * a.k, (int64_t)a.r * a.k * 2);
+    const int w = (int)(blockIdx.x / a.splits);
+    int cur;
+    const int count = find<kListed>(a, lists.in, lists.order, kListed ? w : w % owners, list, cur);
+    for (int first = kListed ? 0 : w / owners * 16; first < count; first += share * 16) {
+        const auto row_of = [&](int j) { return first + j < count ? list[first + j] : -1; };
+        const u32x4_t rx = words16(a.x, (int64_t)a.m * a.ldx * 2), ra = words16(a.a + (int64_t)cur * a.r * a.k, (int64_t)a.r * a.k * 2);
         // Load c of wave w fills KiB 8 c + w of a phase: x first, A behind it.  Chunk c of row r lies at c ^ (r % 16).
         int off[C], chunk[C];
 #pragma unroll
@@ -126,9 +268,6 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(LoraArgs a, int k_part
             for (int c = 0; c < C; ++c)
                 direct(lds_at + b * kBuf + (c * 8 + wave) * 1024, off[c] | past((k1 - k0) / 8 - 1, p * (kPhase / 8) + chunk[c]), c * 8 < kX ? rx : ra, from);
         };
-        if (used)
-            __syncthreads();                                    // (the sums of the tile before have been read)
-        used = true;
 #pragma unroll
         for (int d = 0; d < D; ++d)
             issue(d, d);
@@ -170,27 +309,11 @@ __global__ __launch_bounds__(512) void lora_shrink_kernel(LoraArgs a, int k_part
             for (int w = 1; w < WK; ++w)
                 sum += red[w * (RT * RG * 64) + at];
             if (row >= 0 && rank < a.r)
-                *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)part * a.m + m0 + row) * a.r + rank) = sum;
+                *reinterpret_cast<f32x4_t*>(a.part + ((int64_t)part * a.m + row) * a.r + rank) = sum;
         }
-    };
-
-    if constexpr (kFew) {
-        int cur;
-        const int count = collect(a, blockIdx.z, lane, list, cur);
-        __syncthreads();
-        for (int first = (int)blockIdx.x * (16 * RT); first < count; first += (int)gridDim.x * (16 * RT))
-            tile(cur, 0, a.m, [&](int j) { return first + j < count ? (int)list[first + j] : -1; });
-    } else {
-        const int64_t m0 = (int64_t)(blockIdx.x / a.splits) * (16 * RT);
-        const int rows = (int)min((int64_t)16 * RT, a.m - m0), id = tile_ids(a, m0, rows, lane);
-        uint64_t todo = __ballot(id >= 0);
-        for (int nth = 0; todo; ++nth) {
-            const int cur = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
-            const uint64_t mine = __ballot(id == cur);
-            todo &= ~mine;
-            if (nth % (int)gridDim.z == (int)blockIdx.z)
-                tile(cur, m0, rows, [&](int j) { return mine >> j & 1 ? j : -1; });
-        }
+        if constexpr (kListed)
+            return;
+        __syncthreads();                                        // (the sums have been read)
     }
 }
 
@@ -217,7 +340,7 @@ __device__ __forceinline__ u32x4_t sum_of(const LoraArgs& a, int64_t at, float s
     return o;
 }
 
-// From 512 rows on: t of every row in place of its first part, eight upper numbers and eight lower ones of a thread's eight ranks, so that the
+// t of every row in place of its first part, eight upper numbers and eight lower ones of a thread's eight ranks, so that the
 // workgroups that share a row's outputs read it once, and as the matrix instructions take it.
 __global__ __launch_bounds__(256) void lora_sum_kernel(LoraArgs a)
 {
@@ -350,28 +473,26 @@ struct Expand {
     }
 };
 
-// Below 512 rows: grid z an adapter, x 256 outputs of one of its tiles of 16 rows (and every gridDim.y-th), y the tile.  B's rows stay for all tiles.
-template <int KC>
-__global__ __launch_bounds__(256, 4) void lora_expand_few_kernel(LoraArgs a)
+// Below 512 rows: grid x 256 outputs, y the workgroups of those.
+template <int KC, bool kListed>
+__global__ __launch_bounds__(256, 4) void lora_expand_few_kernel(LoraArgs a, Lists lists, int owners, int share)
 {
     extern __shared__ __align__(16) uint8_t smem[];
+    int* list = reinterpret_cast<int*>(smem);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Expand<KC> e{a, smem + kListBytes, (int)threadIdx.x & 63, wave};
-    uint16_t* list = reinterpret_cast<uint16_t*>(smem);
     int cur;
-    const int count = collect(a, (int)blockIdx.z + 1 < (int)gridDim.z ? (int)blockIdx.z : -1, e.lane, list, cur);
-    const int n0 = ((int)blockIdx.x * 4 + wave) * 64;
-    int first = (int)blockIdx.y * 16;
+    const int w = (int)blockIdx.y, count = find<kListed>(a, lists.out, lists.order, kListed ? w : w % owners, list, cur);
+    int first = kListed ? 0 : w / owners * 16;
     if (first >= count || (cur < 0 && a.base == a.y))
         return;
-    const int own = expand_t(KC) + wave * (1024 * KC);
+    const int n0 = ((int)blockIdx.x * 4 + wave) * 64, own = expand_t(KC) + wave * (1024 * KC);
     if (cur >= 0)
-        e.fetch(lds_address(e.smem) + own, cur, n0);
+        e.fetch(lds_address(e.smem) + own, cur, n0);            // (B's rows stay for all of the adapter's)
     const float scale = a.scales && cur >= 0 ? a.scales[cur] : 1.f;
     const auto base = e.rows_of(a.base, a.ldb, a.m), y = e.rows_of(a.y, a.ldy, a.m);
-    __syncthreads();
-    for (bool next = false; first < count; first += (int)gridDim.y * 16, next = true) {
-        auto row_of = [&](int j) { return first + j < count ? (int)list[first + j] : -1; };
+    for (bool next = false; first < count; first += share * 16, next = true) {
+        const auto row_of = [&](int j) { return first + j < count ? list[first + j] : -1; };
         const int row = row_of(e.lane & 15), from[1] = {e.offset(row, a.ldb)}, to[1] = {e.offset(row, a.ldy)};
         u32x4_t v[1][2], out[1][2];
         e.load(v, base, n0, from);
@@ -389,152 +510,169 @@ __global__ __launch_bounds__(256, 4) void lora_expand_few_kernel(LoraArgs a)
     }
 }
 
-// Grid x: `walks` times 256 outputs, those of 16 RT rows side by side, then the next rows' (a piece of B stays with a die); the adapters among the rows are
-// shared out over grid z.
+// Grid x: `walks` times 256 outputs, those of an item's rows side by side, then the next item's (a piece of B stays with a die).
 template <int KC, int RT>
-__global__ __launch_bounds__(256, KC == 16 ? 2 : 3) void lora_expand_kernel(LoraArgs a, int walks, int chunks)
+__global__ __launch_bounds__(256, KC == 16 ? 2 : 3) void lora_expand_kernel(LoraArgs a, Lists lists, int walks, int chunks)
 {
     extern __shared__ __align__(16) uint8_t smem[];
+    int* list = reinterpret_cast<int*>(smem);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Expand<KC> e{a, smem, (int)threadIdx.x & 63, wave};
-    const int64_t m0 = (int64_t)(blockIdx.x / chunks) * (16 * RT);
-    const int rows = (int)min((int64_t)16 * RT, a.m - m0);
-    const int id = tile_ids(a, m0, rows, e.lane);
-    const int own = wave * (1024 * KC);
-    const uint64_t some = __ballot(id >= 0);
-    const uint64_t none = blockIdx.z == 0 && a.base != a.y ? __ballot(id < 0 && e.lane < rows) : 0;    // rows of no adapter: the base as it is
-    const auto output = [&](int walk) { return (((int)(blockIdx.x % chunks) * walks + walk) * 4 + wave) * 64; };
-    const auto base = e.rows_of(a.base ? a.base + m0 * a.ldb : nullptr, a.ldb, rows), y = e.rows_of(a.y + m0 * a.ldy, a.ldy, rows);
-    u32x4_t v[RT][2], out[RT][2];
-    int from[RT], to[RT];
-    const auto take = [&](uint64_t mine) {
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            const int row = mine >> (16 * i + (e.lane & 15)) & 1 ? 16 * i + (e.lane & 15) : -1;
-            from[i] = e.offset(row, a.ldb);
-            to[i] = e.offset(row, a.ldy);
-        }
-    };
-    take(none);
-    for (int walk = 0; none && walk < walks; ++walk) {
-        e.load(v, base, output(walk), from);
-        e.store(v, y, output(walk), to);
-    }
-    if (!some)
+    const Expand<KC> e{a, smem + kListBytes, (int)threadIdx.x & 63, wave};
+    int cur;
+    const int count = find<true>(a, lists.out, lists.order, (int)(blockIdx.x / chunks), list, cur);
+    if (count == 0 || (cur < 0 && a.base == a.y))
         return;
-    // t of all rows: what a row is of another adapter than the one whose B is multiplied meets no row of that one.
-    const auto sums = __builtin_amdgcn_make_buffer_rsrc(a.part + m0 * a.r, 0, rows * a.r * 4, 0x00020000);
-    bf16x8_t t[RT][KC / 4][2];
-    uint64_t todo = some;
-    bool first = true;
-    for (int nth = 0; todo; ++nth) {
-        const int cur = __builtin_amdgcn_readlane(id, __builtin_ctzll(todo));
-        const uint64_t mine = __ballot(id == cur);
-        todo &= ~mine;
-        if (nth % (int)gridDim.z != (int)blockIdx.z)
-            continue;
-        take(mine);
-        e.fetch(lds_address(smem) + own, cur, output(0));
-        e.load(v, base, output(0), from);
-        if (first) {
+    const int own = wave * (1024 * KC);
+    const auto output = [&](int walk) { return (((int)(blockIdx.x % chunks) * walks + walk) * 4 + wave) * 64; };
+    const auto base = e.rows_of(a.base, a.ldb, a.m), y = e.rows_of(a.y, a.ldy, a.m);
+    u32x4_t v[RT][2], out[RT][2];
+    int row[RT], from[RT], to[RT];
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int q = 0; q < KC / 4; ++q)
-#pragma unroll
-                    for (int part = 0; part < 2; ++part) {
-                        const int row = 16 * i + (e.lane & 15), rank = 32 * q + 8 * (e.lane >> 4);
-                        t[i][q][part] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(sums, rank < a.r ? (row * a.r + rank + 4 * part) * 4 : kOob, 0, 0));
-                    }
-            first = false;
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        // The next outputs' rows of B and base are on their way before this walk's outputs leave, and the wait for them does not wait for the stores.
+    for (int i = 0; i < RT; ++i) {
+        row[i] = 16 * i + (e.lane & 15) < count ? list[16 * i + (e.lane & 15)] : -1;
+        from[i] = e.offset(row[i], a.ldb);
+        to[i] = e.offset(row[i], a.ldy);
+    }
+    if (cur < 0) {                                              // rows of no adapter: the base as it is
         for (int walk = 0; walk < walks; ++walk) {
-            e.product(out, v, smem + own, [&](int i, int q, int part) { return t[i][q][part]; });
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's part has been read)
-            if (walk + 1 < walks) {
-                e.fetch(lds_address(smem) + own, cur, output(walk + 1));
-                e.load(v, base, output(walk + 1), from);
-            }
-            e.store(out, y, output(walk), to);
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * RT) : "memory");
+            e.load(v, base, output(walk), from);
+            e.store(v, y, output(walk), to);
         }
+        return;
+    }
+    e.fetch(lds_address(e.smem) + own, cur, output(0));
+    e.load(v, base, output(0), from);
+    const auto sums = __builtin_amdgcn_make_buffer_rsrc(a.part, 0, a.m * a.r * 4, 0x00020000);
+    bf16x8_t t[RT][KC / 4][2];
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int q = 0; q < KC / 4; ++q)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const int rank = 32 * q + 8 * (e.lane >> 4);
+                t[i][q][part] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(sums, rank < a.r && row[i] >= 0 ? (row[i] * a.r + rank + 4 * part) * 4 : kOob, 0, 0));
+            }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // A wave goes alone: the next outputs' rows of B and base are on their way before this walk's outputs leave, and the wait for them does not wait for
+    // the stores.
+    for (int walk = 0; walk < walks; ++walk) {
+        e.product(out, v, e.smem + own, [&](int i, int q, int part) { return t[i][q][part]; });
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // (the wave's part has been read)
+        if (walk + 1 < walks) {
+            e.fetch(lds_address(e.smem) + own, cur, output(walk + 1));
+            e.load(v, base, output(walk + 1), from);
+        }
+        e.store(out, y, output(walk), to);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * RT) : "memory");
     }
 }
 
+// The rows of one set of launches: lists are made by one workgroup, and offsets into x, base and y have 31 bits.
+int64_t window(const LoraArgs& a) { return min((int64_t)min(a.m, kWindow), ((int64_t)1 << 29) / max(a.ldx, max(a.ldb, a.ldy))); }
 
-// Workgroups of a grid are limited, and so is the reach of an offset into x, base and y: very many rows, and rows very far apart, are several pairs of launches.
-template <int RT, int RG, int WK, int D, bool kFew>
-hipError_t launch(LoraArgs a, hipStream_t stream)
+// The launches of one window: RT tiles of sixteen rows and RG of ranks in shrink, ET tiles of rows in expand; kListed: with the sort in front.
+template <int RT, int RG, int WK, int D, int ET, bool kListed>
+hipError_t launch(const LoraArgs& a, hipStream_t stream)
 {
-    constexpr int KC = RG <= 2 ? 4 : RG <= 4 ? 8 : 16, ET = kFew ? 1 : 2;
-    static LdsLimit shrink, expand;
-    const int list = kFew ? kListBytes : 0, shrink_bytes = shrink_lds(RT, RG, WK, D) + list, expand_bytes = 4 * 1024 * KC + (kFew ? list + expand_t(KC) : 0);
-    const void* second;
-    if constexpr (kFew)
-        second = reinterpret_cast<const void*>(lora_expand_few_kernel<KC>);
-    else
+    constexpr int KC = RG <= 2 ? 4 : RG <= 4 ? 8 : 16;
+    constexpr bool kFew = ET == 1;
+    constexpr int expand_bytes = 4 * 1024 * KC + (kFew ? expand_t(KC) : 0) + kListBytes, shrink_bytes = shrink_lds(RT, RG, WK, D) + kListBytes;
+    static LdsLimit group, shrink, expand;
+    hipError_t e = shrink.raise(reinterpret_cast<const void*>(lora_shrink_kernel<RT, RG, WK, D, kListed>), shrink_bytes);
+    const void *first, *second;
+    if constexpr (kFew) {
+        first = reinterpret_cast<const void*>(lora_group_few_kernel);
+        second = reinterpret_cast<const void*>(lora_expand_few_kernel<KC, kListed>);
+    } else {
+        first = reinterpret_cast<const void*>(lora_group_kernel);
         second = reinterpret_cast<const void*>(lora_expand_kernel<KC, ET>);
-    hipError_t e = shrink.raise(reinterpret_cast<const void*>(lora_shrink_kernel<RT, RG, WK, D, kFew>), shrink_bytes);
+    }
     if (e == hipSuccess)
         e = expand.raise(second, expand_bytes);
+    if (kListed && e == hipSuccess)
+        e = group.raise(first, group_lds(kMostAdapters));
+    if (e != hipSuccess)
+        return e;
+    Lists lists = {};
+    lists.in = reinterpret_cast<Item*>(a.part + (int64_t)a.splits * a.m * a.r);
+    lists.out = lists.in + a.m;
+    lists.order = reinterpret_cast<int*>(lists.out + a.m);
+    // (an adapter's last item may have fewer rows than others, and so may that of the rows of none)
+    // (two workgroups an adapter at least: 128 rows of one among 60, 4096 -> 4096, rank 16, 17.2 us for 25.5; 12.2 for 11.4 where the rows are mixed)
+    const int owners = min(a.adapters, a.m), tiles = (a.m + 15) / 16, share = min(tiles, max(2, (2 * tiles + owners - 1) / owners));
+    const int in = kListed ? min(a.m, a.m / (16 * RT) + owners) : owners * share;
+    const int out = kListed ? min(a.m, a.m / (16 * ET) + owners + 1) : (owners + 1) * share;
+    if constexpr (kListed && kFew)
+        lora_group_few_kernel<<<1, 512, group_lds(a.adapters), stream>>>(a, lists, in, out);
+    else if constexpr (kListed)
+        lora_group_kernel<<<1, 1024, group_lds(a.adapters), stream>>>(a, lists, RT == 4 ? 6 : 5, in, out);
     const int k_part = ((a.k + a.splits - 1) / a.splits + phase_of(WK) - 1) / phase_of(WK) * phase_of(WK);
-    const int64_t pieces = ((int64_t)a.m + 16 * ET - 1) / (16 * ET) * (((int64_t)a.n + 255) / 256);
-    const int walks = kFew ? 1 : (int)min(max(pieces / 768, (int64_t)1), (int64_t)4), step = 256 * walks, chunks = (int)(((int64_t)a.n + step - 1) / step);
-    const int64_t all = a.m, most = kFew ? min(all, ((int64_t)1 << 29) / max(a.ldx, max(a.ldb, a.ldy))) : max((1 << 20) / chunks, 1) * (16 * RT * ET);
-    for (int64_t at = 0; at < all && e == hipSuccess; at += most) {
-        LoraArgs b = a;
-        b.m = (int)min(all - at, most);
-        b.x += at * a.ldx;
-        b.ids += at;
-        b.base = a.base ? a.base + at * a.ldb : nullptr;
-        b.y += at * a.ldy;
-        const int tiles = (b.m + RT * 16 - 1) / (RT * 16);
-        if constexpr (kFew) {
-            const int groups = min(a.adapters, b.m), share = min(tiles, (2 * tiles + groups - 1) / groups);
-            lora_shrink_kernel<RT, RG, WK, D, true><<<dim3(share, a.splits, groups), 512, shrink_bytes, stream>>>(b, k_part);
-            lora_expand_few_kernel<KC><<<dim3(chunks, share, groups + 1), 256, expand_bytes, stream>>>(b);
-        } else {
-            const int wide = (b.m + ET * 16 - 1) / (ET * 16);
-            // (tiles with rows of several adapters: two workgroups share them in shrink, 24 us for 27; in expand one goes through them, 48 for 52)
-            const auto slots = [&](int64_t least, int64_t others) { return (int)min((int64_t)min(a.adapters, 16), max(1024 / others, least)); };
-            lora_shrink_kernel<RT, RG, WK, D, false><<<dim3(tiles * a.splits, 1, slots(2, (int64_t)tiles * a.splits)), 512, shrink_bytes, stream>>>(b, k_part);
-            lora_sum_kernel<<<(unsigned)(((int64_t)b.m * (a.r / 8) + 255) / 256), 256, 0, stream>>>(b);
-            lora_expand_kernel<KC, ET><<<dim3(wide * chunks, 1, slots(1, (int64_t)wide * chunks)), 256, expand_bytes, stream>>>(b, walks, chunks);
-        }
-        e = hipGetLastError();
+    lora_shrink_kernel<RT, RG, WK, D, kListed><<<in * a.splits, 512, shrink_bytes, stream>>>(a, lists, k_part, owners, share);
+    if constexpr (kFew) {
+        lora_expand_few_kernel<KC, kListed><<<dim3((a.n + 255) / 256, out), 256, expand_bytes, stream>>>(a, lists, owners + 1, share);
+    } else {
+        lora_sum_kernel<<<(a.m * (a.r / 8) + 255) / 256, 256, 0, stream>>>(a);
+        const int64_t pieces = ((int64_t)a.m + 16 * ET - 1) / (16 * ET) * ((a.n + 255) / 256);
+        const int walks = (int)min(max(pieces / 768, (int64_t)1), (int64_t)4), chunks = (a.n + 256 * walks - 1) / (256 * walks);
+        lora_expand_kernel<KC, ET><<<out * chunks, 256, expand_bytes, stream>>>(a, lists, walks, chunks);
     }
-    return e;
+    return hipGetLastError();
 }
 
-constexpr bool few(int64_t m) { return m < kFewRows; }
-
-}  // namespace
-
-int lora_splits(int64_t m, int64_t k, int64_t r)
+template <int RG, int D>
+hipError_t launch_few(const LoraArgs& a, hipStream_t stream)
 {
-    const int64_t rows = r > 64 ? 32 : 64, tiles = (m + rows - 1) / rows, phase = phase_of(few(m) ? 8 : 4), most = (k + phase - 1) / phase;
-    if (few(m))
+    return a.m <= kAlone ? launch<1, RG, 8, D, 1, false>(a, stream) : launch<1, RG, 8, D, 1, true>(a, stream);
+}
+
+int splits_of(int64_t m, int64_t k, int64_t r)
+{
+    const int64_t tiles = (m + rows_in(m, r) - 1) / rows_in(m, r), phase = phase_of(m < kSmall ? 8 : 4), most = (k + phase - 1) / phase;
+    if (m < kSmall)
         return (int)(most < kLoraSplits ? most : kLoraSplits);
-    // a power of two: neighbouring workgroups have the parts in turn, so a part of A's columns stays with the dies that have it
-    int s = kLoraSplits;
+    int s = kLoraSplits;                                        // a power of two: see shrink's parts
     while (s > 1 && (s > most || s * tiles > 1024))
         s /= 2;
     return s;
 }
 
-hipError_t launch_lora(const LoraArgs& a, const DeviceInfo&, hipStream_t stream)
+}  // namespace
+
+size_t lora_workspace(int64_t m, int64_t k, int64_t r)
 {
-    const int groups = (a.r + 15) / 16;
-    if (few(a.m))
-        return groups <= 1   ? launch<1, 1, 8, 4, true>(a, stream)
-               : groups <= 2 ? launch<1, 2, 8, 3, true>(a, stream)
-               : groups <= 4 ? launch<1, 4, 8, 2, true>(a, stream)
-                             : launch<1, 8, 8, 2, true>(a, stream);
-    return groups <= 2   ? launch<4, 2, 4, 2, false>(a, stream)
-           : groups <= 4 ? launch<4, 4, 2, 3, false>(a, stream)
-                         : launch<2, 8, 4, 2, false>(a, stream);
+    m = m < kWindow ? m : kWindow;
+    // (a window that far strides make smaller may have more parts, but not of more than 1024 workgroups' rows)
+    const int64_t rows = m < kSmall ? splits_of(m, k, r) * m : min(kLoraSplits * m, max(m, (int64_t)1024 * rows_in(m, r)));
+    return (size_t)(rows * r) * 4 + (m > kAlone ? (size_t)m * (2 * sizeof(Item) + 4) : 0);
+}
+
+hipError_t launch_lora(const LoraArgs& whole, const DeviceInfo&, hipStream_t stream)
+{
+    const int64_t most = window(whole);
+    const int ranks = (whole.r + 15) / 16;
+    for (int64_t at = 0; at < whole.m; at += most) {
+        LoraArgs a = whole;
+        a.m = (int)min(whole.m - at, most);
+        a.x += at * a.ldx;
+        a.ids += at;
+        a.base = a.base ? a.base + at * a.ldb : nullptr;
+        a.y += at * a.ldy;
+        a.splits = splits_of(a.m, a.k, a.r);
+        hipError_t e;
+        if (a.m < kSmall)
+            e = ranks <= 1   ? launch_few<1, 4>(a, stream)
+                : ranks <= 2 ? launch_few<2, 3>(a, stream)
+                : ranks <= 4 ? launch_few<4, 2>(a, stream)
+                             : launch_few<8, 2>(a, stream);
+        else
+            e = ranks <= 2   ? launch<4, 2, 4, 2, 2, true>(a, stream)
+                : ranks <= 4 ? launch<4, 4, 2, 3, 2, true>(a, stream)
+                             : launch<2, 8, 4, 2, 2, true>(a, stream);
+        if (e != hipSuccess)
+            return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace mxfp4
