@@ -340,6 +340,22 @@ def test_adapters_of_every_row_its_own_and_of_one():
         plain.near(binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales), *plain.adapters(x, a, b, ids, base, scales))
 
 
+@pytest.mark.parametrize("m,n,k,rank,many", [(40, 264, 264, 16, 60), (127, 72, 520, 40, 60), (129, 520, 136, 8, 60), (400, 72, 72, 128, 30), (8200, 40, 24, 8, 9),
+                                             (16500, 24, 40, 72, 3), (5, 8, 8, 8, 8192), (260, 8, 8, 8, 8192), (1100, 16, 8, 8, 8192)])
+def test_adapters_of_uneven_shares(m, n, k, rank, many):
+    """Nearly all rows of one adapter (runs of whole waves and broken ones), the others' rows in between; very many rows; as many adapters as may be."""
+    x, base = _bf16((m, k), 3), _bf16((m, n), 4)
+    a, b, scales = _stack(many, rank, n, k, 5)
+    ids = torch.where(torch.rand(m, generator=_gen(6)) < 0.02, _ids(m, many, "mixed", 7).cpu(), torch.tensor(many // 2, dtype=torch.int32)).to(DEV)
+    ids[m // 2 : m // 2 + m // 4] = many - 1
+    y = binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales)
+    plain.near(y, *plain.adapters(x, a, b, ids, base, scales))
+    assert torch.equal(binding.mxfp4_lora(x, a, b, ids, base=base, scales=scales), y)
+    own = base.clone()
+    binding.mxfp4_lora(x, a, b, ids, base=own, scales=scales, y=own)
+    assert torch.equal(own, y)
+
+
 # ---- together ---------------------------------------------------------------------------------------------------------
 
 def _layer(x, r, w, q, s, a, b, ids, scales):
