@@ -14,10 +14,11 @@
 //     by position: [step][block][wave row][i][tile], so that one read gives a lane the bytes of all its tiles, which the
 //     instruction takes by number.  Blocks past K get zero bytes, as their codes load as zeros.
 //
-// 4003 rows x 22016 x 4096 with the gate: 311 us, 2.32 PFLOP/s (a loop of the bare instruction 4.5 of random numbers).  The matrix units are busy for
-// 62 % of the cycles, at a clock that their power draw lowers (all zeros: 9 % less time); the LDS for a third, without conflicts; waves wait for
-// 39 % of their time, mostly at the step's barrier.  Blocks of 256 x 256 have 2/3 of the traffic of 128 x 256; four waves of twice the tile
-// read 40 % less from the LDS and were slower (351 us, 337 with eight then), and so were loads two steps ahead (326, 319).
+// 4003 rows x 22016 x 4096 with the gate: 311 to 327 us by the card's clock, 2.2 to 2.3 PFLOP/s (a loop of the bare instruction: 4.5, of random
+// numbers).  The matrix units are busy for 62 % of the cycles, at a clock that their power draw lowers (all zeros: 9 % less time); the LDS for a third,
+// without conflicts; waves wait for 39 % of their time.  That is in blocks of 128 x 256, two on a unit, which fill the last round better than those of
+// 256 x 256 with their 2/3 of the traffic; alone they take the same time.  In 256 x 256, four waves of twice the tile read 40 % less from the
+// LDS and were slower (351 us, 337 with eight then), and so were loads two steps ahead (326, 319).
 #include "block_out.h"
 #include "gemm_a8.h"
 
