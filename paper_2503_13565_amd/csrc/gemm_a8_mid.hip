@@ -61,10 +61,11 @@ __global__ __launch_bounds__(512, 2) void w4a8_mid_kernel(const uint8_t* __restr
         chunk[c] = of_x ? piece % (S * 8) ^ turn(row, S * 8) : piece % (S * 4) ^ turn(row, S * 4);
         off[c] = u >= kUnits ? kOob : of_x ? (row * k + chunk[c] * 16) | past(rows - 1, row) : (row * (k >> 1) + chunk[c] * 16) | past(cols - 1, row);
     }
-    auto issue = [&](int p, int b) {                            // (past K's end: zeros, so that the loads of a phase are as many)
+    // A quarter of a phase's loads (past K's end: zeros, so that the loads of a phase are as many).
+    auto issue = [&](int p, int b, auto quarter) {
         const int t = min(p * S, steps);
 #pragma unroll
-        for (int c = 0; c < C; ++c) {
+        for (int c = decltype(quarter)::value; c < C; c += 4) {
             const int u = c * 8 + wave;
             if (u < kX)
                 direct(lds_at + b * kBuf + u * 1024, off[c] | past((k >> 4) - 1, t * 8 + chunk[c]), rx, t * 128);
@@ -98,28 +99,39 @@ __global__ __launch_bounds__(512, 2) void w4a8_mid_kernel(const uint8_t* __restr
     const int x_row = wm * MF * 32 + li, w_row = wn * NF * 32 + wrow;
     const int x_read = x_row * (S * 128) + ((8 * wk + lh) ^ turn(x_row, S * 8)) * 16;
     const int w_read = kX * 1024 + w_row * (S * 64) + ((4 * wk + lh) ^ turn(w_row, S * 4)) * 16;
-    int xs_shift[MF], ws_shift[NF];                             // in bits: where the row's first byte is in its dword
+    int xs_first[MF], ws_first[NF];                             // where the row's first byte is in its dword
 #pragma unroll
     for (int f = 0; f < MF; ++f)
-        xs_shift[f] = 8 * (((x_row + f * 32) * nblk) & 3);
+        xs_first[f] = ((x_row + f * 32) * nblk) & 3;
 #pragma unroll
     for (int f = 0; f < NF; ++f)
-        ws_shift[f] = 8 * (((w_row + f * 32) * nblk) & 3);
+        ws_first[f] = ((w_row + f * 32) * nblk) & 3;
     const uint8_t *xs_read = smem + D * kBuf + x_row * kScaleRow, *ws_read = smem + D * kBuf + kSx * 1024 + w_row * kScaleRow;
-    auto read_scales = [&](int p) {
-        const int part16 = p / kPhases, in = (part16 & 1) * (kScaleUnits * 1024) + ((p % kPhases) * S + wk) * 4;
-        const int have = nblk - 4 * (p * S + wk);                // blocks of this step; behind the last, the bytes are another row's
-        const uint32_t keep = have >= 4 ? 0xFFFFFFFFu : have <= 0 ? 0u : (1u << (8 * have)) - 1u;
-        auto bytes = [&](const uint8_t* row, int shift) {
+    // A phase's dwords may leave for registers beside the instructions of the phase before, which still need theirs, and are moved behind these.
+    uint2 xs_raw[MF], ws_raw[NF];
+    auto fetch_scales = [&](int p) {
+        const int in = ((p / kPhases) & 1) * (kScaleUnits * 1024) + ((p % kPhases) * S + wk) * 4;
+        const auto two = [&](const uint8_t* row) {
             const uint32_t* at = reinterpret_cast<const uint32_t*>(row + in);
-            return ((uint32_t)(((uint64_t)at[1] << 32 | at[0]) >> shift) & keep) >> (8 * lh);
+            return make_uint2(at[0], at[1]);
         };
 #pragma unroll
         for (int f = 0; f < MF; ++f)
-            xs_of[f] = bytes(xs_read + f * (32 * kScaleRow), xs_shift[f]);
+            xs_raw[f] = two(xs_read + f * (32 * kScaleRow));
 #pragma unroll
         for (int f = 0; f < NF; ++f)
-            ws_of[f] = bytes(ws_read + f * (32 * kScaleRow), ws_shift[f]);
+            ws_raw[f] = two(ws_read + f * (32 * kScaleRow));
+    };
+    auto take_scales = [&](int p) {
+        const int have = nblk - 4 * (p * S + wk);               // blocks of this step; behind the last, the bytes are another row's
+        const uint32_t keep = have >= 4 ? 0xFFFFFFFFu : have <= 0 ? 0u : (1u << (8 * have)) - 1u;
+        const auto bytes = [&](const uint2& raw, int first) { return (__builtin_amdgcn_alignbyte(raw.y, raw.x, first) & keep) >> (8 * lh); };
+#pragma unroll
+        for (int f = 0; f < MF; ++f)
+            xs_of[f] = bytes(xs_raw[f], xs_first[f]);
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+            ws_of[f] = bytes(ws_raw[f], ws_first[f]);
     };
     auto read = [&](int b, int kh, Half& h) {                   // half kh of the phase in buffer b
         const uint8_t* buf = smem + b * kBuf;
@@ -150,31 +162,54 @@ __global__ __launch_bounds__(512, 2) void w4a8_mid_kernel(const uint8_t* __restr
     issue_scales(0);
 #pragma unroll
     for (int d = 0; d < D; ++d)
-        issue(d, d);
+        each<4>([&](auto quarter) { issue(d, d, quarter); });
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * C) : "memory");
     lds_barrier();
     issue_scales(1);
-    read_scales(0);
+    fetch_scales(0);
+    take_scales(0);
     read(0, 0, half[0]);
-    int b = 0;
+    int b = 0, before = D - 1;
+    // Where two phases are on their way, the loads of another go out a quarter at a time between the reads and the instructions: all at once behind
+    // the barrier, the waves of all SIMDs wait for the way out (16 cycles a load) before they read (128 x 4096 x 4096 10.0 us, 9.7 so).  Where it is one,
+    // every cycle that they leave earlier counts (128 x 22016 x 4096 23.9 us, 27.3 in quarters), and so does a register (25.7 with the scales fetched early).
+    constexpr bool kSpread = D > 2;
+    constexpr std::integral_constant<int, 0> first;
+    constexpr std::integral_constant<int, 1> second;
+    constexpr std::integral_constant<int, 2> third;
+    constexpr std::integral_constant<int, 3> fourth;
     for (int p = 0; p < phases; ++p) {
         const int next = b == D - 1 ? 0 : b + 1;
         read(b, 1, half[1]);
+        if (kSpread && p)
+            issue(p - 1 + D, before, third);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(half[0], std::integral_constant<int, 0>{});
+        multiply(half[0], first);
         __builtin_amdgcn_sched_barrier(0);
+        if (kSpread && p)
+            issue(p - 1 + D, before, fourth);
         // The next phase is here when no more loads than those of the phases behind it are on their way (with scales among them, a wait is longer); this one's
         // buffer is free when every wave has its second half in registers.
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 2) * C) : "memory");
         lds_barrier();
-        issue(p + D, b);
+        if constexpr (kSpread)
+            issue(p + D, b, first);
+        else
+            each<4>([&](auto quarter) { issue(p + D, b, quarter); });
         if (p % kPhases == kPhases - 1)
             issue_scales(p / kPhases + 2);                      // (of the sixteen steps behind the next: into the place of those that end here)
+        if (kSpread)
+            fetch_scales(p + 1);
         read(next, 0, half[0]);
         __builtin_amdgcn_sched_barrier(0);
-        multiply(half[1], std::integral_constant<int, 1>{});
-        read_scales(p + 1);
+        multiply(half[1], second);
+        if (kSpread)
+            issue(p + D, b, second);
+        if (!kSpread)
+            fetch_scales(p + 1);
+        take_scales(p + 1);
         __builtin_amdgcn_sched_barrier(0);
+        before = b;
         b = next;
     }
     drain_vmem();                                               // (the loads behind the last phase write the LDS)
