@@ -7,9 +7,10 @@
 // that no wait of the compiler's stands in front of: they come into the LDS by direct loads too, sixteen steps at a time (64 bytes a row and up to 16
 // around them: a row of K / 32 bytes may start anywhere, a load starts at a dword; 80 bytes from row to row put two lanes on a bank), and a lane reads a
 // step's four in two dwords and moves its own to the bytes that the instruction names.
-// Bound by the lines that a unit gets from beyond its die's cache (80 to 90 bytes a ns whatever is in flight; 64-byte pieces 52) and by the chain from a
-// phase's arrival to its sums: 77 rows x 4096 x 11008 15.0 us in 192 blocks of 32 x 64 (24 MB, 5.3 us at a copy's rate; each block's 704 KB at 47 bytes a
-// ns).  K cut across workgroups with a second kernel that adds was slower (17 to 18 us).
+// Bound by the walk of each block, and for larger ones by the lines that a unit gets from beyond its die's cache (80 to 90 bytes a ns).  77 rows x
+// 4096 x 11008 take 14.4 us in 192 blocks of 32 x 64 (24 MB, 5.3 us at a copy's rate): start, first phase and end are 4.9, and in the 21 phases behind it
+// loads, scales and matrix instructions wait for each other in part (each left out alone saves 3.8, 2.5 and 3.1).  No gain: four phases in the
+// LDS, eight waves along K, sixteen waves; K cut across workgroups with a second kernel that adds was slower (17 to 18 us).
 #include "block_out.h"
 #include "gemm_a8.h"
 
