@@ -59,13 +59,6 @@ struct Lists {
 };
 
 constexpr int rows_in(int64_t m, int64_t r) { return m < kSmall ? 16 : r > 64 ? 32 : 64; }
-constexpr int rows_out(int64_t m) { return m < kSmall ? 16 : 32; }
-
-__device__ __forceinline__ int adapter_of(const LoraArgs& a, int row, int none)
-{
-    const int id = a.ids[row];
-    return id >= 0 && id < a.adapters ? id : none;
-}
 
 // T threads with U rows each, all ids at once.  `lds`: four numbers an adapter (and as many for none), kGroupBytes in front.  Items of 2^in_shift and
 // 2^out_shift rows, in_most and out_most of them (those behind the last: nothing).
@@ -568,8 +561,11 @@ __global__ __launch_bounds__(256, KC == 16 ? 2 : 3) void lora_expand_kernel(Lora
     }
 }
 
-// The rows of one set of launches: lists are made by one workgroup, and offsets into x, base and y have 31 bits.
-int64_t window(const LoraArgs& a) { return min((int64_t)min(a.m, kWindow), ((int64_t)1 << 29) / max(a.ldx, max(a.ldb, a.ldy))); }
+// The rows of one set of launches: lists are made by one workgroup, offsets into x, base and y have 31 bits, and a grid less than 2^32 threads.
+int64_t window(const LoraArgs& a)
+{
+    return min(min((int64_t)min(a.m, kWindow), ((int64_t)1 << 29) / max(a.ldx, max(a.ldb, a.ldy))), max(((int64_t)1 << 31) / a.n, (int64_t)64));
+}
 
 // The launches of one window: RT tiles of sixteen rows and RG of ranks in shrink, ET tiles of rows in expand; kListed: with the sort in front.
 template <int RT, int RG, int WK, int D, int ET, bool kListed>
@@ -598,8 +594,8 @@ hipError_t launch(const LoraArgs& a, hipStream_t stream)
     lists.in = reinterpret_cast<Item*>(a.part + (int64_t)a.splits * a.m * a.r);
     lists.out = lists.in + a.m;
     lists.order = reinterpret_cast<int*>(lists.out + a.m);
-    // (an adapter's last item may have fewer rows than others, and so may that of the rows of none)
-    // (two workgroups an adapter at least: 128 rows of one among 60, 4096 -> 4096, rank 16, 17.2 us for 25.5; 12.2 for 11.4 where the rows are mixed)
+    // An adapter's last item may have fewer rows than the others, and so may that of the rows of none.  Without lists, two workgroups an adapter
+    // at least: 128 rows of one among 60, 4096 -> 4096, rank 16, 17.2 us for 25.5; 12.2 for 11.4 where the rows are mixed.
     const int owners = min(a.adapters, a.m), tiles = (a.m + 15) / 16, share = min(tiles, max(2, (2 * tiles + owners - 1) / owners));
     const int in = kListed ? min(a.m, a.m / (16 * RT) + owners) : owners * share;
     const int out = kListed ? min(a.m, a.m / (16 * ET) + owners + 1) : (owners + 1) * share;

@@ -121,6 +121,13 @@ def test_norm_of_many_rows(m, k):
         assert torch.equal(got.q8, code) and torch.equal(got.s, scale)
 
 
+def test_norm_of_more_rows_than_a_launch_has():
+    m, k = (1 << 21) + 37, 8
+    x, r = _bf16((m, k), 5), _bf16((m, k), 6, 0.3)
+    got = binding.mxfp4_rms_norm(x, None, residual=r, eps=1e-5)
+    _check_norm(x, None, r, 1e-5, got)
+
+
 def test_norm_of_rows_that_are_not_finite():
     x = _bf16((4, 4096), 6).cpu()
     x[0, 7], x[1, 9], x[2, 11] = NAN, INF, -INF
