@@ -3,6 +3,7 @@
 
 #include <utility>
 
+#include "a8_stage.h"
 #include "common.h"
 #include "layer.h"
 #include "../../include/mxfp4.h"
@@ -11,11 +12,6 @@ namespace mxfp4 {
 namespace a8 {
 
 typedef __attribute__((ext_vector_type(8))) int i32x8_t;
-
-constexpr int kOob = 0x7FFFFFF0;        // lane offset beyond any descriptor: the load returns zero
-
-// 0 where at <= last, else an offset beyond any descriptor (arithmetic, as a branch around a load makes the compiler wait for it).
-__device__ __forceinline__ int past(int last, int at) { return ((last - at) >> 31) & kOob; }
 
 __device__ __forceinline__ f32x4_t mfma(u32x4_t w, const u32x4_t* x, f32x4_t sum, uint32_t ws, uint32_t xs)
 {
@@ -89,10 +85,6 @@ __device__ __forceinline__ void finish(const Out& o, int m, int n, f32x4_t z)
         o.y[m * o.ldy + n + i] = f32_to_bf16_rne(z[i]);
     }
 }
-
-// Which of a row's chunks of 16 bytes (a power of two) takes the first place: 256 bytes of the LDS then hold sixteen rows' chunks of
-// one number, so that the sixteen lanes that a turn of the LDS serves find sixteen different places.
-constexpr __device__ int turn(int row, int chunks) { return chunks >= 16 ? row & 15 : row / (16 / chunks) & (chunks - 1); }
 
 typedef __attribute__((ext_vector_type(16))) float f32x16_t;
 

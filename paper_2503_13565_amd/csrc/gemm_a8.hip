@@ -59,20 +59,19 @@ __global__ __launch_bounds__(512) void w4a8_rows_kernel(const uint8_t* __restric
     for (int c = 0; c < C; ++c) {
         const int u = c * 8 + wave;
         const bool of_x = u < kX;
-        const int at = (of_x ? u : u - kX) * 64 + lane;
-        const int row = of_x ? at / (WK * 8) : at / (WK * 4);
-        chunk[c] = of_x ? at % (WK * 8) ^ turn(row, WK * 8) : at % (WK * 4) ^ turn(row, WK * 4);
-        off[c] = u >= kUnits ? kOob : of_x ? (row * k + chunk[c] * 16) | past(rows - 1, row) : (row * (k >> 1) + chunk[c] * 16) | past(cols - 1, row);
+        const int piece = (of_x ? u : u - kX) * 64 + lane;
+        chunk[c] = of_x ? piece_chunk(piece, WK * 8) : piece_chunk(piece, WK * 4);
+        off[c] = u >= kUnits ? kOob : of_x ? piece_offset(piece, WK * 8, rows, k) : piece_offset(piece, WK * 4, cols, k >> 1);
     }
     auto issue = [&](int p, int b) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            const int u = c * 8 + wave;
+            const int u = c * 8 + wave, t = p * WK;
             if (u < kX)
-                direct(lds_at + b * kBuf + u * 1024, off[c] | past((k >> 4) - 1, p * (WK * 8) + chunk[c]), rx, p < phases ? p * (WK * 128) : 0);
+                direct(lds_at + b * kBuf + u * 1024, off[c] | past((k >> 4) - 1, phase_chunk(t, steps, 128) + chunk[c]), rx, phase_from(t, steps, 128));
             else
-                direct(lds_at + (u < kUnits ? b * kBuf + u * 1024 : kFixed - 1024), off[c] | past(nblk - 1, p * (WK * 4) + chunk[c]), rq,
-                       p < phases ? p * (WK * 64) : 0);
+                direct(lds_at + (u < kUnits ? b * kBuf + u * 1024 : kFixed - 1024), off[c] | past(nblk - 1, phase_chunk(t, steps, 64) + chunk[c]), rq,
+                       phase_from(t, steps, 64));
         }
     };
 

@@ -58,20 +58,20 @@ __global__ __launch_bounds__(512, 2) void w4a8_mid_kernel(const uint8_t* __restr
         const int u = c * 8 + wave;
         const bool of_x = u < kX;
         const int piece = (of_x ? u : u - kX) * 64 + lane;
-        const int row = of_x ? piece / (S * 8) : piece / (S * 4);
-        chunk[c] = of_x ? piece % (S * 8) ^ turn(row, S * 8) : piece % (S * 4) ^ turn(row, S * 4);
-        off[c] = u >= kUnits ? kOob : of_x ? (row * k + chunk[c] * 16) | past(rows - 1, row) : (row * (k >> 1) + chunk[c] * 16) | past(cols - 1, row);
+        chunk[c] = of_x ? piece_chunk(piece, S * 8) : piece_chunk(piece, S * 4);
+        off[c] = u >= kUnits ? kOob : of_x ? piece_offset(piece, S * 8, rows, k) : piece_offset(piece, S * 4, cols, k >> 1);
     }
     // A quarter of a phase's loads (past K's end: zeros, so that the loads of a phase are as many).
     auto issue = [&](int p, int b, auto quarter) {
-        const int t = min(p * S, steps);
+        const int t = p * S;
 #pragma unroll
         for (int c = decltype(quarter)::value; c < C; c += 4) {
             const int u = c * 8 + wave;
             if (u < kX)
-                direct(lds_at + b * kBuf + u * 1024, off[c] | past((k >> 4) - 1, t * 8 + chunk[c]), rx, t * 128);
+                direct(lds_at + b * kBuf + u * 1024, off[c] | past((k >> 4) - 1, phase_chunk(t, steps, 128) + chunk[c]), rx, phase_from(t, steps, 128));
             else
-                direct(lds_at + (u < kUnits ? b * kBuf + u * 1024 : D * kBuf + 2048 * kScaleUnits), off[c] | past(nblk - 1, t * 4 + chunk[c]), rq, t * 64);
+                direct(lds_at + (u < kUnits ? b * kBuf + u * 1024 : D * kBuf + 2048 * kScaleUnits), off[c] | past(nblk - 1, phase_chunk(t, steps, 64) + chunk[c]),
+                       rq, phase_from(t, steps, 64));
         }
     };
     auto issue_scales = [&](int part16) {                       // of the sixteen steps from 16 part16 on
