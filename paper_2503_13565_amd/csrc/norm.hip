@@ -9,7 +9,7 @@
 // (two thirds are reads).
 //
 // Squares leave FP32's range before the values do (above 2^64 or with h = x + r beyond the largest number).  Where the sum says so the row
-// is scaled by a power of two, which y does not depend on: the rare row reads its inputs again, every other pays one comparison.
+// is scaled by the power of two of its largest h, which y does not depend on: the rare row reads its inputs again, every other pays one comparison.
 #include "cast_block8.h"
 #include "common.h"
 #include "layer.h"
@@ -111,17 +111,19 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void rms_norm_kernel(NormArgs a,
                 sums[i][e] = f32_to_bf16_rne2(h[i][2 * e], h[i][2 * e + 1]);
     inv = rsqrtf(fmaf(ss, inverse_k, a.eps));
     if (!(ss < INFINITY) || (ss < kSmall && a.eps < kSmallEps)) {
+        // From h / 2, which no addition brings out of FP32 and which is exact where h is: the power of two has to follow h, not x and r, as these may cancel.
+        const auto half = [](float v, float u) { return fmaf(u, 0.5f, v * 0.5f); };
         float top = 0.f;
         for (int c = t; c < chunks; c += T) {
-            const u32x4_t v = chunk(x, c), u = r ? chunk(r, c) : u32x4_t{0, 0, 0, 0};
+            const u32x4_t v = chunk(x, c), u = r ? chunk(r, c) : u32x4_t{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};
             for (int e = 0; e < 4; ++e)
-                top = fmaxf(fmaxf(top, fmaxf(fabsf(low(v[e])), fabsf(high(v[e])))), fmaxf(fabsf(low(u[e])), fabsf(high(u[e]))));
+                top = fmaxf(top, fmaxf(fabsf(half(low(v[e]), low(u[e]))), fabsf(half(high(v[e]), high(u[e])))));
         }
         top = row_reduce<T, true>(top, lds);
         // 2^-126 .. 2^126; a row with infinities has them in its sums, a row of NaN keeps them (the maximum leaves NaN out)
         const int exponent = (int)(__float_as_uint(top) >> 23);
         factor = __uint_as_float((uint32_t)min(max(254 - exponent, 1), 253) << 23);
-        const float eps = a.eps * factor * factor;
+        const float eps = a.eps * (0.5f * factor) * (0.5f * factor);
         if (top > 0.f && eps < INFINITY) {
             float s2 = 0.f;
 #pragma unroll
@@ -130,13 +132,12 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void rms_norm_kernel(NormArgs a,
                 u32x4_t v = {0, 0, 0, 0}, u = {0, 0, 0, 0};
                 if (c < chunks) {
                     v = chunk(x, c);
-                    if (r)
-                        u = chunk(r, c);
+                    u = r ? chunk(r, c) : u32x4_t{0x80008000u, 0x80008000u, 0x80008000u, 0x80008000u};      // (-0, which changes nothing)
                 }
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    h[i][2 * e] = fmaf(low(u[e]), factor, low(v[e]) * factor);
-                    h[i][2 * e + 1] = fmaf(high(u[e]), factor, high(v[e]) * factor);
+                    h[i][2 * e] = half(low(v[e]), low(u[e])) * factor;
+                    h[i][2 * e + 1] = half(high(v[e]), high(u[e])) * factor;
                     s2 = fmaf(h[i][2 * e], h[i][2 * e], s2);
                     s2 = fmaf(h[i][2 * e + 1], h[i][2 * e + 1], s2);
                 }
