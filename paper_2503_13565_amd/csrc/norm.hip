@@ -109,8 +109,9 @@ __global__ __launch_bounds__(T <= 64 ? 256 : T) void rms_norm_kernel(NormArgs a,
 #pragma unroll
             for (int e = 0; e < 4; ++e)
                 sums[i][e] = f32_to_bf16_rne2(h[i][2 * e], h[i][2 * e + 1]);
-    inv = rsqrtf(fmaf(ss, inverse_k, a.eps));
-    if (!(ss < INFINITY) || (ss < kSmall && a.eps < kSmallEps)) {
+    const float mean = fmaf(ss, inverse_k, a.eps);              // (infinite or NaN where ss is, and where only the addition of eps leaves FP32)
+    inv = rsqrtf(mean);
+    if (!(mean < INFINITY) || (ss < kSmall && a.eps < kSmallEps)) {
         // From h / 2, which no addition brings out of FP32 and which is exact where h is: the power of two has to follow h, not x and r, as these may cancel.
         const auto half = [](float v, float u) { return fmaf(u, 0.5f, v * 0.5f); };
         float top = 0.f;

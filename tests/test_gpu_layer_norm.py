@@ -41,3 +41,14 @@ def test_norm_of_a_residual_that_cancels(m, k):
     x[8::3, 5] *= 2
     for eps in (1e-30, 0.0, 1e-38, 1e-5):
         _check(x, r, eps)
+
+
+@pytest.mark.parametrize("m", [1, 300])
+@pytest.mark.parametrize("k", [8, 64, 4096, 8192])
+def test_norm_of_an_eps_near_the_largest_number(m, k):
+    """The mean and eps are FP32 numbers, their sum is not."""
+    gen = torch.Generator().manual_seed(k)
+    x = (0.5 + torch.rand((m, k), generator=gen)).to(torch.bfloat16)
+    for size in (2.0 ** 127 / k, 2.0 ** 126, 2.0 ** 100):
+        _check((x * (size ** 0.5)).to(torch.bfloat16), None, 3.3e38)
+        _check((x * (size ** 0.5)).to(torch.bfloat16), (x * (size ** 0.5) / 4).to(torch.bfloat16), 3.4e38)
