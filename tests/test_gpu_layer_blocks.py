@@ -1,4 +1,4 @@
-"""The product of 8-bit rows in its larger blocks (gemm_a8_mid.hip, gemm_a8_block.hip) on the GPU, against the definition in 64 bits (layer_plain.py).  Which
+"""The product of 8-bit rows on the GPU, its larger blocks (gemm_a8_mid.hip, gemm_a8_block.hip) above all, against the definition in 64 bits (layer_plain.py).  Which
 block a call takes follows from its sizes and the device's units; the sizes here are for 256 of them."""
 import pytest
 import torch
@@ -30,3 +30,22 @@ def test_product_of_a_last_block_of_a_row_and_a_column(m, n, k):
     q, s = binding.mxfp4_direct_cast(_bf16((n, k), 2, 0.05, 4.0))
     y = binding.mxfp4_w4a8_gemm(x8, xs, q, s)
     plain.near(y, *plain.product(x8, xs, q, s, device=DEV))
+
+
+@pytest.mark.parametrize("m", [2, 9, 30, 300])
+def test_product_of_a_closed_gate(m):
+    """Gates from -86 to -88.5, whose silu is 2^-118 and less, beside numbers that bring it back; some at the other ends of FP32.  Codes of zero, so that
+    the sums are the bias."""
+    n, k = 9000 if m > 30 else 200, 64
+    bias = torch.empty((n,), device=DEV)
+    bias[0::2] = torch.tensor([-86, -86.5, -87, -87.5, -88, -88.5, 3e38, 1e-36], device=DEV).repeat(n // 16 + 1)[: n // 2]
+    bias[1::2] = 1.0e38 * (1 + torch.arange(n // 2, device=DEV) % 5 * 0.5)
+    bias[13::16] = 0.5
+    bias = bias.to(torch.bfloat16)
+    x8, xs = torch.zeros((m, k), dtype=torch.uint8, device=DEV), torch.full((m, k // 32), 127, dtype=torch.uint8, device=DEV)
+    q, s = torch.zeros((n, k // 2), dtype=torch.uint8, device=DEV), torch.full((n, k // 32), 127, dtype=torch.uint8, device=DEV)
+    y = binding.mxfp4_w4a8_gemm(x8, xs, q, s, bias=bias, act=binding.ACT_SWIGLU)
+    g, u = bias.double()[0::2], bias.double()[1::2]
+    want = (g * torch.sigmoid(g) * u).expand(m, -1)
+    # e^-g through a power of two whose argument (128 at most) is rounded: 127 2^-24; the power, the reciprocal and the products: a step or two each
+    plain.near(y, want, want.abs() * (2.0 ** -16 + plain.ROUND))
