@@ -244,9 +244,26 @@ a8::Shape shape_of(int64_t m, int64_t n, int64_t k, const DeviceInfo& dev)
 
 }  // namespace
 
-hipError_t launch_w4a8(const A8Args& a, const DeviceInfo& dev, hipStream_t stream)
+hipError_t launch_w4a8(const A8Args& whole, const DeviceInfo& dev, hipStream_t stream)
 {
     using namespace a8;
+    // A grid holds less than 2^32 threads (a larger one is cut without an error), so very many weight rows are several launches: 2^26 of them are 2^22
+    // workgroups of the narrowest blocks.  (Very many rows of x: each kernel's launch.)
+    constexpr int kMost = 1 << 26;
+    A8Args a = whole;
+    for (int64_t at = 0; whole.n - at > kMost; at += kMost) {
+        a.n = kMost;
+        const hipError_t e = launch_w4a8(a, dev, stream);
+        if (e != hipSuccess)
+            return e;
+        const int64_t columns = a.epi.act == MXFP4_ACT_SWIGLU ? kMost / 2 : kMost;
+        a.q += (int64_t)kMost * (a.k >> 1);
+        a.s += (int64_t)kMost * (a.k >> 5);
+        a.epi.bias = a.epi.bias ? a.epi.bias + kMost : nullptr;
+        a.epi.residual = a.epi.residual ? a.epi.residual + columns : nullptr;
+        a.y += columns;
+        a.n = (int)(whole.n - at - kMost);
+    }
     const Shape shape = shape_of(a.m, a.n, a.k, dev);
     switch (shape) {
     case kRows1:

@@ -49,3 +49,34 @@ def test_product_of_a_closed_gate(m):
     want = (g * torch.sigmoid(g) * u).expand(m, -1)
     # e^-g through a power of two whose argument (128 at most) is rounded: 127 2^-24; the power, the reciprocal and the products: a step or two each
     plain.near(y, want, want.abs() * (2.0 ** -16 + plain.ROUND))
+
+
+@pytest.mark.parametrize("m,gate", [(1, False), (1, True), (20, False)])
+def test_product_of_more_weight_rows_than_a_launch_has(m, gate):
+    """Grids of sixteen weight rows a workgroup end at 2^27.  Ones against any codes: sums of 32 multiples of 1/2, exact."""
+    n, k = (1 << 27) + 54, 32
+    gen = torch.Generator(device=DEV).manual_seed(m)
+    q = torch.randint(0, 256, (n, k // 2), generator=gen, dtype=torch.uint8, device=DEV)
+    s = torch.randint(126, 129, (n, 1), generator=gen, dtype=torch.uint8, device=DEV)
+    x8, xs = torch.full((m, k), 0x38, dtype=torch.uint8, device=DEV), torch.arange(m, dtype=torch.int32, device=DEV)[:, None]
+    c = n // 2 if gate else n
+    bias = torch.randint(-4, 5, (n,), generator=gen, device=DEV).to(torch.bfloat16)
+    residual = torch.randint(-4, 5, (m, c), generator=gen, dtype=torch.int8, device=DEV).to(torch.bfloat16)
+    y = binding.mxfp4_w4a8_gemm(x8, (127 - xs % 3).to(torch.uint8), q, s, bias=bias, act=binding.ACT_SWIGLU if gate else binding.ACT_NONE, residual=residual)
+    grid = torch.tensor([0, .5, 1, 1.5, 2, 3, 4, 6, 0, -.5, -1, -1.5, -2, -3, -4, -6], device=DEV)
+    two = grid.repeat(16) + grid.repeat_interleave(16)
+    scale = torch.exp2(-(xs % 3).float())
+    for at in range(0, n, 1 << 22):
+        z = (two[q[at : at + (1 << 22)].int()].sum(1) * torch.exp2(s[at : at + (1 << 22), 0].float() - 127))[None] * scale + bias[at : at + (1 << 22)].float()
+        off = torch.zeros_like(z)
+        if gate:
+            g, u = z.double()[:, 0::2], z.double()[:, 1::2]
+            z = g * torch.sigmoid(g) * u
+            # e^-g and the products around it: see the closed gates; below -88.72 e^-g is no FP32 number and the gate is 0, where
+            # |g| / (1 + e^-g) falls as g does and is less than 88.8 2^-128 < 2^-121
+            off = 2.0 ** -16 * z.abs() + (g < -88.72) * 2.0 ** -121 * u.abs()
+        lo = at // 2 if gate else at
+        z = z + residual[:, lo : lo + z.shape[1]]
+        off = off + (plain.ROUND + plain.STEP * gate) * z.abs()
+        bad = torch.nonzero(~((y[:, lo : lo + z.shape[1]].double() - z.double()).abs() <= off.double()))
+        assert not len(bad), "%d off behind %d, first at %r: %r for %r" % (len(bad), lo, bad[0].tolist(), float(y[bad[0][0], lo + bad[0][1]]), float(z[tuple(bad[0])]))
