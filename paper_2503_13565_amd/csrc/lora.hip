@@ -324,11 +324,12 @@ __device__ __forceinline__ u32x4_t sum_of(const LoraArgs& a, int64_t at, float s
     u32x4_t o;
 #pragma unroll
     for (int e = 0; e < 4; e += 2) {
-        // cut off, not rounded: the largest numbers stay finite; an infinity leaves no rest
-        auto cut = [](float v) { return v == v ? __float_as_uint(v) >> 16 : 0x7FC0u; };
-        auto rest = [](float v) { const float d = v - __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); return d == d ? d : 0.f; };
-        o[e >> 1] = cut(t[e]) | cut(t[e + 1]) << 16;
-        o[2 + (e >> 1)] = f32_to_bf16_rne2(rest(t[e]), rest(t[e + 1]));
+        // cut off, not rounded: the largest numbers stay finite.  A number of few bits is cut below itself, so that the lower part of none but 0 is 0:
+        // that would make NaN of an infinity of B.  (Infinity itself: the largest number and infinity; NaN stays in the lower part.)
+        auto cut = [](float v) { return (__float_as_uint(v) - (v != 0.f)) >> 16; };
+        const uint32_t upper[2] = {cut(t[e]), cut(t[e + 1])};
+        o[e >> 1] = upper[0] | upper[1] << 16;
+        o[2 + (e >> 1)] = f32_to_bf16_rne2(t[e] - bf16_bits_to_f32(upper[0]), t[e + 1] - bf16_bits_to_f32(upper[1]));
     }
     return o;
 }
