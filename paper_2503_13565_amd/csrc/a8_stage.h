@@ -26,10 +26,10 @@ constexpr int piece_offset(int piece, int chunks, int rows, int row_bytes)
     return (piece_row(piece, chunks) * row_bytes + piece_chunk(piece, chunks) * 16) | past(rows - 1, piece_row(piece, chunks));
 }
 
-// The phase from step `step` on, of `steps`; a step is `step_bytes` of a row.  The scalar offset (of a phase behind the last: 0, as `steps` steps may be
-// more than a descriptor of a row or two has), and the first chunk of the row.
-constexpr int phase_from(int step, int steps, int step_bytes) { return step < steps ? step * step_bytes : 0; }
-constexpr int phase_chunk(int step, int steps, int step_bytes) { return (step < steps ? step : steps) * (step_bytes / 16); }
+// The phase from step `step` on, of `steps`; a step is `step_bytes` of a row.  The scalar offset (of a phase behind the last: the last step's, as `steps`
+// steps may be more than a descriptor of a row or two has), and the first chunk of the row.
+constexpr int phase_from(int step, int steps, int step_bytes) { return (step < steps ? step : steps - 1) * step_bytes; }
+constexpr int phase_chunk(int step, int step_bytes) { return step * (step_bytes / 16); }
 
 }  // namespace a8
 }  // namespace mxfp4

@@ -68,9 +68,9 @@ __global__ __launch_bounds__(512, 2) void w4a8_mid_kernel(const uint8_t* __restr
         for (int c = decltype(quarter)::value; c < C; c += 4) {
             const int u = c * 8 + wave;
             if (u < kX)
-                direct(lds_at + b * kBuf + u * 1024, off[c] | past((k >> 4) - 1, phase_chunk(t, steps, 128) + chunk[c]), rx, phase_from(t, steps, 128));
+                direct(lds_at + b * kBuf + u * 1024, off[c] | past((k >> 4) - 1, phase_chunk(t, 128) + chunk[c]), rx, phase_from(t, steps, 128));
             else
-                direct(lds_at + (u < kUnits ? b * kBuf + u * 1024 : D * kBuf + 2048 * kScaleUnits), off[c] | past(nblk - 1, phase_chunk(t, steps, 64) + chunk[c]),
+                direct(lds_at + (u < kUnits ? b * kBuf + u * 1024 : D * kBuf + 2048 * kScaleUnits), off[c] | past(nblk - 1, phase_chunk(t, 64) + chunk[c]),
                        rq, phase_from(t, steps, 64));
         }
     };

@@ -20,7 +20,7 @@ extern "C" int walk(int rows, int have, int row_bytes, int steps, int step_bytes
     const unsigned bytes = (unsigned)(have * row_bytes);
     for (int p = 0; p < (steps + s - 1) / s + ahead; ++p) {
         *phase = p;
-        const int from = phase_from(p * s, steps, step_bytes), first = phase_chunk(p * s, steps, step_bytes);
+        const int from = phase_from(p * s, steps, step_bytes), first = phase_chunk(p * s, step_bytes);
         if (from < 0 || (unsigned)from > bytes)
             return 1;
         for (int piece = 0; piece < rows * chunks; ++piece) {
