@@ -80,3 +80,89 @@ def test_product_of_more_weight_rows_than_a_launch_has(m, gate):
         off = off + (plain.ROUND + plain.STEP * gate) * z.abs()
         bad = torch.nonzero(~((y[:, lo : lo + z.shape[1]].double() - z.double()).abs() <= off.double()))
         assert not len(bad), "%d off behind %d, first at %r: %r for %r" % (len(bad), lo, bad[0].tolist(), float(y[bad[0][0], lo + bad[0][1]]), float(z[tuple(bad[0])]))
+
+
+BLOCKS = [(17, 66), (17, 8194), (35, 8197), (98, 8195), (227, 8194), (258, 7237), (449, 8201), (1025, 7170)]     # every block where K is some thousands
+
+
+def _whole(shape, most, gen):
+    """Whole numbers -most .. most (at most 4) and half of them zeros: as values, as E4M3 codes, as E2M1 codes."""
+    v = torch.randint(-most, most + 1, shape, generator=gen, device=DEV)
+    v = torch.where(torch.rand(shape, generator=gen, device=DEV) < 0.5, 0, v)
+    eight = torch.tensor([0, 0x38, 0x40, 0x44, 0x48], dtype=torch.uint8, device=DEV)[v.abs()] | (v < 0).to(torch.uint8) << 7
+    four = torch.tensor([0, 2, 4, 5, 6], dtype=torch.uint8, device=DEV)[v.abs()] | (v < 0).to(torch.uint8) << 3
+    return v.double(), eight, four
+
+
+@pytest.mark.parametrize("k", [160, 2080, 4128, 16416])
+@pytest.mark.parametrize("m,n", BLOCKS)
+def test_product_of_whole_numbers(m, n, k):
+    """Whole numbers under scales of 1/2 to 2: products are multiples of 1/4, and eight neighbours, which share their scales, are nothing that the instruction
+    cuts; sums of magnitudes stay below 2^23 of those, so FP32 holds every sum on the way, and every output is the exact sum rounded once."""
+    gen = torch.Generator(device=DEV).manual_seed(m + n + k)
+    (x, x8, _), (w, _, w4) = _whole((m, k), 4, gen), _whole((n, k), 4, gen)
+    xs, ws = (torch.randint(126, 129, (rows, k // 32), generator=gen, device=DEV) for rows in (m, n))
+    q = w4[:, 0::2] | w4[:, 1::2] << 4
+    y = binding.mxfp4_w4a8_gemm(x8, xs.to(torch.uint8), q, ws.to(torch.uint8))
+    x *= torch.exp2(xs.double() - 127).repeat_interleave(32, dim=1)
+    w *= torch.exp2(ws.double() - 127).repeat_interleave(32, dim=1)
+    want = x @ w.T
+    assert 4 * 64 * k < 2 ** 23 and torch.equal(want, want.float().double())
+    want = want.to(torch.float32).to(torch.bfloat16)
+    bad = torch.nonzero(y != want)
+    assert not len(bad), "%d off, first at %r: %r for %r" % (len(bad), bad[0].tolist(), float(y[tuple(bad[0])]), float(want[tuple(bad[0])]))
+
+
+@pytest.mark.parametrize("k", [160, 4128])
+@pytest.mark.parametrize("m,n", BLOCKS)
+def test_product_of_every_scale_byte(m, n, k):
+    """A row has a number in one place, weights are 1 and -1, and scale bytes are any: every output is the product of the two scales of that place's block,
+    exact in BF16.  Rows that hold a NaN or the byte 0xFF, and weight rows with that byte, are NaN, and no others."""
+    gen = torch.Generator(device=DEV).manual_seed(m + n + k)
+    rows, nblk = torch.arange(m, device=DEV), k // 32
+    at = (rows * 32 + rows % 32) % k
+    x8 = torch.zeros((m, k), dtype=torch.uint8, device=DEV)
+    x8[rows, at] = 0x38
+    q = torch.randint(0, 4, (n, k // 2), generator=gen, device=DEV)
+    q = (0x22 | (q & 1) << 3 | (q & 2) << 6).to(torch.uint8)
+    xs, ws = (torch.randint(67, 188, (r, nblk), generator=gen, device=DEV) for r in (m, n))        # (2^-60 .. 2^60: any two make a BF16 number)
+    xs[:, nblk // 2], ws[:, nblk // 3] = 70, 187
+    sign = torch.where(q.long()[:, at // 2] >> (3 + 4 * (at % 2)) & 1 == 1, -1.0, 1.0)
+    want = (sign * torch.exp2((xs[rows, at // 32][None] + ws[:, at // 32] - 254).double())).T
+    assert torch.equal(want, want.to(torch.bfloat16).double())
+    y = binding.mxfp4_w4a8_gemm(x8, xs.to(torch.uint8), q, ws.to(torch.uint8))
+    assert torch.equal(y.double(), want)
+    xs[m // 3, 0], xs[m - 1, nblk - 1], ws[0, nblk - 1], ws[n - 1, 0], ws[n // 2, nblk // 2] = 255, 255, 255, 255, 255
+    x8[m // 2, k - 1] = 0xFF
+    want[[m // 3, m - 1, m // 2]] = torch.nan
+    want[:, [0, n - 1, n // 2]] = torch.nan
+    y = binding.mxfp4_w4a8_gemm(x8, xs.to(torch.uint8), q, ws.to(torch.uint8)).double()
+    assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(), want.nan_to_num())
+
+
+@pytest.mark.parametrize("m,n", BLOCKS)
+def test_product_in_place_of_a_strided_residual(m, n):
+    k = 2272
+    x8, xs = binding.mxfp4_e4m3_direct_cast(_bf16((m, k), 1))
+    q, s = binding.mxfp4_direct_cast(_bf16((n, k), 2, 0.05, 4.0))
+    r = _bf16((m, n), 3)
+    want = binding.mxfp4_w4a8_gemm(x8, xs, q, s, residual=r)
+    plain.near(want, *plain.product(x8, xs, q, s, residual=r, device=DEV))
+    for extra in (3, 16 - n % 8):                               # rows at odd addresses, and where whole pieces are aligned
+        held = torch.full((m, n + extra), float("nan"), dtype=torch.bfloat16, device=DEV)
+        y = held[:, :n]
+        y.copy_(r)
+        assert binding.mxfp4_w4a8_gemm(x8, xs, q, s, residual=y, y=y) is y and torch.equal(y, want)
+        assert bool(held[:, n:].isnan().all())
+
+
+def test_calls_of_no_rows():
+    """Nothing to do for the norm and the adapters; the product refuses it, as the other products do."""
+    x, w = torch.empty((0, 64), dtype=torch.bfloat16, device=DEV), torch.ones(64, dtype=torch.bfloat16, device=DEV)
+    got = binding.mxfp4_rms_norm(x, w, residual=x.clone(), out="both")
+    assert got.y.shape == got.total.shape == got.q8.shape == (0, 64) and got.s.shape == (0, 2)
+    a, b = torch.ones((2, 8, 64), dtype=torch.bfloat16, device=DEV), torch.ones((2, 24, 8), dtype=torch.bfloat16, device=DEV)
+    assert binding.mxfp4_lora(x, a, b, torch.empty(0, dtype=torch.int32, device=DEV)).shape == (0, 24)
+    q, s = binding.mxfp4_direct_cast(_bf16((8, 64), 1))
+    with pytest.raises(binding.Mxfp4Error, match="M=0"):
+        binding.mxfp4_w4a8_gemm(got.q8, got.s, q, s)
