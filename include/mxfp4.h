@@ -421,7 +421,8 @@ int mxfp4_kv_copy_pages(const mxfp4_kv_cache* cache, const int32_t* src, const i
  * aligned; eps finite and not negative.  M may be 0 (no-op).  sum and y may each be x or the residual itself (same row
  * stride), not each other; any other overlap is not allowed.
  * Any finite inputs give finite rows in the BF16 range that the formula says, also where squares leave FP32's range.  A row that
- * holds NaN is NaN; infinite elements make themselves NaN and the others 0; zeros with eps = 0 are NaN.
+ * holds NaN is NaN; infinite elements make themselves NaN and the others 0; zeros with eps = 0 are NaN.  (h / sqrt(..) is an FP32 number before
+ * the weight: what is below 2^-126 there has fewer bits, whatever the weight.)
  */
 int mxfp4_rms_norm(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, const void* residual_bf16, int64_t ldr,
                    const void* weight_bf16, float eps, void* sum_bf16, int64_t lds, void* y_bf16, int64_t ldy,
@@ -437,7 +438,8 @@ int mxfp4_rms_norm(const void* x_bf16, int64_t M, int64_t K, int64_t ldx, const 
  *   x_e4m3, x_scales_e8m0  in  E4M3 codes uint8 [M, K] (16-byte aligned), scale bytes [M, K/32] (4-byte aligned)
  *   q_packed, scales_e8m0, bias_bf16, act, residual_bf16, ldr, y_bf16, ldy   as in mxfp4_woq_gemm_fused
  * M, N >= 1, K a positive multiple of 32, at most MXFP4_MAX_K.  A scale byte 0xFF or a NaN code makes what it meets NaN: the row m of x or
- * the column n of w that holds it.  The summation order is fixed per (M, N, K), not specified.
+ * the column n of w that holds it.  The summation order is fixed per (M, N, K), not specified.  (At one row, and mostly at two, mxfp4_woq_gemm with
+ * the BF16 rows takes less time.)
  */
 int mxfp4_w4a8_gemm(const void* x_e4m3, const void* x_scales_e8m0, int64_t M,
                     const void* q_packed, const void* scales_e8m0, int64_t N, int64_t K,

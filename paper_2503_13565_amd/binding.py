@@ -1403,7 +1403,8 @@ def mxfp4_rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, resid
 def mxfp4_w4a8_gemm(x8: torch.Tensor, xs: torch.Tensor, q: torch.Tensor, s: torch.Tensor, bias: Optional[torch.Tensor] = None,
                     act: int = ACT_NONE, residual: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The product of 8-bit rows (``x8 [M, K]``, ``xs [M, K/32]`` from :func:`mxfp4_rms_norm` or :func:`mxfp4_e4m3_direct_cast`) with MXFP4
-    weights, with bias, gate and residual add behind it as in :func:`mxfp4_woq_gemm_fused`; ``residual`` may be ``y`` itself."""
+    weights, with bias, gate and residual add behind it as in :func:`mxfp4_woq_gemm_fused`; ``residual`` may be ``y`` itself.  (At
+    one row, and mostly at two, the product of the BF16 rows takes less time.)"""
     if y is None:
         got = _layer_host().w4a8(x8, xs, q, s, bias, act, residual)
         if got is not None:

@@ -17,8 +17,9 @@
 //   - XR rows of x are held; with fewer than 16, the instruction's other columns read them again, and are not stored.
 //   - The scale bytes of the workgroup's rows are one piece of memory, which is copied at the start; a lane reads its byte.
 //   - What lies past K loads as zeros, under the row's last scale (which is NaN only where the row is).
-// Bound by the weights' way from memory: one row x 12288 x 4096 7.5 us (27 MB, 5.4 us at a copy's rate), nine rows x 22016 x 4096 with the gate 10.6
-// (48 MB, 9.7): the start, the first loads and the last sums are the rest.
+// Bound by the start, the first loads and the last sums of a workgroup, and by the weights' way from memory: one row x 12288 x 4096 7.2 us, 8.4 where the weights
+// are in no cache (27 MB, 3.8 us at the rate of a kernel that only reads; the decode kernel of BF16 rows 6.7), nine rows x 22016 x 4096 with the gate 10.5 and
+// 12.4 (48 MB, 6.9).
 #include "gemm_a8.h"
 
 namespace mxfp4 {

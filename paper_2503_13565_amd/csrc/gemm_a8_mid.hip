@@ -8,8 +8,9 @@
 // around them: a row of K / 32 bytes may start anywhere, a load starts at a dword; 80 bytes from row to row put two lanes on a bank), and a lane reads a
 // step's four in two dwords and moves its own to the bytes that the instruction names.
 // Bound by the walk of each block, and for larger ones by the lines that a unit gets from beyond its die's cache (80 to 90 bytes a ns).  77 rows x
-// 4096 x 11008 take 14.4 us in 192 blocks of 32 x 64 (24 MB, 5.3 us at a copy's rate): start, first phase and end are 4.9, and in the 21 phases behind it
-// loads, scales and matrix instructions wait for each other in part (each left out alone saves 3.8, 2.5 and 3.1).  No gain: four phases in the
+// 4096 x 11008 take 14.4 us in 192 blocks of 32 x 64, 16.4 where the weights are in no cache (25 MB, 3.8 us at the rate of a kernel that only reads): start, first
+// phase and end are 4.9, and in the 21 phases behind it loads, scales and matrix instructions wait for each other in part (each left out alone saved 3.8, 2.5 and
+// 3.1 of the 15.8 before the loads went out in quarters); 42 % of the LDS's active cycles are conflicts.  No gain: four phases in the
 // LDS, eight waves along K, sixteen waves; K cut across workgroups with a second kernel that adds was slower (17 to 18 us).
 #include "block_out.h"
 #include "gemm_a8.h"
